@@ -294,6 +294,116 @@ ozk_status ozk_stage_mma_probe(const uint8_t* P, const uint8_t* Q, int64_t K, in
  * registered workspace of at least 192 KiB. */
 ozk_status ozk_stage_wait_probe(void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * 8-bit operands: quantisation, the block-scaled product, AdamW.  Not in the paper: the forms in
+ * which a model's layers are multiplied and updated on the same tensor cores.
+ *
+ * Unlike the calls above, matrices here are ROW-MAJOR (element (r,c) at ptr[r*ld + c], strides in
+ * elements), as activations and weights are stored.  Codes are E4M3 bytes (sign, 4 exponent bits of
+ * bias 7, 3 fraction bits; 0x7F and 0xFF are NaN, there is no infinity, the largest value is 448).
+ * Every 128 elements along the axis that a product sums over share one scale.  Scales are UE8M0
+ * bytes c standing for 2^(c-127), c <= 254, unless a call says float.  A power-of-two scale makes
+ * x / scale exact, so a code is the one rounding of its element.
+ *
+ * Scale layouts ("lines" are the rows of the operand, or its columns, whichever the product does
+ * not sum over; block b covers elements 128 b .. 128 b + 127 of the summed axis):
+ *   LINES   one scale per line and block: byte ((b / 4) * lines + line) * 4 + b % 4, i.e. 32-bit words of four
+ *           blocks, [ceil(blocks/4)][lines]; ozk_fp8_line_scale_bytes() bytes, 4-byte aligned.  Bytes of the last
+ *           word beyond the last block are not read by the product and written as 127 by the quantiser.
+ *   TILES   one scale per 128 x 128 tile of the matrix as stored: byte (r / 128) * ceil(cols / 128) + c / 128.
+ *   LINES_F32, TILES_F32   32-bit floats, row-major [lines][blocks] and [ceil(rows/128)][ceil(cols/128)].
+ * ------------------------------------------------------------------------------------- */
+enum { OZK_F32 = 0, OZK_BF16 = 1 };
+enum { OZK_SCALE_LINES = 0, OZK_SCALE_TILES = 1, OZK_SCALE_LINES_F32 = 2, OZK_SCALE_TILES_F32 = 3 };
+
+/* Bytes of the LINES scales of an operand with this many lines and summed elements (0 on invalid arguments). */
+size_t ozk_fp8_line_scale_bytes(int64_t lines, int64_t k);
+
+/* Quantises X (rows x cols, OZK_F32 or OZK_BF16, ldx >= cols) with one scale per 1 x 128 block of a row
+ * (row_codes, row_scales: for products that sum over the columns; lines = rows), or per 128 x 1 block of a
+ * column (col_codes, col_scales: for products that sum over the rows, such as a weight gradient, which sums
+ * over the tokens; lines = cols), or both in one pass over X.  A pair that is not wanted is NULL, NULL.
+ *   scale = 2^max(-127, ceil(log2(amax / 448))) with amax the largest finite magnitude of the block (scale 1 for a block
+ *   of zeros); code = E4M3(x / scale), to nearest even; NaN and infinities become NaN and do not enter amax.
+ * Codes have leading dimensions row_ld, col_ld >= cols, multiples of 16, and 16-byte aligned bases; columns beyond
+ * `cols` are not written.  rows, cols = 0 are allowed. */
+ozk_status ozk_fp8_quantize_lines(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx,
+                                  uint8_t* row_codes, int64_t row_ld, uint8_t* row_scales,
+                                  uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales, void* stream);
+
+/* The same with one scale per 128 x 128 tile (TILES): weights, which products sum over either way. */
+ozk_status ozk_fp8_quantize_tiles(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx,
+                                  uint8_t* codes, int64_t ld, uint8_t* scales, void* stream);
+
+/* One operand of ozk_fp8_gemm.  contract_rows = 0: stored [lines][K], the product sums over the stored columns;
+ * 1: stored [K][lines], it sums over the stored rows (no transposed copy is made or needed).
+ * codes 16-byte aligned, ld a multiple of 16, at least the stored columns. */
+typedef struct {
+  const uint8_t* codes;
+  int64_t ld;
+  const void* scales;
+  int scale_kind;      /* OZK_SCALE_* */
+  int contract_rows;
+} ozk_fp8_operand;
+
+/* C[m,n] = sum_k A(m,k) B(n,k) on the scaled values, FP32 accumulation, C row-major M x N (OZK_F32 or OZK_BF16,
+ * ldc >= N), rounded once; accumulate = 1 (OZK_F32 only) adds the product to C instead.
+ *   UE8M0 scales (LINES or TILES on either operand): the tensor cores apply them.  Float scales: A is
+ *   LINES_F32 and B TILES_F32, both contract_rows = 0.  Other combinations return OZK_ERR_UNSUPPORTED.
+ *   A forward product y = x w^T has A = x (LINES), B = w (TILES); its input gradient dy w has A = dy (LINES), B = w
+ *   with contract_rows = 1; its weight gradient dy^T x has A = dy, B = x, both LINES with contract_rows = 1.
+ *   FP32 results: sums over more than 8192 are formed in ranges of at most 8192 that are added in FP32 in order,
+ *   because the tensor cores truncate when they accumulate.  Results do not depend on timing.
+ *   M, N, K = 0 are allowed (K = 0: C = 0, or unchanged with accumulate).  M, N, K < 2^31.
+ * workspace: device memory of ozk_fp8_gemm_workspace_bytes() (one size for all shapes), 256-byte aligned, whose first
+ * kibibyte has been cleared once (cudaMemset); NULL takes the registered one.  Calls that share it must be ordered by
+ * the caller.  A bounded device wait that expired is recorded at its start, see ozk_get_workspace_status().
+ * The call only enqueues kernels and, after one eager call, may be captured into a CUDA graph. */
+size_t ozk_fp8_gemm_workspace_bytes(void);
+ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B,
+                        void* C, int c_type, int64_t ldc, int accumulate,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ozk_get_async_status() for a workspace that was passed to a call rather than registered. */
+ozk_status ozk_get_workspace_status(void* workspace, void* stream);
+
+/* One tensor of an AdamW step: n elements, contiguous.  Element i of the optimiser's block b has i / 128 = b.
+ *   32-bit states: m, v are floats.  8-bit states: m holds E4M3 codes of the first moment and v E4M3 codes of the
+ *   ROOT r = sqrt(v) of the second (its 17.8 binades below a block's largest entry are 35 of v), m_scale and v_scale one
+ *   UE8M0 byte per block of 128. */
+typedef struct {
+  void* param;         /* options.param_type, updated */
+  const void* grad;    /* options.grad_type */
+  void* m;
+  void* v;
+  uint8_t* m_scale;    /* 8-bit states only, else NULL */
+  uint8_t* v_scale;
+  void* copy;          /* optional BF16 copy of an FP32 param, written */
+  int64_t n;
+} ozk_adamw_tensor;
+
+typedef struct {
+  int param_type, grad_type;   /* OZK_F32 or OZK_BF16 */
+  int state_bits;              /* 32 or 8 */
+  int stochastic;              /* 1: 8-bit roots and BF16 params are rounded up or down by a hash of (seed, tensor, element) */
+  uint32_t seed;
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;                /* 1 for the first step */
+  const float* grad_scale;     /* optional device scalar: gradients are multiplied by it (clipping, loss scale) */
+  const int* skip;             /* optional device flag: nonzero leaves everything unchanged (overflow in the gradients) */
+} ozk_adamw_options;
+
+/* One AdamW step over `count` tensors (host array) in one launch per 448 of them, all FP32 arithmetic:
+ *   g' = g grad_scale;  m' = beta1 m + (1 - beta1) g';  v' = beta2 v + (1 - beta2) g'^2;  r = sqrt(v')
+ *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m' / (r / sqrt(1 - beta2^step) + eps)
+ * 8-bit states are then rounded to their block's scale as by the quantiser: m' to nearest, r to nearest or, with
+ * `stochastic`, up or down (a root that changes by less than half a unit per step would never change otherwise);
+ * a root that is not zero is stored as at least 2^-9 of its scale, so that m / (r + eps) stays bounded.  The hash is
+ * mix(i ^ mix(index of the tensor + 1) ^ mix(seed)), mix(x): x ^= x>>16, x *= 0x7feb352d, x ^= x>>15, x *= 0x846ca68b,
+ * x ^= x>>16; the root uses its upper 16 bits, a BF16 parameter the lower 16.
+ * Non-finite gradients give non-finite (8-bit: NaN) values in their own element only.  No tensor may overlap another. */
+ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t count, const ozk_adamw_options* options, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

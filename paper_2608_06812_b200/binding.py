@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char, c_char_p, c_int, c_int64, c_size_t, c_void_p
+from ctypes import c_char, c_char_p, c_double, c_int, c_int64, c_size_t, c_uint32, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libozk.so")
@@ -25,6 +25,24 @@ OZK_ERR_DEVICE_TIMEOUT = -6
 OZK_MIN_MODULI, OZK_MAX_MODULI, OZK_DEFAULT_MODULI = 2, 27, 19
 OZK_CHUNK_K, OZK_MAX_K = 131072, 2097152
 OZK_MAX_EXTENDED_BITS = 62
+OZK_F32, OZK_BF16 = 0, 1
+OZK_SCALE_LINES, OZK_SCALE_TILES, OZK_SCALE_LINES_F32, OZK_SCALE_TILES_F32 = 0, 1, 2, 3
+
+
+class ozk_fp8_operand(ctypes.Structure):
+    _fields_ = [("codes", c_void_p), ("ld", c_int64), ("scales", c_void_p), ("scale_kind", c_int), ("contract_rows", c_int)]
+
+
+class ozk_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
+                ("copy", c_void_p), ("n", c_int64)]
+
+
+class ozk_adamw_options(ctypes.Structure):
+    _fields_ = [("param_type", c_int), ("grad_type", c_int), ("state_bits", c_int), ("stochastic", c_int), ("seed", c_uint32),
+                ("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("weight_decay", c_double), ("step", c_int64),
+                ("grad_scale", c_void_p), ("skip", c_void_p)]
+
 
 # name -> (restype, argtypes): every symbol include/ozk.h declares
 SIGNATURES = {
@@ -57,6 +75,13 @@ SIGNATURES = {
     "ozk_stage_gemm_cycles": (c_int, [c_void_p]),
     "ozk_stage_set_karatsuba": (c_int, [c_int]),
     "ozk_stage_timing_read": (c_int, [c_void_p]),
+    "ozk_get_workspace_status": (c_int, [c_void_p, c_void_p]),
+    "ozk_fp8_line_scale_bytes": (c_size_t, [c_int64, c_int64]),
+    "ozk_fp8_quantize_lines": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "ozk_fp8_quantize_tiles": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
+    "ozk_fp8_gemm_workspace_bytes": (c_size_t, []),
+    "ozk_fp8_gemm": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
+    "ozk_adamw_step": (c_int, [c_void_p, c_int64, c_void_p, c_void_p]),
     "ozk_stage_mma_probe": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
 }
 
@@ -215,3 +240,33 @@ def ozk_dgemm_host_workspace_bytes(M: int, N: int, K: int, num_moduli: int) -> i
 def ozk_dgemm_host(M, N, K, A, lda, B, ldb, C, ldc, num_moduli, stream=0) -> int:
     """A, B, C are HOST addresses (pinned memory for full speed)."""
     return lib().ozk_dgemm_host(M, N, K, A, lda, B, ldb, C, ldc, num_moduli, stream)
+
+
+def ozk_get_workspace_status(workspace, stream=0) -> int:
+    return lib().ozk_get_workspace_status(workspace, stream)
+
+
+def ozk_fp8_line_scale_bytes(lines: int, k: int) -> int:
+    return lib().ozk_fp8_line_scale_bytes(lines, k)
+
+
+def ozk_fp8_quantize_lines(rows, cols, X, x_type, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream=0) -> int:
+    return lib().ozk_fp8_quantize_lines(rows, cols, X, x_type, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream)
+
+
+def ozk_fp8_quantize_tiles(rows, cols, X, x_type, ldx, codes, ld, scales, stream=0) -> int:
+    return lib().ozk_fp8_quantize_tiles(rows, cols, X, x_type, ldx, codes, ld, scales, stream)
+
+
+def ozk_fp8_gemm_workspace_bytes() -> int:
+    return lib().ozk_fp8_gemm_workspace_bytes()
+
+
+def ozk_fp8_gemm(M, N, K, A, B, C, c_type, ldc, accumulate=0, workspace=None, workspace_bytes=0, stream=0) -> int:
+    """A, B: ozk_fp8_operand structures."""
+    return lib().ozk_fp8_gemm(M, N, K, ctypes.byref(A), ctypes.byref(B), C, c_type, ldc, accumulate, workspace, workspace_bytes, stream)
+
+
+def ozk_adamw_step(tensors, count, options, stream=0) -> int:
+    """tensors: a ctypes array of ozk_adamw_tensor; options: ozk_adamw_options."""
+    return lib().ozk_adamw_step(tensors, count, ctypes.byref(options), stream)

@@ -222,18 +222,20 @@ ozk_status ozk_set_workspace(void* dev_ptr, size_t bytes) {
   return OZK_OK;
 }
 
-ozk_status ozk_get_async_status(void* stream) {
-  if (!g_ws.ptr) return OZK_ERR_WORKSPACE;
+ozk_status ozk_get_workspace_status(void* workspace, void* stream) {
+  if (!workspace) return OZK_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (cudaStreamSynchronize(st) != cudaSuccess) return OZK_ERR_CUDA;
   StatusBlock sb;
-  if (cudaMemcpy(&sb, g_ws.ptr, sizeof sb, cudaMemcpyDeviceToHost) != cudaSuccess) return OZK_ERR_CUDA;
+  if (cudaMemcpy(&sb, workspace, sizeof sb, cudaMemcpyDeviceToHost) != cudaSuccess) return OZK_ERR_CUDA;
   if (sb.code != 0) {
     if (sb.code == OZK_ERR_DEVICE_TIMEOUT) fprintf(stderr, "ozk: bounded wait expired at 0x%x\n", sb.where);
-    cudaMemset(g_ws.ptr, 0, sizeof(StatusBlock));
+    cudaMemset(workspace, 0, sizeof(StatusBlock));
   }
   return sb.code;
 }
+
+ozk_status ozk_get_async_status(void* stream) { return ozk_get_workspace_status(g_ws.ptr, stream); }
 
 ozk_status ozk_stage_preprocess(int64_t M, int64_t N, int64_t K, const double* A, int64_t lda, const double* B,
                                 int64_t ldb, int num_moduli, int32_t* s_out, int32_t* t_out, int64_t* At_out,

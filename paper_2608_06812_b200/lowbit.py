@@ -1,0 +1,304 @@
+"""The 8-bit operators on torch tensors: quantisation by blocks of 128, the block-scaled product, AdamW.
+
+A linear layer in 8 bits:
+
+    x8, xt8 = quantize_lines(x, rows=True, cols=True)   # for the forward product and for the weight gradient
+    w8 = quantize_tiles(w)                              # one set of codes serves forward and backward
+    y = matmul(x8, w8)                                  # y  = x w^T
+    dx = matmul(quantize_lines(dy)[0], w8, over_rows=True)                       # dx = dy w
+    dw = matmul(quantize_lines(dy, rows=False, cols=True)[1], xt8, over_rows=True, dtype=torch.float32)   # dw = dy^T x
+
+`linear` is the same as a differentiable function.  Everything runs on the current stream of the tensors' device
+through libozk.so; arguments are checked here (ValueError) and in the library (OzkError), nothing falls back.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as ozk
+
+ROWS, COLS, TILES = "rows", "cols", "tiles"
+_TYPES = {torch.float32: ozk.OZK_F32, torch.bfloat16: ozk.OZK_BF16}
+
+
+def _up(n: int, m: int) -> int:
+    return -(-n // m) * m
+
+
+def _stream(device: torch.device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError(f"{what} is float32 or bfloat16, not {t.dtype}") from None
+
+
+def _need_cuda(t: torch.Tensor, what: str) -> None:
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on a GPU")
+
+
+# The product's scratch, one for each device and stream (calls on one stream are ordered, calls on two may overlap).
+_workspaces: dict[tuple[int, int], torch.Tensor] = {}
+
+
+def _workspace(device: torch.device, stream: int) -> torch.Tensor:
+    ws = _workspaces.get((device.index, stream))
+    if ws is None:
+        ws = torch.zeros(ozk.ozk_fp8_gemm_workspace_bytes(), dtype=torch.uint8, device=device)
+        _workspaces[device.index, stream] = ws
+    return ws
+
+
+def check_async(device: torch.device | None = None) -> None:
+    """Waits for the current stream and raises OzkError if a wait inside a product kernel on it had run out."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    stream = _stream(device)
+    if (device.index, stream) in _workspaces:
+        with torch.cuda.device(device):
+            ozk.check(ozk.ozk_get_workspace_status(_workspaces[device.index, stream].data_ptr(), stream), "product")
+
+
+class Fp8Matrix:
+    """A rows x cols matrix of E4M3 codes (uint8 [rows, ld], ld a multiple of 16) and its scales.
+
+    kind ROWS: a scale per 1 x 128 block, for products that sum over the columns; COLS: per 128 x 1 block, for products
+    that sum over the rows; TILES: per 128 x 128 tile, for either.  Scales are uint8 UE8M0 codes, [ceil(k/512), lines, 4]
+    for ROWS and COLS, [ceil(rows/128), ceil(cols/128)] for TILES; or float32 [rows, ceil(cols/128)] for ROWS and
+    [ceil(rows/128), ceil(cols/128)] for TILES."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, kind: str):
+        if kind not in (ROWS, COLS, TILES):
+            raise ValueError(f"kind is {ROWS!r}, {COLS!r} or {TILES!r}, not {kind!r}")
+        _need_cuda(codes, "codes")
+        if codes.dtype == torch.float8_e4m3fn:
+            codes = codes.view(torch.uint8)
+        if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[0] != rows or codes.shape[1] < cols:
+            raise ValueError(f"codes are uint8 or float8_e4m3fn [{rows}, at least {cols}], not {codes.dtype} {tuple(codes.shape)}")
+        ld = codes.stride(0) if rows > 1 else _up(max(codes.shape[1], 1), 16)
+        if rows and cols and (codes.stride(1) != 1 or ld % 16 or ld < cols or codes.data_ptr() % 16):
+            raise ValueError("codes lie in rows of a multiple of 16 bytes, at a multiple of 16 bytes")
+        floats = scales.dtype == torch.float32
+        br, bc = -(-rows // 128), -(-cols // 128)
+        if floats:
+            want = {ROWS: (rows, bc), TILES: (br, bc)}.get(kind)
+        else:
+            want = {ROWS: (-(-cols // 512), rows, 4), COLS: (-(-rows // 512), cols, 4), TILES: (br, bc)}[kind]
+        if (not floats and scales.dtype != torch.uint8) or scales.device != codes.device or not scales.is_contiguous() or want is None or tuple(scales.shape) != want:
+            raise ValueError(f"scales of {rows} x {cols} by {kind}: {scales.dtype} {tuple(scales.shape)}, wanted {want} on {codes.device}")
+        self.codes, self.scales, self.rows, self.cols, self.kind = codes, scales, rows, cols, kind
+        if floats:
+            code = ozk.OZK_SCALE_LINES_F32 if kind == ROWS else ozk.OZK_SCALE_TILES_F32
+        else:
+            code = ozk.OZK_SCALE_TILES if kind == TILES else ozk.OZK_SCALE_LINES
+        self.ld = ld
+        # the operand summed over its columns, and over its rows
+        self._operand = [ozk.ozk_fp8_operand(codes.data_ptr(), ld, scales.data_ptr(), code, over) for over in (0, 1)]
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, kind: str, device: torch.device | str = "cuda") -> "Fp8Matrix":
+        codes = torch.empty(rows, max(_up(cols, 16), 16), dtype=torch.uint8, device=device)
+        shape = {ROWS: (-(-cols // 512), rows, 4), COLS: (-(-rows // 512), cols, 4), TILES: (-(-rows // 128), -(-cols // 128))}[kind]
+        return cls(codes, torch.empty(shape, dtype=torch.uint8, device=device), rows, cols, kind)
+
+    def values8(self) -> torch.Tensor:
+        """The codes as torch's 8-bit type, [rows, cols], without the scales."""
+        return self.codes.view(torch.float8_e4m3fn)[:, :self.cols]
+
+    def scale_codes(self) -> torch.Tensor:
+        """Scales by stored block: [rows, blocks] (ROWS), [blocks, cols] (COLS), [row tiles, column tiles] (TILES)."""
+        if self.kind == TILES or self.scales.dtype == torch.float32:
+            return self.scales
+        k = self.cols if self.kind == ROWS else self.rows
+        s = self.scales.permute(0, 2, 1).reshape(-1, self.scales.shape[1])[:-(-k // 128)]
+        return s.T if self.kind == ROWS else s
+
+    def dequantize(self) -> torch.Tensor:
+        """Codes times scales in float32."""
+        s = self.scale_codes()
+        if s.dtype != torch.float32:
+            s = torch.where(s > 0, s.int() << 23, 1 << 22).view(torch.float32)
+        lines, blocks = {ROWS: (1, 128), COLS: (128, 1), TILES: (128, 128)}[self.kind]
+        full = s.repeat_interleave(lines, 0)[:self.rows].repeat_interleave(blocks, 1)[:, :self.cols]
+        return self.values8().float() * full
+
+
+def _input(x: torch.Tensor) -> tuple[int, int, int, int]:
+    _need_cuda(x, "x")
+    if x.dim() != 2:
+        raise ValueError(f"x has two dimensions, not {x.dim()}")
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError("the rows of x are contiguous")
+    return rows, cols, _type(x, "x"), x.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _output(q: Fp8Matrix, x: torch.Tensor, kind: str) -> None:
+    if (q.rows, q.cols, q.kind) != (*x.shape, kind) or q.scales.dtype != torch.uint8 or q.codes.device != x.device:
+        raise ValueError(f"out is a {x.shape[0]} x {x.shape[1]} Fp8Matrix by {kind} with UE8M0 scales on {x.device}")
+
+
+def quantize_lines(x: torch.Tensor, rows: "bool | Fp8Matrix | None" = True, cols: "bool | Fp8Matrix | None" = False):
+    """x [rows, cols] (float32 or bfloat16) by 1 x 128 blocks, by 128 x 1 blocks, or both in one pass over x.
+    `rows`, `cols`: whether that form is wanted, or an Fp8Matrix to write it to.  Returns the pair (None where not wanted)."""
+    r, c, kind, ld = _input(x)
+    by_rows = Fp8Matrix.empty(r, c, ROWS, x.device) if rows is True else rows or None
+    by_cols = Fp8Matrix.empty(r, c, COLS, x.device) if cols is True else cols or None
+    if by_rows is None and by_cols is None:
+        raise ValueError("neither rows nor columns are wanted")
+    args = []
+    for q, k in ((by_rows, ROWS), (by_cols, COLS)):
+        if q is None:
+            args += [None, 0, None]
+        else:
+            _output(q, x, k)
+            args += [q.codes.data_ptr(), q.ld, q.scales.data_ptr()]
+    with torch.cuda.device(x.device):
+        ozk.check(ozk.ozk_fp8_quantize_lines(r, c, x.data_ptr(), kind, ld, *args, _stream(x.device)), "quantize_lines")
+    return by_rows, by_cols
+
+
+def quantize_tiles(x: torch.Tensor, out: Fp8Matrix | None = None) -> Fp8Matrix:
+    """x [rows, cols] (float32 or bfloat16) by 128 x 128 tiles."""
+    r, c, kind, ld = _input(x)
+    q = Fp8Matrix.empty(r, c, TILES, x.device) if out is None else out
+    _output(q, x, TILES)
+    with torch.cuda.device(x.device):
+        ozk.check(ozk.ozk_fp8_quantize_tiles(r, c, x.data_ptr(), kind, ld, q.codes.data_ptr(), q.ld, q.scales.data_ptr(), _stream(x.device)), "quantize_tiles")
+    return q
+
+
+def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_rows: bool = False, dtype: torch.dtype = torch.bfloat16,
+           accumulate: bool = False) -> torch.Tensor:
+    """The product of two 8-bit matrices, each summed over the axis its scales run along: columns for ROWS, rows for COLS.
+    TILES serve either: `over_rows` says that b, if it is by tiles, is summed over its rows (and a by tiles over its rows if b is COLS).
+      matmul(x by ROWS, w by TILES)                   x w^T
+      matmul(dy by ROWS, w by TILES, over_rows=True)  dy w
+      matmul(dy by COLS, x by COLS)                   dy^T x
+    Returns a [lines of a, lines of b] tensor, `out` if given (float32 or bfloat16; float32 with accumulate, which adds)."""
+    a_over = a.kind == COLS or (a.kind == TILES and b.kind == COLS)
+    b_over = b.kind == COLS or (b.kind == TILES and over_rows)
+    m, k = (a.cols, a.rows) if a_over else (a.rows, a.cols)
+    n, kb = (b.cols, b.rows) if b_over else (b.rows, b.cols)
+    if k != kb:
+        raise ValueError(f"the operands are summed over {k} and {kb} elements")
+    device = a.codes.device
+    if b.codes.device != device:
+        raise ValueError("the operands are on two devices")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        if dtype not in _TYPES:
+            raise ValueError(f"the result is float32 or bfloat16, not {dtype}")
+        out = torch.empty(m, _up(n, 8), dtype=dtype, device=device)[:, :n]   # rows at 16-byte boundaries
+    elif out.shape != (m, n) or out.device != device or (n > 1 and out.stride(1) != 1):
+        raise ValueError(f"out is [{m}, {n}] on {device} with contiguous rows")
+    ctype = _type(out, "out")
+    stream = _stream(device)
+    ldc = out.stride(0) if m > 1 else max(n, 1)
+    with torch.cuda.device(device):
+        ws = _workspace(device, stream)
+        ozk.check(ozk.ozk_fp8_gemm(m, n, k, a._operand[a_over], b._operand[b_over], out.data_ptr(), ctype, ldc, 1 if accumulate else 0,
+                                   ws.data_ptr(), ws.numel(), stream), "matmul")
+    return out
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, w8):
+        flat = x.reshape(-1, x.shape[-1])
+        by_rows, by_cols = quantize_lines(flat, True, ctx.needs_input_grad[1])
+        ctx.x8, ctx.w8, ctx.shape, ctx.types = by_cols, w8, x.shape, (x.dtype, w.dtype)
+        return matmul(by_rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
+
+    @staticmethod
+    def backward(ctx, dy):
+        need_x, need_w = ctx.needs_input_grad[:2]
+        by_rows, by_cols = quantize_lines(dy.reshape(-1, dy.shape[-1]).contiguous(), need_x, need_w)
+        dx = matmul(by_rows, ctx.w8, over_rows=True, dtype=ctx.types[0]).reshape(ctx.shape) if need_x else None
+        dw = matmul(by_cols, ctx.x8, dtype=torch.float32).to(ctx.types[1]) if need_w else None
+        return dx, dw, None
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> torch.Tensor:
+    """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms).
+    x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps."""
+    return _Linear.apply(x, w, quantize_tiles(w.detach()) if w8 is None else w8)
+
+
+class AdamWTable:
+    """The tensors of an AdamW step: lists of equal length, entries of equal size, each contiguous.
+
+    params float32 or bfloat16, grads float32 or bfloat16; m, v float32, or uint8 E4M3 codes with m_scale, v_scale (uint8,
+    one for each 128 elements; v then holds the ROOT of the second moment); copies: optional bfloat16 copies of float32
+    params, written at every step.  The table holds the tensors' addresses (and keeps the tensors alive): build it once."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
+        lists = dict(params=list(params), grads=list(grads), m=list(m), v=list(v))
+        count = len(lists["params"])
+        for name, given in (("m_scale", m_scale), ("v_scale", v_scale), ("copies", copies)):
+            lists[name] = None if given is None else list(given)
+        for name, tensors in lists.items():
+            if tensors is None:
+                continue
+            if len(tensors) != count:
+                raise ValueError(f"{len(tensors)} {name} for {count} params")
+            for t, p in zip(tensors, lists["params"]):
+                _need_cuda(t, name)
+                want = -(-p.numel() // 128) if name.endswith("scale") else p.numel()
+                if t.numel() != want or not t.is_contiguous() or t.device != p.device or t.dtype != tensors[0].dtype or p.device != lists["params"][0].device:
+                    raise ValueError(f"{name}: contiguous tensors of one type, {want} elements here, on the device of the params")
+        first = {name: t[0].dtype if t else None for name, t in lists.items()}
+        if count:
+            if first["params"] not in _TYPES or first["grads"] not in _TYPES:
+                raise ValueError("params and grads are float32 or bfloat16")
+            eight = first["m"] == torch.uint8
+            if first["m"] != first["v"] or first["m"] not in (torch.uint8, torch.float32):
+                raise ValueError("m and v are both float32 or both uint8")
+            if eight != (lists["m_scale"] is not None) or eight != (lists["v_scale"] is not None) or (eight and (first["m_scale"], first["v_scale"]) != (torch.uint8,) * 2):
+                raise ValueError("m_scale and v_scale (uint8) go with 8-bit m and v")
+            if copies is not None and (first["params"] != torch.float32 or first["copies"] != torch.bfloat16):
+                raise ValueError("copies are bfloat16, of float32 params")
+        self.tensors, self.count = lists, count
+        self._table = (ozk.ozk_adamw_tensor * max(count, 1))()
+        self._options = ozk.ozk_adamw_options()
+        if count:
+            self.device = lists["params"][0].device
+            at = lambda name, i: None if lists[name] is None else lists[name][i].data_ptr()  # noqa: E731
+            for i in range(count):
+                self._table[i] = ozk.ozk_adamw_tensor(*(at(name, i) for name in ("params", "grads", "m", "v", "m_scale", "v_scale", "copies")), lists["params"][i].numel())
+            self._options.param_type, self._options.grad_type = _TYPES[first["params"]], _TYPES[first["grads"]]
+            self._options.state_bits = 8 if eight else 32
+
+    @classmethod
+    def zeros(cls, params, grads, bits: int = 8, copies=None) -> "AdamWTable":
+        """With states of zero, in 8 or 32 bits."""
+        params = list(params)
+        if bits not in (8, 32):
+            raise ValueError("states have 8 or 32 bits")
+        make = lambda: [torch.zeros(p.numel(), dtype=torch.uint8 if bits == 8 else torch.float32, device=p.device) for p in params]  # noqa: E731
+        scale = lambda: [torch.full((-(-p.numel() // 128),), 127, dtype=torch.uint8, device=p.device) for p in params] if bits == 8 else None  # noqa: E731
+        return cls(params, grads, make(), make(), scale(), scale(), copies)
+
+    def step(self, lr: float, step: int, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, seed: int | None = None,
+             grad_scale: torch.Tensor | None = None, skip: torch.Tensor | None = None) -> None:
+        """Step number `step` (1 is the first), in place.  seed: round 8-bit roots and bfloat16 params stochastically, with
+        another seed at each step; None: to nearest.  grad_scale: float32 scalar on the GPU that multiplies the gradients.
+        skip: int32 scalar on the GPU; if it is not zero, nothing changes."""
+        if self.count == 0:
+            return
+        for t, dtype, name in ((grad_scale, torch.float32, "grad_scale"), (skip, torch.int32, "skip")):
+            if t is not None and (t.dtype != dtype or t.numel() != 1 or t.device != self.device):
+                raise ValueError(f"{name} is one {dtype} on {self.device}")
+        o = self._options
+        o.stochastic, o.seed = (0, 0) if seed is None else (1, seed & 0xFFFFFFFF)
+        o.lr, (o.beta1, o.beta2), o.eps, o.weight_decay, o.step = lr, betas, eps, weight_decay, step
+        o.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
+        o.skip = None if skip is None else skip.data_ptr()
+        with torch.cuda.device(self.device):
+            ozk.check(ozk.ozk_adamw_step(ctypes.byref(self._table), self.count, o, _stream(self.device)), "AdamW step")
