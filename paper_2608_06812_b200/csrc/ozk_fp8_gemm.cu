@@ -1,63 +1,805 @@
-// The block-scaled product C[m,n] = sum_k A(m,k) sa(m,k/128) B(n,k) sb(n,k/128) of E4M3 operands.
+// The block-scaled product C[m,n] = sum_k A(m,k) sa(m,k/128) B(n,k) sb(n,k/128) of E4M3 operands on the tensor cores.
+//
+// UE8M0 scales: tcgen05.mma kind::mxf8f6f4 takes a scale byte for each operand row and 32 values of k.  Four
+//   instructions of one block of 128 are given the same byte, so that a 32-bit word of scale bytes per row serves
+//   512 values of k, and the product needs no arithmetic besides the tensor cores'.
+// FP32 scales: kind::f8f6f4 sums each block of 128 by itself; the epilogue warps multiply it by its scales and add it up
+//   in registers while the tensor cores form the next blocks.
+//
+// An operand whose k runs along its rows (contract_rows) is not transposed: its tiles are fetched with the 128-byte
+// rows along the lines, and the instruction reads them that way.
+//
+// Two kernels.  product_pair_kernel: a CTA pair forms a 256 x 256 tile of C (256 x 128 with FP32 scales), persistent,
+// TMA producer / MMA issuer / scale writers / epilogue in warps of their own; K is split over several pairs when there are
+// few tiles, the partial sums being joined in order by join_kernel.  product_rows_kernel: for few rows of C, where reading B
+// is what costs: B's lines become the 128 rows of the instruction, the rows of C its columns; the CTAs of a
+// cluster share a tile's K and add their sums through distributed shared memory.
+#include <cuda.h>
+
+#include <atomic>
+
 #include "ozk_fp8.cuh"
+#include "ozk_ptx.cuh"
+#include "ozk_wait.cuh"
 
 namespace ozk {
 namespace {
 
 using namespace fp8;
+using namespace ptx;
 
+// ---- operands -------------------------------------------------------------------------
 struct Operand {
   const uint8_t* codes;
   int64_t ld;
   const void* scales;
   int kind, contract_rows;
-  int lines;
-  int64_t tiles;   // tiles per stored row of tiles (TILES kinds)
+  int lines, blocks;   // blocks = ceil(K / 128)
+  int64_t tiles;       // tiles (TILES) or blocks per stored row of scales
 };
 
-__device__ __forceinline__ float operand_scale(const Operand& o, int line, int b) {
-  switch (o.kind) {
-    case OZK_SCALE_LINES: return scale_value(static_cast<const uint8_t*>(o.scales)[((int64_t)(b / 4) * o.lines + line) * 4 + b % 4]);
-    case OZK_SCALE_TILES: {
-      const int64_t i = o.contract_rows ? (int64_t)b * o.tiles + line / kBlock : (int64_t)(line / kBlock) * o.tiles + b;
-      return scale_value(static_cast<const uint8_t*>(o.scales)[i]);
-    }
-    case OZK_SCALE_LINES_F32: return static_cast<const float*>(o.scales)[(int64_t)line * o.tiles + b];
-    default: return static_cast<const float*>(o.scales)[(int64_t)(line / kBlock) * o.tiles + b];
-  }
+// Scale bytes of blocks 4 g .. 4 g + 3 of one line; 1 (127) where there is none.
+__device__ __forceinline__ uint32_t scale_word(const Operand& o, int line, int g) {
+  if (line >= o.lines) return 0x7F7F7F7Fu;
+  if (o.kind == OZK_SCALE_LINES) return __ldg(static_cast<const uint32_t*>(o.scales) + (int64_t)g * o.lines + line);
+  const uint8_t* s = static_cast<const uint8_t*>(o.scales);
+  const int64_t at = o.contract_rows ? (int64_t)(4 * g) * o.tiles + line / kBlock : (int64_t)(line / kBlock) * o.tiles + 4 * g;
+  const int64_t step = o.contract_rows ? o.tiles : 1;
+  uint32_t w = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) w |= (uint32_t)(4 * g + b < o.blocks ? __ldg(s + at + b * step) : 127u) << (8 * b);
+  return w;
 }
-__device__ __forceinline__ float operand_code(const Operand& o, int line, int k) {
-  const uint8_t c = o.contract_rows ? o.codes[(int64_t)k * o.ld + line] : o.codes[(int64_t)line * o.ld + k];
-  return unpack2(c).x;
+// Line and block of an FP32-scaled operand.
+__device__ __forceinline__ float scale_line_f32(const Operand& o, int line, int b) {
+  return line < o.lines ? __ldg(static_cast<const float*>(o.scales) + (int64_t)line * o.tiles + b) : 0.f;
+}
+__device__ __forceinline__ float scale_tile_f32(const Operand& o, int line, int b) {
+  return line < o.lines ? __ldg(static_cast<const float*>(o.scales) + (int64_t)(line / kBlock) * o.tiles + b) : 0.f;
 }
 
-// Plain form: one 32 x 32 tile of C per block, operands decoded into shared memory 32 values of k at a time.
-template <class T>
-__global__ void __launch_bounds__(256) product_kernel(Operand A, Operand B, int M, int N, int K, T* C, int64_t ldc, int accumulate) {
-  __shared__ float a[32][33], b[32][33];
-  const int m0 = blockIdx.y * 32, n0 = blockIdx.x * 32, tx = threadIdx.x % 32, ty = threadIdx.x / 32;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f}, total[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < K; k0 += 32) {
-    for (int i = ty; i < 32; i += 8) {
-      // the thread index that runs fastest follows the contiguous axis of each operand
-      const int la = A.contract_rows ? tx : i, ka = A.contract_rows ? i : tx;
-      const int lb = B.contract_rows ? tx : i, kb = B.contract_rows ? i : tx;
-      a[la][ka] = m0 + la < M && k0 + ka < K ? operand_code(A, m0 + la, k0 + ka) * operand_scale(A, m0 + la, (k0 + ka) / kBlock) : 0.f;
-      b[lb][kb] = n0 + lb < N && k0 + kb < K ? operand_code(B, n0 + lb, k0 + kb) * operand_scale(B, n0 + lb, (k0 + kb) / kBlock) : 0.f;
+// Coordinates of the tile of an operand that starts at `line` and block `b`: its 128-byte rows run along k, or along the lines.
+__device__ __forceinline__ void tile_at(int contract_rows, int line, int b, int& x, int& y) {
+  x = contract_rows ? line : b * kBlock;
+  y = contract_rows ? b * kBlock : line;
+}
+__device__ __forceinline__ uint64_t operand_desc(int contract_rows, uint32_t addr) {
+  return contract_rows ? smem_desc_sw128_lines(addr) : smem_desc_sw128(addr);
+}
+// Descriptor units (16 bytes) from one instruction's 32 values of k to the next.
+__device__ __forceinline__ uint32_t operand_step(int contract_rows) { return contract_rows ? 4096u >> 4 : 32u >> 4; }
+
+struct Output {
+  void* ptr;
+  int64_t ld;
+  int M, N;
+  int add;   // add to what is there (FP32)
+  int tma;   // 16-byte aligned rows: whole boxes by TMA
+};
+
+struct ProductParams {
+  Operand a, b;
+  Output out;          // C, or the partial sums [splits][M][ld] when splits > 1
+  int tiles_m, tiles_n, splits, groups;   // groups = ceil(K / 512)
+  int chunk_groups;    // groups summed in tensor memory before the sum is added to C in FP32
+  StatusBlock* status;
+};
+
+constexpr int kGroupK = 4 * kBlock;
+constexpr int kRangeGroups = 8192 / kGroupK;   // FP32 results: longest range summed by the tensor cores alone
+
+// ---- CTA-pair kernel --------------------------------------------------------------------
+constexpr int kTileM = 256;
+constexpr int kPairThreads = 14 * 32;   // producer, issuer, 4 scale warps, 8 epilogue warps
+constexpr int kMaxPairStages = 8;
+template <bool kFloat>
+struct PairShape {
+  static constexpr int kTileN = kFloat ? 128 : 256;
+  static constexpr int kABytes = 128 * kBlock;             // this CTA's 128 lines of A
+  static constexpr int kBBytes = kTileN / 2 * kBlock;      // and half of the lines of B
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = kFloat ? 8 : 6;
+  // Accumulators in tensor memory.  UE8M0: two of 256 columns that overlap in 32 (columns 224..255), so that both and the
+  // scale words fit 512: a new tile waits only until those 32 columns of the previous one have been read.
+  // FP32 scales: a ring of four, one per block of 128.
+  static constexpr int kBuffers = kFloat ? 4 : 2;
+  static constexpr int kBufferStep = kFloat ? 128 : 224;
+  [[maybe_unused]] static constexpr int kScaleCol = 480;                    // two sets of 4 columns for A, 8 for B
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * 4096 + 512 + 1024;
+};
+struct __align__(8) PairShared {
+  uint64_t full[kMaxPairStages], empty[kMaxPairStages];
+  uint64_t sf_full[2], sf_empty[2];
+  uint64_t acc_full[4], acc_empty[4];
+  uint64_t overlap, drained;
+  uint32_t tmem_base;
+  volatile int abort;
+};
+static_assert(sizeof(PairShared) <= 512, "room reserved behind the stages");
+
+struct Item {
+  int m0, n0, split, g_begin, g_end;
+};
+template <bool kFloat>
+__device__ __forceinline__ Item pair_item(const ProductParams& p, int item) {
+  // bands of eight row tiles sweep the column tiles: the pairs at work at one time share few panels of A and B
+  Item r;
+  const int tile = item / p.splits;
+  r.split = item - tile * p.splits;
+  const int band = 8 * p.tiles_n, g = tile / band, rem = tile - g * band;
+  const int rows = min(8, p.tiles_m - 8 * g);
+  r.n0 = rem / rows * PairShape<kFloat>::kTileN;
+  r.m0 = (8 * g + rem % rows) * kTileM;
+  r.g_begin = (int)((int64_t)r.split * p.groups / p.splits);
+  r.g_end = (int)((int64_t)(r.split + 1) * p.groups / p.splits);
+  return r;
+}
+
+// One warp's 32 rows x 128 bytes of results (32 FP32 or 64 BF16 columns; word w of lane r is bytes 4 w .. of row r)
+// through 4 KiB of staging.  Rows of the staging box are swizzled as the tensor map says: 16-byte piece j of row r at j ^ (r % 8).
+template <bool kBf16>
+__device__ __forceinline__ void store_box(const Output& o, const CUtensorMap* map, uint8_t* staging, int lane, const uint32_t (&w)[32], int m, int n, int z,
+                                          bool add) {
+  if (m >= o.M || n >= o.N) return;   // the same for all lanes
+  if (o.tma) {
+    if (lane == 0) bulk_wait_read();
+    __syncwarp();
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<uint4*>(staging + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  if (o.tma) {
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      if (!kBf16 && add) tma_add_3d(map, smem_u32(staging), n, m, z); else tma_store_3d(map, smem_u32(staging), n, m, z);
+      bulk_commit();
     }
-    __syncthreads();
-    for (int k = 0; k < 32; ++k)
-      for (int j = 0; j < 4; ++j) sum[j] = fmaf(a[ty + 8 * j][k], b[tx][k], sum[j]);
-    __syncthreads();
-    if ((k0 + 32) % 8192 == 0 || k0 + 32 >= K)   // ranges of 8192, added in order
-      for (int j = 0; j < 4; ++j) total[j] += sum[j], sum[j] = 0.f;
+    return;
   }
-  for (int j = 0; j < 4; ++j) {
-    const int m = m0 + ty + 8 * j, n = n0 + tx;
-    if (m >= M || n >= N) continue;
-    T* c = C + (int64_t)m * ldc + n;
-    store_element(c, accumulate ? load_element(c) + total[j] : total[j]);
+  __syncwarp();
+  const int rows = min(32, o.M - m);
+  for (int r = 0; r < rows; ++r) {   // a row at a time: consecutive lanes, consecutive elements
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(staging + r * 128 + (((lane / 4) ^ (r & 7)) * 16) + (lane % 4) * 4);
+    const int64_t at = (int64_t)(m + r) * o.ld;
+    if constexpr (kBf16) {
+      uint16_t* c = static_cast<uint16_t*>(o.ptr) + at;
+      if (n + 2 * lane < o.N) c[n + 2 * lane] = (uint16_t)v;
+      if (n + 2 * lane + 1 < o.N) c[n + 2 * lane + 1] = (uint16_t)(v >> 16);
+    } else if (n + lane < o.N) {
+      float* c = static_cast<float*>(o.ptr) + at + n + lane;
+      *c = add ? *c + __uint_as_float(v) : __uint_as_float(v);
+    }
   }
+  __syncwarp();
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <bool kFloat, bool kBf16>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
+                    const __grid_constant__ ProductParams p) {
+  using S = PairShape<kFloat>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* staging = tiles + S::kStages * S::kStageBytes;
+  PairShared* sh = reinterpret_cast<PairShared*>(staging + 8 * 4096);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+  const int items = p.tiles_m * p.tiles_n * p.splits;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map_a);
+    prefetch_tensormap(&map_b);
+    prefetch_tensormap(&map_c);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(smem_u32(&sh->full[s]), 1), mbar_init(smem_u32(&sh->empty[s]), 1);   // full: the leader's only
+    for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&sh->sf_full[s]), 8), mbar_init(smem_u32(&sh->sf_empty[s]), 1);      // 4 scale warps of each CTA
+    for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&sh->acc_full[s]), 1), mbar_init(smem_u32(&sh->acc_empty[s]), 16);   // 8 epilogue warps of each CTA
+    mbar_init(smem_u32(&sh->overlap), 8);
+    mbar_init(smem_u32(&sh->drained), 1);
+    sh->abort = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&sh->tmem_base), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();   // the peer's barriers are initialised before anything is sent to them
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+
+  if (warp == 0) {
+    // ------------------------------ TMA producer (both CTAs) ------------------------------
+    if (lane == 0) {
+      int stage = 0, issued = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int item = pair; item < items && ok; item += npairs) {
+        const Item it = pair_item<kFloat>(p, item);
+        const int b_end = min(4 * it.g_end, p.a.blocks);
+        for (int b = 4 * it.g_begin; b < b_end; ++b) {
+          if (!wait_bounded(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort, p.status, 0x800 + stage)) {
+            ok = false;
+            break;
+          }
+          const uint32_t full = map_to_cta(smem_u32(&sh->full[stage]), 0);
+          const uint32_t dst = smem_u32(tiles + stage * S::kStageBytes);
+          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh->full[stage]), 2 * S::kStageBytes);
+          int x, y;
+          tile_at(p.a.contract_rows, it.m0 + rank * 128, b, x, y);
+          tma_load_2d_pair(dst, &map_a, full, x, y);
+          tile_at(p.b.contract_rows, it.n0 + rank * (S::kTileN / 2), b, x, y);
+          tma_load_2d_pair(dst + S::kABytes, &map_b, full, x, y);
+          ++issued;
+          if (++stage == S::kStages) stage = 0, phase ^= 1u;
+        }
+      }
+      if (sh->abort && rank == 0) {   // copies in flight land before this CTA leaves
+        const uint64_t t0 = global_timer_ns();
+        for (int j = max(0, issued - S::kStages); j < issued; ++j)
+          while (!mbar_try_wait(smem_u32(&sh->full[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {
+          }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------ MMA issuer (leader only) ------------------------------
+    if (lane == 0 && rank == 0) {
+      int stage = 0;
+      uint32_t phase = 0, unit = 0, sf_unit = 0;
+      const int a_lines = p.a.contract_rows, b_lines = p.b.contract_rows;
+      const uint32_t a_step = operand_step(a_lines), b_step = operand_step(b_lines);
+      const uint32_t idesc = kFloat ? idesc_f8(kTileM, S::kTileN) : idesc_mxf8(kTileM, S::kTileN, a_lines, b_lines);
+      bool ok = true;
+      for (int item = pair; item < items && ok; item += npairs) {
+        const Item it = pair_item<kFloat>(p, item);
+        for (int g0 = it.g_begin; g0 < it.g_end && ok; g0 += p.chunk_groups) {
+          const int b_begin = 4 * g0, b_end = min(4 * min(it.g_end, g0 + p.chunk_groups), p.a.blocks);
+          uint32_t acc = 0;
+          if constexpr (!kFloat) {
+            const uint32_t buf = unit % S::kBuffers;
+            acc = tmem + buf * S::kBufferStep;
+            if (!wait_bounded(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x810)) { ok = false; break; }
+            if (unit && !wait_bounded(smem_u32(&sh->overlap), (unit - 1) & 1u, &sh->abort, p.status, 0x811)) { ok = false; break; }
+            tc_fence_after();
+          }
+          for (int b = b_begin; b < b_end; ++b) {
+            uint32_t sfa = 0, sfb = 0;
+            if constexpr (kFloat) {
+              const uint32_t buf = unit % S::kBuffers;
+              acc = tmem + buf * S::kBufferStep;
+              if (!wait_bounded(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x812)) { ok = false; break; }
+            } else {
+              const uint32_t set = sf_unit & 1u;
+              if ((b & 3) == 0 && !wait_bounded(smem_u32(&sh->sf_full[set]), (sf_unit >> 1) & 1u, &sh->abort, p.status, 0x813)) { ok = false; break; }
+              sfa = tmem + S::kScaleCol + set * 12;
+              sfb = sfa + 4;
+            }
+            if (!wait_bounded(smem_u32(&sh->full[stage]), phase, &sh->abort, p.status, 0x820 + stage)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
+            const uint64_t da = operand_desc(a_lines, base), db = operand_desc(b_lines, base + S::kABytes);
+#pragma unroll
+            for (uint32_t ks = 0; ks < 4; ++ks) {
+              if constexpr (kFloat)
+                mma_f8_pair(acc, da + ks * a_step, db + ks * b_step, idesc, ks ? 1u : 0u);
+              else
+                mma_mxf8_pair(acc, da + ks * a_step, db + ks * b_step, idesc | idesc_mxf8_block((uint32_t)b & 3u), sfa, sfb, (b > b_begin || ks) ? 1u : 0u);
+            }
+            mma_commit_pair(smem_u32(&sh->empty[stage]), (uint16_t)3);
+            if (++stage == S::kStages) stage = 0, phase ^= 1u;
+            if constexpr (kFloat) {
+              mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
+              ++unit;
+            } else if ((b & 3) == 3 || b + 1 == b_end) {
+              mma_commit_pair(smem_u32(&sh->sf_empty[sf_unit & 1u]), (uint16_t)3);
+              ++sf_unit;
+            }
+          }
+          if (!ok) break;
+          if constexpr (!kFloat) {
+            mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
+            ++unit;
+          }
+        }
+      }
+      if (sh->abort) {
+        mma_commit_pair(smem_u32(&sh->drained), (uint16_t)1);
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
+        }
+      }
+    }
+  } else if (warp < 6) {
+    // ------------------------------ scale words into tensor memory (both CTAs) ------------------------------
+    // Row r of an operand's 128 lines is lane r % 32, column r / 32 of its four columns, in every quarter of the lanes:
+    // each warp writes the quarter it may touch.  This CTA's 128 lines of A, all 256 of B.
+    if constexpr (!kFloat) {
+      const uint32_t at = tmem + (((uint32_t)(warp & 3) * 32u) << 16) + S::kScaleCol;
+      const uint32_t leader = map_to_cta(smem_u32(&sh->sf_full[0]), 0);
+      uint32_t unit = 0;
+      bool ok = true;
+      for (int item = pair; item < items && ok; item += npairs) {
+        const Item it = pair_item<kFloat>(p, item);
+        for (int g = it.g_begin; g < it.g_end; ++g, ++unit) {
+          uint32_t wa[4], wb0[4], wb1[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            wa[c] = scale_word(p.a, it.m0 + rank * 128 + c * 32 + lane, g);
+            wb0[c] = scale_word(p.b, it.n0 + c * 32 + lane, g);
+            wb1[c] = scale_word(p.b, it.n0 + 128 + c * 32 + lane, g);
+          }
+          const uint32_t set = unit & 1u;
+          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->sf_empty[set]), ((unit >> 1) & 1u) ^ 1u, &sh->abort, p.status, 0x830))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          tmem_st_32x4(at + set * 12, wa);
+          tmem_st_32x4(at + set * 12 + 4, wb0);
+          tmem_st_32x4(at + set * 12 + 8, wb1);
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(leader + set * 8);
+        }
+      }
+    }
+  } else {
+    // ------------------------------ epilogue (both CTAs) ----------------------------------
+    const uint32_t quad = (uint32_t)(warp & 3);
+    const int half = (warp - 6) >> 2;
+    uint8_t* box = staging + (warp - 6) * 4096;
+    const uint32_t lanes = tmem + ((quad * 32u) << 16);
+    const uint32_t empty0 = map_to_cta(smem_u32(&sh->acc_empty[0]), 0), overlap = map_to_cta(smem_u32(&sh->overlap), 0);
+    uint32_t unit = 0;
+    bool ok = true;
+    for (int item = pair; item < items && ok; item += npairs) {
+      const Item it = pair_item<kFloat>(p, item);
+      const int m = it.m0 + rank * 128 + (int)quad * 32;
+      if constexpr (kFloat) {
+        const int n = it.n0 + half * 64, row = m + lane;
+        const int b_begin = 4 * it.g_begin, b_end = min(4 * it.g_end, p.a.blocks);
+        float acc[64];
+#pragma unroll
+        for (int e = 0; e < 64; ++e) acc[e] = 0.f;
+        float sa = scale_line_f32(p.a, row, b_begin), sb = scale_tile_f32(p.b, it.n0, b_begin);
+        for (int b = b_begin; b < b_end; ++b, ++unit) {
+          const uint32_t buf = unit % S::kBuffers;
+          const float s = sa * sb;
+          if (b + 1 < b_end) sa = scale_line_f32(p.a, row, b + 1), sb = scale_tile_f32(p.b, it.n0, b + 1);
+          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x840))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          uint32_t d0[32], d1[32];
+          tmem_ld_32x32(lanes + buf * S::kBufferStep + half * 64, d0);
+          tmem_ld_32x32(lanes + buf * S::kBufferStep + half * 64 + 32, d1);
+          tmem_wait_ld();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(empty0 + buf * 8);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[e] = fmaf(__uint_as_float(d0[e]), s, acc[e]), acc[32 + e] = fmaf(__uint_as_float(d1[e]), s, acc[32 + e]);
+        }
+        if (!ok) break;
+        uint32_t w[32];
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) w[e] = pack_bf16(acc[2 * e], acc[2 * e + 1]);
+          store_box<true>(p.out, &map_c, box, lane, w, m, n, it.split, false);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(acc[32 * h + e]);
+            store_box<false>(p.out, &map_c, box, lane, w, m, n + 32 * h, it.split, p.out.add);
+          }
+        }
+      } else {
+        const int n = it.n0 + half * 128;
+        for (int g0 = it.g_begin; g0 < it.g_end; g0 += p.chunk_groups, ++unit) {
+          const uint32_t buf = unit % S::kBuffers;
+          const bool later = g0 > it.g_begin;   // a later range of the same tile is added to the earlier ones
+          if (later && p.out.tma && lane == 0) bulk_wait();
+          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x841))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t from = lanes + buf * S::kBufferStep + half * 128;
+          const bool shared_half = buf == 0 ? half == 1 : half == 0;   // holds the columns that the other accumulator shares
+          constexpr int kPieces = kBf16 ? 2 : 4, kWidth = kBf16 ? 64 : 32;
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            const int c = buf == 0 && half == 1 ? kPieces - 1 - i : i;   // those columns first
+            uint32_t w[32];
+            if constexpr (kBf16) {
+              uint32_t d0[32], d1[32];
+              tmem_ld_32x32(from + c * 64, d0);
+              tmem_ld_32x32(from + c * 64 + 32, d1);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                w[e] = pack_bf16(__uint_as_float(d0[2 * e]), __uint_as_float(d0[2 * e + 1]));
+                w[16 + e] = pack_bf16(__uint_as_float(d1[2 * e]), __uint_as_float(d1[2 * e + 1]));
+              }
+            } else {
+              tmem_ld_32x32(from + c * 32, w);
+              tmem_wait_ld();
+            }
+            if ((i == 0 && shared_half) || i == kPieces - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) {
+                if (i == 0 && shared_half) mbar_arrive_cluster(overlap);
+                if (i == kPieces - 1) mbar_arrive_cluster(empty0 + buf * 8);
+              }
+            }
+            store_box<kBf16>(p.out, &map_c, box, lane, w, m, n + c * kWidth, it.split, p.out.add || later);
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait();   // the staging memory is read until then
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();   // neither CTA leaves while the other may still signal its barriers
+  cluster_wait();
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc_pair(tmem, 512);
+  }
+}
+
+// C (+)= the partial sums of the K ranges, added in order.
+template <bool kBf16>
+__global__ void __launch_bounds__(256) join_kernel(const float* part, int splits, int M, int N, int64_t ld, void* C, int64_t ldc, int add) {
+  const int64_t total = (int64_t)M * N, stride = (int64_t)M * ld;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int m = (int)(i / N), n = (int)(i - (int64_t)m * N);
+    const float* q = part + (int64_t)m * ld + n;
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s) sum += q[s * stride];
+    if constexpr (kBf16) {
+      static_cast<__nv_bfloat16*>(C)[(int64_t)m * ldc + n] = __float2bfloat16_rn(sum);
+    } else {
+      float* c = static_cast<float*>(C) + (int64_t)m * ldc + n;
+      *c = add ? *c + sum : sum;
+    }
+  }
+}
+
+// ---- few rows of C --------------------------------------------------------------------
+constexpr int kRowsThreads = 6 * 32;   // producer, issuer, 4 warps for scales and epilogue
+template <int NT, bool kFloat>
+struct RowsShape {
+  static constexpr int kWBytes = 128 * kBlock;
+  static constexpr int kStageBytes = kWBytes + NT * kBlock;
+  static constexpr int kStages = NT == 128 ? 3 : 4;
+  static constexpr int kSets = 4;                                   // scale words of four groups in flight (UE8M0)
+  static constexpr int kBuffers = kFloat ? (NT == 128 ? 2 : 4) : 1; // accumulators, one per block of 128 (FP32 scales)
+  static constexpr int kNeeded = kFloat ? kBuffers * NT : NT + kSets * 8;
+  static constexpr int kCols = kNeeded <= 64 ? 64 : kNeeded <= 128 ? 128 : 256;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 512 + 4 * 2 * NT * 4 + 1024;
+  static_assert(NT * 128 * 4 <= kStages * kStageBytes, "the partial sums are exchanged in the stages' memory");
+};
+struct __align__(8) RowsShared {
+  uint64_t full[4], empty[4], sf_full[4], sf_empty[4], acc_full[4], acc_empty[4], drained;
+  uint32_t tmem_base;
+  volatile int abort;
+};
+static_assert(sizeof(RowsShared) <= 512, "room reserved behind the stages");
+
+__device__ __forceinline__ float load_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+
+// p.a: the few rows of C (lines of the instruction's column side), p.b: the lines that become its 128 rows.
+template <int NT, bool kFloat, class T>
+__global__ void __launch_bounds__(kRowsThreads)
+product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProductParams p) {
+  using S = RowsShape<NT, kFloat>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  RowsShared* sh = reinterpret_cast<RowsShared*>(tiles + S::kStages * S::kStageBytes);
+  float* block_scales = reinterpret_cast<float*>(tiles + S::kStages * S::kStageBytes + 512);   // [warp][2][NT]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank(), size = (int)cluster_size();
+  const int n0 = (int)(blockIdx.x / size) * 128;
+  const int g_begin = (int)((int64_t)rank * p.groups / size), g_end = (int)((int64_t)(rank + 1) * p.groups / size);
+  const int b_begin = 4 * g_begin, b_end = min(4 * g_end, p.a.blocks);
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map_x);
+    prefetch_tensormap(&map_w);
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1), mbar_init(smem_u32(&sh->empty[s]), 1);
+      mbar_init(smem_u32(&sh->sf_full[s]), 4), mbar_init(smem_u32(&sh->sf_empty[s]), 1);
+      mbar_init(smem_u32(&sh->acc_full[s]), 1), mbar_init(smem_u32(&sh->acc_empty[s]), 4);
+    }
+    mbar_init(smem_u32(&sh->drained), 1);
+    sh->abort = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&sh->tmem_base), S::kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+  float* sums = reinterpret_cast<float*>(tiles);   // [NT][128] once the operands have been consumed
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int issued = 0;
+      for (int b = b_begin; b < b_end; ++b, ++issued) {
+        const int stage = issued % S::kStages;
+        if (!wait_bounded(smem_u32(&sh->empty[stage]), ((uint32_t)(issued / S::kStages) & 1u) ^ 1u, &sh->abort, p.status, 0x900 + stage)) break;
+        const uint32_t dst = smem_u32(tiles + stage * S::kStageBytes), full = smem_u32(&sh->full[stage]);
+        mbar_arrive_expect_tx(full, S::kStageBytes);
+        int x, y;
+        tile_at(p.b.contract_rows, n0, b, x, y);
+        tma_load_2d(dst, &map_w, full, x, y);
+        tma_load_2d(dst + S::kWBytes, &map_x, full, b * kBlock, 0);
+      }
+      if (sh->abort) {   // copies in flight land before this CTA leaves
+        const uint64_t t0 = global_timer_ns();
+        for (int j = max(0, issued - S::kStages); j < issued; ++j)
+          while (!mbar_try_wait(smem_u32(&sh->full[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {
+          }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const int w_lines = p.b.contract_rows;
+      const uint32_t w_step = operand_step(w_lines);
+      const uint32_t idesc = kFloat ? idesc_f8(128, NT) : idesc_mxf8(128, NT, w_lines, 0);
+      bool ok = true;
+      for (int b = b_begin; b < b_end; ++b) {
+        const int i = b - b_begin, stage = i % S::kStages, buf = i % S::kBuffers, set = (i / 4) % S::kSets;
+        if (kFloat && !wait_bounded(smem_u32(&sh->acc_empty[buf]), ((uint32_t)(i / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x910)) { ok = false; break; }
+        if (!kFloat && i % 4 == 0 && !wait_bounded(smem_u32(&sh->sf_full[set]), (uint32_t)(i / 4 / S::kSets) & 1u, &sh->abort, p.status, 0x911)) { ok = false; break; }
+        if (!wait_bounded(smem_u32(&sh->full[stage]), (uint32_t)(i / S::kStages) & 1u, &sh->abort, p.status, 0x920 + stage)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
+        const uint64_t dw = operand_desc(w_lines, base), dx = smem_desc_sw128(base + S::kWBytes);
+#pragma unroll
+        for (uint32_t ks = 0; ks < 4; ++ks) {
+          if constexpr (kFloat)
+            mma_f8(tmem + buf * NT, dw + ks * w_step, dx + ks * 2u, idesc, ks ? 1u : 0u);
+          else
+            mma_mxf8(tmem, dw + ks * w_step, dx + ks * 2u, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
+        }
+        mma_commit(smem_u32(&sh->empty[stage]));
+        if (kFloat) mma_commit(smem_u32(&sh->acc_full[buf]));
+        if (!kFloat && (i % 4 == 3 || b + 1 == b_end)) mma_commit(smem_u32(&sh->sf_empty[set]));
+      }
+      if (!kFloat && ok) mma_commit(smem_u32(&sh->acc_full[0]));
+      if (sh->abort) {
+        mma_commit(smem_u32(&sh->drained));
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
+        }
+      }
+    }
+  } else {
+    const uint32_t quad = (uint32_t)(warp & 3);
+    const uint32_t lanes = tmem + ((quad * 32u) << 16);
+    const int line = (int)quad * 32 + lane;   // of the 128
+    bool ok = true;
+    if constexpr (kFloat) {
+      float acc[NT];
+#pragma unroll
+      for (int e = 0; e < NT; ++e) acc[e] = 0.f;
+      float* mine = block_scales + (warp - 2) * 2 * NT;
+      constexpr int kPer = (NT + 31) / 32;
+      float sx[kPer], sw = scale_tile_f32(p.b, n0, b_begin);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, lane + 32 * j, b_begin) : 0.f;
+      for (int b = b_begin; b < b_end; ++b) {
+        const int i = b - b_begin, buf = i % S::kBuffers;
+        float* s = mine + (i & 1) * NT;   // two, so that one barrier of the warp is enough
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+          if (lane + 32 * j < NT) s[lane + 32 * j] = sx[j] * sw;
+        __syncwarp();
+        if (b + 1 < b_end) {
+          sw = scale_tile_f32(p.b, n0, b + 1);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, lane + 32 * j, b + 1) : 0.f;
+        }
+        if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (uint32_t)(i / S::kBuffers) & 1u, &sh->abort, p.status, 0x930))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < NT / 16; ++c) {
+          uint32_t d[16];
+          tmem_ld_32x16(lanes + buf * NT + c * 16, d);
+          tmem_wait_ld();
+          if (c == NT / 16 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->acc_empty[buf]));
+          }
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(s + c * 16 + e);
+            acc[c * 16 + e] = fmaf(__uint_as_float(d[e]), f.x, acc[c * 16 + e]);
+            acc[c * 16 + e + 1] = fmaf(__uint_as_float(d[e + 1]), f.y, acc[c * 16 + e + 1]);
+            acc[c * 16 + e + 2] = fmaf(__uint_as_float(d[e + 2]), f.z, acc[c * 16 + e + 2]);
+            acc[c * 16 + e + 3] = fmaf(__uint_as_float(d[e + 3]), f.w, acc[c * 16 + e + 3]);
+          }
+        }
+      }
+      // every warp has seen the last block: all operands have been consumed, their memory takes the sums
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+      for (int e = 0; e < NT; ++e) sums[e * 128 + line] = acc[e];
+    } else {
+      for (int g = g_begin; g < g_end; ++g) {
+        const int i = g - g_begin, set = i % S::kSets;
+        uint32_t ww[4], wx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          ww[c] = scale_word(p.b, n0 + c * 32 + lane, g);
+          wx[c] = c * 32 < NT ? scale_word(p.a, c * 32 + lane, g) : 0x7F7F7F7Fu;
+        }
+        if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->sf_empty[set]), ((uint32_t)(i / S::kSets) & 1u) ^ 1u, &sh->abort, p.status, 0x931))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        tmem_st_32x4(lanes + NT + set * 8, ww);
+        tmem_st_32x4(lanes + NT + set * 8 + 4, wx);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->sf_full[set]));
+      }
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[0]), 0u, &sh->abort, p.status, 0x932));
+      if (ok) {
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < NT / 16; ++c) {
+          uint32_t d[16];
+          tmem_ld_32x16(lanes + c * 16, d);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sums[(c * 16 + e) * 128 + line] = __uint_as_float(d[e]);
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem, S::kCols);
+  }
+  // each CTA of the cluster joins its share of the sums, in the order of the ranges
+  const uint32_t local = smem_u32(sums);
+  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < p.out.M * 128; e += size * kRowsThreads) {
+    const int n = n0 + e % 128;
+    if (n >= p.out.N) continue;
+    float sum = 0.f;
+    for (int r = 0; r < size; ++r) sum += load_cluster_f32(map_to_cta(local + (uint32_t)e * 4u, (uint32_t)r));
+    T* c = static_cast<T*>(p.out.ptr) + (int64_t)(e / 128) * p.out.ld + n;
+    store_element(c, p.out.add ? load_element(c) + sum : sum);
+  }
+  cluster_arrive();   // no CTA leaves while another reads its sums
+  cluster_wait();
+}
+
+// ---- host side ------------------------------------------------------------------------
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static std::atomic<EncodeTiledFn> fn{nullptr};
+  EncodeTiledFn f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    void* sym = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess) return nullptr;
+    f = reinterpret_cast<EncodeTiledFn>(sym);
+    fn.store(f, std::memory_order_release);
+  }
+  return f;
+}
+// Tiles of an operand: `lines` x 128 values of k, rows of 128 bytes along k (or along the lines).  What lies outside reads as zero.
+bool operand_map(CUtensorMap* map, const Operand& o, int64_t K, int lines) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)(o.contract_rows ? o.lines : K), (cuuint64_t)(o.contract_rows ? K : o.lines)};
+  cuuint64_t strides[1] = {(cuuint64_t)o.ld};
+  cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)(o.contract_rows ? kBlock : lines)};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(o.codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool output_map(CUtensorMap* map, const Output& o, bool bf16, int splits) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t size = bf16 ? 2 : 4;
+  cuuint64_t dims[3] = {(cuuint64_t)o.N, (cuuint64_t)o.M, (cuuint64_t)splits};
+  cuuint64_t strides[2] = {(cuuint64_t)o.ld * size, (cuuint64_t)o.ld * size * (cuuint64_t)o.M};
+  cuuint32_t box[3] = {(cuuint32_t)(128 / size), 32, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, o.ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kMaxDevices = 64;
+// Raises a kernel's dynamic shared memory once per device.
+template <class K>
+bool raise_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices]) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
+  if (done[dev].load(std::memory_order_acquire)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  done[dev].store(true, std::memory_order_release);
+  return true;
+}
+
+template <bool kFloat, bool kBf16>
+bool launch_pair(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_c, const ProductParams& p, int pairs, cudaStream_t st) {
+  static std::atomic<bool> done[kMaxDevices];
+  auto kernel = product_pair_kernel<kFloat, kBf16>;
+  if (!raise_smem(kernel, PairShape<kFloat>::kSmem, done)) return false;
+  kernel<<<(unsigned)(2 * pairs), kPairThreads, PairShape<kFloat>::kSmem, st>>>(map_a, map_b, map_c, p);
+  return cudaGetLastError() == cudaSuccess;
+}
+
+template <int NT, bool kFloat, class T>
+bool launch_rows(const CUtensorMap& map_x, const CUtensorMap& map_w, const ProductParams& p, int tiles, int cluster, cudaStream_t st) {
+  static std::atomic<bool> done[kMaxDevices];
+  auto kernel = product_rows_kernel<NT, kFloat, T>;
+  if (!raise_smem(kernel, RowsShape<NT, kFloat>::kSmem, done)) return false;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * cluster), 1, 1);
+  cfg.blockDim = dim3(kRowsThreads, 1, 1);
+  cfg.dynamicSmemBytes = RowsShape<NT, kFloat>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, map_x, map_w, p) == cudaSuccess;
+}
+template <int NT>
+bool launch_rows_as(bool floats, bool bf16, const CUtensorMap& map_x, const CUtensorMap& map_w, const ProductParams& p, int tiles, int cluster, cudaStream_t st) {
+  if (floats)
+    return bf16 ? launch_rows<NT, true, __nv_bfloat16>(map_x, map_w, p, tiles, cluster, st) : launch_rows<NT, true, float>(map_x, map_w, p, tiles, cluster, st);
+  return bf16 ? launch_rows<NT, false, __nv_bfloat16>(map_x, map_w, p, tiles, cluster, st) : launch_rows<NT, false, float>(map_x, map_w, p, tiles, cluster, st);
 }
 
 bool check_operand(const ozk_fp8_operand* o, int64_t lines, int64_t k, Operand* out) {
@@ -66,11 +808,81 @@ bool check_operand(const ozk_fp8_operand* o, int64_t lines, int64_t k, Operand* 
   if (o->scale_kind < OZK_SCALE_LINES || o->scale_kind > OZK_SCALE_TILES_F32) return false;
   if (o->contract_rows != 0 && o->contract_rows != 1) return false;
   if (o->scale_kind != OZK_SCALE_TILES && (reinterpret_cast<uintptr_t>(o->scales) & 3)) return false;
-  *out = Operand{o->codes, o->ld, o->scales, o->scale_kind, o->contract_rows, (int)lines, ceil_div(cols, kBlock)};
+  *out = Operand{o->codes, o->ld, o->scales, o->scale_kind, o->contract_rows, (int)lines, (int)ceil_div(k, kBlock), ceil_div(cols, kBlock)};
   return true;
 }
 
-constexpr size_t kGemmWorkspace = 24u << 20;
+constexpr size_t kGemmStatusBytes = 1024;
+constexpr size_t kGemmWorkspace = 24u << 20;   // status, and the partial sums of at most one tile per CTA pair (74 x 256 KiB)
+
+// Few rows of C: the instruction's column side holds them, 16 to 128 at a time.
+ozk_status run_rows(ProductParams p, int64_t K, bool floats, bool bf16, cudaStream_t st) {
+  const int M = p.out.M, NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+  CUtensorMap map_x, map_w;
+  if (!operand_map(&map_x, p.a, K, NT) || !operand_map(&map_w, p.b, K, 128)) return OZK_ERR_CUDA;
+  const int tiles = (int)ceil_div(p.out.N, 128), sms = device_sm_count();
+  if (sms < 1) return OZK_ERR_CUDA;
+  // two CTAs fit a multiprocessor: split K over a cluster while that fills them
+  int cluster = 2 * sms / tiles;
+  cluster = cluster < 1 ? 1 : cluster > 8 ? 8 : cluster;
+  if (cluster > p.groups) cluster = p.groups;
+  bool ok;
+  switch (NT) {
+    case 16: ok = launch_rows_as<16>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
+    case 32: ok = launch_rows_as<32>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
+    case 64: ok = launch_rows_as<64>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
+    default: ok = launch_rows_as<128>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
+  }
+  return ok ? OZK_OK : OZK_ERR_CUDA;
+}
+
+ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t* workspace, cudaStream_t st) {
+  const int tile_n = floats ? 128 : 256;
+  const int64_t tm = ceil_div(p.out.M, kTileM), tn = ceil_div(p.out.N, tile_n);
+  if (tm * tn > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+  const int pairs = device_sm_count() / 2;
+  if (pairs < 1) return OZK_ERR_CUDA;
+  p.tiles_m = (int)tm, p.tiles_n = (int)tn;
+  const Output c = p.out;
+  // fewer tiles than half the pairs: split K so that each pair has one range of at least 1024
+  int splits = 1;
+  if (tm * tn * 2 <= pairs) {
+    splits = (int)(pairs / (tm * tn));
+    if (splits > p.groups / 2) splits = p.groups / 2;
+    if (splits < 1) splits = 1;
+  }
+  p.splits = splits;
+  const bool out_bf16 = bf16 && splits == 1;
+  p.chunk_groups = out_bf16 || floats ? p.groups : kRangeGroups;
+  if (splits > 1) {
+    p.out = Output{workspace + kGemmStatusBytes, round_up(c.N, 4), c.M, c.N, 0, 1};
+    if ((size_t)splits * c.M * p.out.ld * 4 + kGemmStatusBytes > kGemmWorkspace) return OZK_ERR_UNSUPPORTED;
+  }
+  CUtensorMap map_a, map_b, map_c;
+  if (!operand_map(&map_a, p.a, K, 128) || !operand_map(&map_b, p.b, K, tile_n / 2)) return OZK_ERR_CUDA;
+  if (p.out.tma) {
+    if (!output_map(&map_c, p.out, out_bf16, splits)) return OZK_ERR_CUDA;
+  } else {
+    map_c = map_a;   // not used
+  }
+  const int64_t items = tm * tn * splits;
+  if (items > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+  const int grid = (int)(items < pairs ? items : pairs);
+  const bool ok = floats ? (out_bf16 ? launch_pair<true, true>(map_a, map_b, map_c, p, grid, st) : launch_pair<true, false>(map_a, map_b, map_c, p, grid, st))
+                         : (out_bf16 ? launch_pair<false, true>(map_a, map_b, map_c, p, grid, st) : launch_pair<false, false>(map_a, map_b, map_c, p, grid, st));
+  if (!ok) return OZK_ERR_CUDA;
+  if (splits > 1) {
+    const int64_t blocks = ceil_div((int64_t)c.M * c.N, 256);
+    const unsigned g = (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16);
+    const float* part = static_cast<const float*>(p.out.ptr);
+    if (bf16)
+      join_kernel<true><<<g, 256, 0, st>>>(part, splits, c.M, c.N, p.out.ld, c.ptr, c.ld, 0);
+    else
+      join_kernel<false><<<g, 256, 0, st>>>(part, splits, c.M, c.N, p.out.ld, c.ptr, c.ld, c.add);
+    if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
+  }
+  return OZK_OK;
+}
 
 }  // namespace
 }  // namespace ozk
@@ -99,12 +911,22 @@ ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* 
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)ceil_div(N, 32), (unsigned)ceil_div(M, 32));
-  if (c_type == OZK_F32)
-    product_kernel<<<grid, 256, 0, st>>>(a, b, (int)M, (int)N, (int)K, static_cast<float*>(C), ldc, accumulate);
-  else
-    product_kernel<<<grid, 256, 0, st>>>(a, b, (int)M, (int)N, (int)K, static_cast<__nv_bfloat16*>(C), ldc, 0);
-  return cudaGetLastError() == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
+  const bool bf16 = c_type == OZK_BF16;
+  const size_t size = bf16 ? 2 : 4;
+  if (K == 0) {   // an empty sum
+    if (!accumulate && cudaMemset2DAsync(C, (size_t)ldc * size, 0, (size_t)N * size, (size_t)M, st) != cudaSuccess) return OZK_ERR_CUDA;
+    return OZK_OK;
+  }
+  ProductParams p = {};
+  p.a = a, p.b = b;
+  p.out = Output{C, ldc, (int)M, (int)N, accumulate, aligned16(C) && ((size_t)ldc * size) % 16 == 0 ? 1 : 0};
+  p.splits = 1;
+  p.groups = (int)ceil_div(K, kGroupK);
+  p.status = static_cast<StatusBlock*>(workspace);
+  // Up to 128 rows the kernel for few rows reads B once with nothing to spare; an A summed over its rows has no 128-byte
+  // rows of k to serve as that kernel's column side.
+  if (M <= 128 && !a.contract_rows) return run_rows(p, K, floats, bf16, st);
+  return run_pair(p, K, floats, bf16, static_cast<uint8_t*>(workspace), st);
 }
 
 }  // extern "C"

@@ -26,6 +26,7 @@
 
 #include "ozk_common.cuh"
 #include "ozk_ptx.cuh"
+#include "ozk_wait.cuh"
 
 namespace ozk {
 namespace {
@@ -35,7 +36,6 @@ using namespace ptx;
 constexpr int kPTileBytes = kTileRows * kTileKBytes;  // 16 KiB: 128 rows x 128 bytes
 constexpr int kTmemCols = 512;
 constexpr int kScaleCol = 496;  // scale-factor bytes live in TMEM columns 496..511
-constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int kMaxStages = 4;
 
 struct GemmCore {
@@ -64,26 +64,6 @@ struct __align__(8) GemmShared {
   uint32_t tmem_base;
   volatile int abort;
 };
-
-// Bounded wait on an mbarrier phase.  Returns false after the time limit or when another role
-// of this CTA has already given up.
-__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, volatile int* abort, StatusBlock* status, int where) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_timer_ns();
-  for (uint32_t it = 1;; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 63u) == 0u) {
-      if (*abort) return false;
-      if (global_timer_ns() - t0 > kWaitLimitNs) {
-        *abort = 1;
-        atomicMin(&status->code, (int)OZK_ERR_DEVICE_TIMEOUT);
-        atomicExch(&status->where, where);
-        return false;
-      }
-    }
-  }
-}
-
 
 // Producer-side wave barrier: before loading the operands of its n-th item a producer announces
 // itself on a global counter and waits (bounded) until every producer that has an n-th item has
