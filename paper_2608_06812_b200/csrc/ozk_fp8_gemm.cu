@@ -9,7 +9,7 @@
 // An operand whose k runs along its rows (contract_rows) is not transposed: its tiles are fetched with the 128-byte
 // rows along the lines, and the instruction reads them that way.
 //
-// Two kernels.  product_pair_kernel: a CTA pair forms a 256 x 256 tile of C (256 x 128 with FP32 scales), persistent,
+// Two kernels.  product_pair_kernel: a CTA pair forms a 256 x 256 tile of C, persistent,
 // TMA producer / MMA issuer / scale writers / epilogue in warps of their own; K is split over several pairs when there are
 // few tiles, the partial sums being joined in order by join_kernel.  product_rows_kernel: for few rows of C, where reading B
 // is what costs: B's lines become the 128 rows of the instruction, the rows of C its columns; the CTAs of a
@@ -38,17 +38,27 @@ struct Operand {
   int64_t tiles;       // tiles (TILES) or blocks per stored row of scales
 };
 
-// Scale bytes of blocks 4 g .. 4 g + 3 of one line; 1 (127) where there is none.
-__device__ __forceinline__ uint32_t scale_word(const Operand& o, int line, int g) {
-  if (line >= o.lines) return 0x7F7F7F7Fu;
-  if (o.kind == OZK_SCALE_LINES) return __ldg(static_cast<const uint32_t*>(o.scales) + (int64_t)g * o.lines + line);
-  const uint8_t* s = static_cast<const uint8_t*>(o.scales);
-  const int64_t at = o.contract_rows ? (int64_t)(4 * g) * o.tiles + line / kBlock : (int64_t)(line / kBlock) * o.tiles + 4 * g;
-  const int64_t step = o.contract_rows ? o.tiles : 1;
-  uint32_t w = 0;
+// Scale bytes of blocks 4 g .. 4 g + 3 for the lines line0 + 32 c + lane of 128, c = 0 .. columns - 1; 1 (127) where there is none.
+// line0 is a multiple of 128: with TILES all 128 lines have the same word.
+template <int kColumns>
+__device__ __forceinline__ void scale_words(const Operand& o, int line0, int lane, int g, uint32_t (&w)[4]) {
+  if (o.kind == OZK_SCALE_LINES) {
+    const uint32_t* s = static_cast<const uint32_t*>(o.scales) + (int64_t)g * o.lines + line0 + lane;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) w |= (uint32_t)(4 * g + b < o.blocks ? __ldg(s + at + b * step) : 127u) << (8 * b);
-  return w;
+    for (int c = 0; c < 4; ++c) w[c] = c < kColumns && line0 + c * 32 + lane < o.lines ? __ldg(s + c * 32) : 0x7F7F7F7Fu;
+  } else {
+    const uint8_t* s = static_cast<const uint8_t*>(o.scales);
+    const int64_t tile = line0 / kBlock, b0 = 4 * (int64_t)g;
+    const int64_t at = o.contract_rows ? b0 * o.tiles + tile : tile * o.tiles + b0, step = o.contract_rows ? o.tiles : 1;
+    uint32_t v = 0x7F7F7F7Fu;
+    if (line0 < o.lines) {
+      v = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) v |= (uint32_t)(4 * g + b < o.blocks ? __ldg(s + at + b * step) : 127u) << (8 * b);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = v;
+  }
 }
 // Line and block of an FP32-scaled operand.
 __device__ __forceinline__ float scale_line_f32(const Operand& o, int line, int b) {
@@ -90,27 +100,32 @@ constexpr int kRangeGroups = 8192 / kGroupK;   // FP32 results: longest range su
 
 // ---- CTA-pair kernel --------------------------------------------------------------------
 constexpr int kTileM = 256;
-constexpr int kPairThreads = 14 * 32;   // producer, issuer, 4 scale warps, 8 epilogue warps
-constexpr int kMaxPairStages = 8;
+constexpr int kTileN = 256;
+constexpr int kMaxPairStages = 6;
 template <bool kFloat>
 struct PairShape {
-  static constexpr int kTileN = kFloat ? 128 : 256;
+  // producer, issuer, then 4 scale warps (UE8M0) or 2 idle ones (FP32 scales), and 8 epilogue warps of 32 rows x 128 columns
+  static constexpr int kFirstEpilogue = kFloat ? 4 : 6;
+  static constexpr int kEpilogueWarps = 8;
+  static constexpr int kThreads = 32 * (kFirstEpilogue + kEpilogueWarps);
+  // FP32 scales: an epilogue thread keeps its 128 sums in registers.  384 threads are launched with 168 each (64512); the
+  // first four warps keep 40 of them, so that the eight of the epilogue may have 232 (5120 + 59392).
+  [[maybe_unused]] static constexpr int kLaunchRegs = 168, kFewRegs = 40, kEpilogueRegs = 232;
   static constexpr int kABytes = 128 * kBlock;             // this CTA's 128 lines of A
   static constexpr int kBBytes = kTileN / 2 * kBlock;      // and half of the lines of B
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = kFloat ? 8 : 6;
-  // Accumulators in tensor memory.  UE8M0: two of 256 columns that overlap in 32 (columns 224..255), so that both and the
-  // scale words fit 512: a new tile waits only until those 32 columns of the previous one have been read.
-  // FP32 scales: a ring of four, one per block of 128.
-  static constexpr int kBuffers = kFloat ? 4 : 2;
-  static constexpr int kBufferStep = kFloat ? 128 : 224;
-  [[maybe_unused]] static constexpr int kScaleCol = 480;                    // two sets of 4 columns for A, 8 for B
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 8 * 4096 + 512 + 1024;
+  static constexpr int kStages = 6;
+  // Two accumulators in tensor memory.  FP32 scales: one block of 128 each.  UE8M0: they overlap in 32 columns (224..255), so that both
+  // and the scale words fit 512: a new tile waits only until those 32 columns of the previous one have been read.
+  static constexpr int kBuffers = 2;
+  static constexpr int kBufferStep = kFloat ? 256 : 224;
+  [[maybe_unused]] static constexpr int kScaleCol = 480;   // two sets of 4 columns for A, 8 for B
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpilogueWarps * 4096 + 512 + 1024;
 };
 struct __align__(8) PairShared {
   uint64_t full[kMaxPairStages], empty[kMaxPairStages];
   uint64_t sf_full[2], sf_empty[2];
-  uint64_t acc_full[4], acc_empty[4];
+  uint64_t acc_full[2], acc_empty[2];
   uint64_t overlap, drained;
   uint32_t tmem_base;
   volatile int abort;
@@ -120,7 +135,6 @@ static_assert(sizeof(PairShared) <= 512, "room reserved behind the stages");
 struct Item {
   int m0, n0, split, g_begin, g_end;
 };
-template <bool kFloat>
 __device__ __forceinline__ Item pair_item(const ProductParams& p, int item) {
   // bands of eight row tiles sweep the column tiles: the pairs at work at one time share few panels of A and B
   Item r;
@@ -128,7 +142,7 @@ __device__ __forceinline__ Item pair_item(const ProductParams& p, int item) {
   r.split = item - tile * p.splits;
   const int band = 8 * p.tiles_n, g = tile / band, rem = tile - g * band;
   const int rows = min(8, p.tiles_m - 8 * g);
-  r.n0 = rem / rows * PairShape<kFloat>::kTileN;
+  r.n0 = rem / rows * kTileN;
   r.m0 = (8 * g + rem % rows) * kTileM;
   r.g_begin = (int)((int64_t)r.split * p.groups / p.splits);
   r.g_end = (int)((int64_t)(r.split + 1) * p.groups / p.splits);
@@ -179,14 +193,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 template <bool kFloat, bool kBf16>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<kFloat>::kThreads, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
                     const __grid_constant__ ProductParams p) {
   using S = PairShape<kFloat>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* staging = tiles + S::kStages * S::kStageBytes;
-  PairShared* sh = reinterpret_cast<PairShared*>(staging + 8 * 4096);
+  PairShared* sh = reinterpret_cast<PairShared*>(staging + S::kEpilogueWarps * 4096);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
@@ -198,7 +212,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     prefetch_tensormap(&map_c);
     for (int s = 0; s < S::kStages; ++s) mbar_init(smem_u32(&sh->full[s]), 1), mbar_init(smem_u32(&sh->empty[s]), 1);   // full: the leader's only
     for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&sh->sf_full[s]), 8), mbar_init(smem_u32(&sh->sf_empty[s]), 1);      // 4 scale warps of each CTA
-    for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&sh->acc_full[s]), 1), mbar_init(smem_u32(&sh->acc_empty[s]), 16);   // 8 epilogue warps of each CTA
+    for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&sh->acc_full[s]), 1), mbar_init(smem_u32(&sh->acc_empty[s]), 2 * S::kEpilogueWarps);   // of both CTAs
     mbar_init(smem_u32(&sh->overlap), 8);
     mbar_init(smem_u32(&sh->drained), 1);
     sh->abort = 0;
@@ -216,211 +230,221 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = sh->tmem_base;
 
-  if (warp == 0) {
-    // ------------------------------ TMA producer (both CTAs) ------------------------------
-    if (lane == 0) {
-      int stage = 0, issued = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int item = pair; item < items && ok; item += npairs) {
-        const Item it = pair_item<kFloat>(p, item);
-        const int b_end = min(4 * it.g_end, p.a.blocks);
-        for (int b = 4 * it.g_begin; b < b_end; ++b) {
-          if (!wait_bounded(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort, p.status, 0x800 + stage)) {
-            ok = false;
-            break;
+  if (warp < S::kFirstEpilogue) {
+    if constexpr (kFloat) set_registers_fewer<S::kFewRegs>();
+    if (warp == 0) {
+      // ------------------------------ TMA producer (both CTAs) ------------------------------
+      if (lane == 0) {
+        int stage = 0, issued = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int item = pair; item < items && ok; item += npairs) {
+          const Item it = pair_item(p, item);
+          const int b_end = min(4 * it.g_end, p.a.blocks);
+          for (int b = 4 * it.g_begin; b < b_end; ++b) {
+            if (!wait_bounded(smem_u32(&sh->empty[stage]), phase ^ 1u, &sh->abort, p.status, 0x800 + stage)) {
+              ok = false;
+              break;
+            }
+            const uint32_t full = map_to_cta(smem_u32(&sh->full[stage]), 0);
+            const uint32_t dst = smem_u32(tiles + stage * S::kStageBytes);
+            if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh->full[stage]), 2 * S::kStageBytes);
+            int x, y;
+            tile_at(p.a.contract_rows, it.m0 + rank * 128, b, x, y);
+            tma_load_2d_pair(dst, &map_a, full, x, y);
+            tile_at(p.b.contract_rows, it.n0 + rank * (kTileN / 2), b, x, y);
+            tma_load_2d_pair(dst + S::kABytes, &map_b, full, x, y);
+            ++issued;
+            if (++stage == S::kStages) stage = 0, phase ^= 1u;
           }
-          const uint32_t full = map_to_cta(smem_u32(&sh->full[stage]), 0);
-          const uint32_t dst = smem_u32(tiles + stage * S::kStageBytes);
-          if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh->full[stage]), 2 * S::kStageBytes);
-          int x, y;
-          tile_at(p.a.contract_rows, it.m0 + rank * 128, b, x, y);
-          tma_load_2d_pair(dst, &map_a, full, x, y);
-          tile_at(p.b.contract_rows, it.n0 + rank * (S::kTileN / 2), b, x, y);
-          tma_load_2d_pair(dst + S::kABytes, &map_b, full, x, y);
-          ++issued;
-          if (++stage == S::kStages) stage = 0, phase ^= 1u;
+        }
+        if (sh->abort && rank == 0) {   // copies in flight land before this CTA leaves
+          const uint64_t t0 = global_timer_ns();
+          for (int j = max(0, issued - S::kStages); j < issued; ++j)
+            while (!mbar_try_wait(smem_u32(&sh->full[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {
+            }
         }
       }
-      if (sh->abort && rank == 0) {   // copies in flight land before this CTA leaves
-        const uint64_t t0 = global_timer_ns();
-        for (int j = max(0, issued - S::kStages); j < issued; ++j)
-          while (!mbar_try_wait(smem_u32(&sh->full[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {
-          }
-      }
-    }
-  } else if (warp == 1) {
-    // ------------------------------ MMA issuer (leader only) ------------------------------
-    if (lane == 0 && rank == 0) {
-      int stage = 0;
-      uint32_t phase = 0, unit = 0, sf_unit = 0;
-      const int a_lines = p.a.contract_rows, b_lines = p.b.contract_rows;
-      const uint32_t a_step = operand_step(a_lines), b_step = operand_step(b_lines);
-      const uint32_t idesc = kFloat ? idesc_f8(kTileM, S::kTileN) : idesc_mxf8(kTileM, S::kTileN, a_lines, b_lines);
-      bool ok = true;
-      for (int item = pair; item < items && ok; item += npairs) {
-        const Item it = pair_item<kFloat>(p, item);
-        for (int g0 = it.g_begin; g0 < it.g_end && ok; g0 += p.chunk_groups) {
-          const int b_begin = 4 * g0, b_end = min(4 * min(it.g_end, g0 + p.chunk_groups), p.a.blocks);
-          uint32_t acc = 0;
-          if constexpr (!kFloat) {
-            const uint32_t buf = unit % S::kBuffers;
-            acc = tmem + buf * S::kBufferStep;
-            if (!wait_bounded(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x810)) { ok = false; break; }
-            if (unit && !wait_bounded(smem_u32(&sh->overlap), (unit - 1) & 1u, &sh->abort, p.status, 0x811)) { ok = false; break; }
-            tc_fence_after();
-          }
-          for (int b = b_begin; b < b_end; ++b) {
-            uint32_t sfa = 0, sfb = 0;
-            if constexpr (kFloat) {
+    } else if (warp == 1) {
+      // ------------------------------ MMA issuer (leader only) ------------------------------
+      // The whole warp walks the loop and waits; one elected lane issues.  Descriptors stay uniform that way.
+      if (rank == 0) {
+        int stage = 0;
+        uint32_t phase = 0, unit = 0, sf_unit = 0;
+        const int a_lines = p.a.contract_rows, b_lines = p.b.contract_rows;
+        const uint32_t a_step = operand_step(a_lines), b_step = operand_step(b_lines);
+        const uint32_t idesc = kFloat ? idesc_f8(kTileM, kTileN) : idesc_mxf8(kTileM, kTileN, a_lines, b_lines);
+        bool ok = true;
+        for (int item = pair; item < items && ok; item += npairs) {
+          const Item it = pair_item(p, item);
+          for (int g0 = it.g_begin; g0 < it.g_end && ok; g0 += p.chunk_groups) {
+            const int b_begin = 4 * g0, b_end = min(4 * min(it.g_end, g0 + p.chunk_groups), p.a.blocks);
+            uint32_t acc = 0;
+            if constexpr (!kFloat) {
               const uint32_t buf = unit % S::kBuffers;
               acc = tmem + buf * S::kBufferStep;
-              if (!wait_bounded(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x812)) { ok = false; break; }
-            } else {
-              const uint32_t set = sf_unit & 1u;
-              if ((b & 3) == 0 && !wait_bounded(smem_u32(&sh->sf_full[set]), (sf_unit >> 1) & 1u, &sh->abort, p.status, 0x813)) { ok = false; break; }
-              sfa = tmem + S::kScaleCol + set * 12;
-              sfb = sfa + 4;
+              if (!wait_warp(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x810)) { ok = false; break; }
+              if (unit && !wait_warp(smem_u32(&sh->overlap), (unit - 1) & 1u, &sh->abort, p.status, 0x811)) { ok = false; break; }
+              tc_fence_after();
             }
-            if (!wait_bounded(smem_u32(&sh->full[stage]), phase, &sh->abort, p.status, 0x820 + stage)) { ok = false; break; }
+            for (int b = b_begin; b < b_end; ++b) {
+              uint32_t sfa = 0, sfb = 0;
+              if constexpr (kFloat) {
+                const uint32_t buf = unit % S::kBuffers;
+                acc = tmem + buf * S::kBufferStep;
+                if (!wait_warp(smem_u32(&sh->acc_empty[buf]), ((unit / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x812)) { ok = false; break; }
+              } else {
+                const uint32_t set = sf_unit & 1u;
+                if ((b & 3) == 0 && !wait_warp(smem_u32(&sh->sf_full[set]), (sf_unit >> 1) & 1u, &sh->abort, p.status, 0x813)) { ok = false; break; }
+                sfa = tmem + S::kScaleCol + set * 12;
+                sfb = sfa + 4;
+              }
+              if (!wait_warp(smem_u32(&sh->full[stage]), phase, &sh->abort, p.status, 0x820 + stage)) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
+              const uint64_t da = operand_desc(a_lines, base), db = operand_desc(b_lines, base + S::kABytes);
+              const bool last_of_scales = (b & 3) == 3 || b + 1 == b_end;
+              if (elect_one()) {
+#pragma unroll
+                for (uint32_t ks = 0; ks < 4; ++ks) {
+                  if constexpr (kFloat)
+                    mma_f8_pair(acc, da + ks * a_step, db + ks * b_step, idesc, ks ? 1u : 0u);
+                  else
+                    mma_mxf8_pair(acc, da + ks * a_step, db + ks * b_step, idesc | idesc_mxf8_block((uint32_t)b & 3u), sfa, sfb, (b > b_begin || ks) ? 1u : 0u);
+                }
+                mma_commit_pair(smem_u32(&sh->empty[stage]), (uint16_t)3);
+                if constexpr (kFloat) {
+                  mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
+                } else {
+                  if (last_of_scales) mma_commit_pair(smem_u32(&sh->sf_empty[sf_unit & 1u]), (uint16_t)3);
+                  if (b + 1 == b_end) mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
+                }
+              }
+              __syncwarp();
+              if (++stage == S::kStages) stage = 0, phase ^= 1u;
+              if constexpr (kFloat) ++unit; else sf_unit += last_of_scales;
+            }
+            if constexpr (!kFloat) ++unit;
+          }
+        }
+        if (sh->abort && elect_one()) {
+          mma_commit_pair(smem_u32(&sh->drained), (uint16_t)1);
+          const uint64_t t0 = global_timer_ns();
+          while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
+          }
+        }
+      }
+    } else if (warp < S::kFirstEpilogue) {
+      // ------------------------------ scale words into tensor memory (both CTAs) ------------------------------
+      // Row r of an operand's 128 lines is lane r % 32, column r / 32 of its four columns, in every quarter of the lanes:
+      // each warp writes the quarter it may touch.  This CTA's 128 lines of A, all 256 of B.
+      if constexpr (!kFloat) {
+        const uint32_t at = tmem + (((uint32_t)(warp & 3) * 32u) << 16) + S::kScaleCol;
+        const uint32_t leader = map_to_cta(smem_u32(&sh->sf_full[0]), 0);
+        uint32_t unit = 0;
+        bool ok = true;
+        for (int item = pair; item < items && ok; item += npairs) {
+          const Item it = pair_item(p, item);
+          uint32_t wa[4], wb0[4], wb1[4];   // the words of the next group, on their way while this one's are written
+          auto fetch = [&](int g) {
+            scale_words<4>(p.a, it.m0 + rank * 128, lane, g, wa);
+            scale_words<4>(p.b, it.n0, lane, g, wb0);
+            scale_words<4>(p.b, it.n0 + 128, lane, g, wb1);
+          };
+          fetch(it.g_begin);
+          for (int g = it.g_begin; g < it.g_end; ++g, ++unit) {
+            const uint32_t set = unit & 1u;
+            if (!wait_warp(smem_u32(&sh->sf_empty[set]), ((unit >> 1) & 1u) ^ 1u, &sh->abort, p.status, 0x830)) {
+              ok = false;
+              break;
+            }
             tc_fence_after();
-            const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
-            const uint64_t da = operand_desc(a_lines, base), db = operand_desc(b_lines, base + S::kABytes);
-#pragma unroll
-            for (uint32_t ks = 0; ks < 4; ++ks) {
-              if constexpr (kFloat)
-                mma_f8_pair(acc, da + ks * a_step, db + ks * b_step, idesc, ks ? 1u : 0u);
-              else
-                mma_mxf8_pair(acc, da + ks * a_step, db + ks * b_step, idesc | idesc_mxf8_block((uint32_t)b & 3u), sfa, sfb, (b > b_begin || ks) ? 1u : 0u);
-            }
-            mma_commit_pair(smem_u32(&sh->empty[stage]), (uint16_t)3);
-            if (++stage == S::kStages) stage = 0, phase ^= 1u;
-            if constexpr (kFloat) {
-              mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
-              ++unit;
-            } else if ((b & 3) == 3 || b + 1 == b_end) {
-              mma_commit_pair(smem_u32(&sh->sf_empty[sf_unit & 1u]), (uint16_t)3);
-              ++sf_unit;
-            }
+            tmem_st_32x4(at + set * 12, wa);
+            tmem_st_32x4(at + set * 12 + 4, wb0);
+            tmem_st_32x4(at + set * 12 + 8, wb1);
+            if (g + 1 < it.g_end) fetch(g + 1);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(leader + set * 8);
           }
-          if (!ok) break;
-          if constexpr (!kFloat) {
-            mma_commit_pair(smem_u32(&sh->acc_full[unit % S::kBuffers]), (uint16_t)3);
-            ++unit;
-          }
-        }
-      }
-      if (sh->abort) {
-        mma_commit_pair(smem_u32(&sh->drained), (uint16_t)1);
-        const uint64_t t0 = global_timer_ns();
-        while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
-        }
-      }
-    }
-  } else if (warp < 6) {
-    // ------------------------------ scale words into tensor memory (both CTAs) ------------------------------
-    // Row r of an operand's 128 lines is lane r % 32, column r / 32 of its four columns, in every quarter of the lanes:
-    // each warp writes the quarter it may touch.  This CTA's 128 lines of A, all 256 of B.
-    if constexpr (!kFloat) {
-      const uint32_t at = tmem + (((uint32_t)(warp & 3) * 32u) << 16) + S::kScaleCol;
-      const uint32_t leader = map_to_cta(smem_u32(&sh->sf_full[0]), 0);
-      uint32_t unit = 0;
-      bool ok = true;
-      for (int item = pair; item < items && ok; item += npairs) {
-        const Item it = pair_item<kFloat>(p, item);
-        for (int g = it.g_begin; g < it.g_end; ++g, ++unit) {
-          uint32_t wa[4], wb0[4], wb1[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            wa[c] = scale_word(p.a, it.m0 + rank * 128 + c * 32 + lane, g);
-            wb0[c] = scale_word(p.b, it.n0 + c * 32 + lane, g);
-            wb1[c] = scale_word(p.b, it.n0 + 128 + c * 32 + lane, g);
-          }
-          const uint32_t set = unit & 1u;
-          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->sf_empty[set]), ((unit >> 1) & 1u) ^ 1u, &sh->abort, p.status, 0x830))) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          tmem_st_32x4(at + set * 12, wa);
-          tmem_st_32x4(at + set * 12 + 4, wb0);
-          tmem_st_32x4(at + set * 12 + 8, wb1);
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(leader + set * 8);
         }
       }
     }
   } else {
+    if constexpr (kFloat) set_registers_more<S::kEpilogueRegs>();
     // ------------------------------ epilogue (both CTAs) ----------------------------------
     const uint32_t quad = (uint32_t)(warp & 3);
-    const int half = (warp - 6) >> 2;
-    uint8_t* box = staging + (warp - 6) * 4096;
+    const int part = (warp - S::kFirstEpilogue) >> 2;   // which kWarpCols of the columns
+    uint8_t* box = staging + (warp - S::kFirstEpilogue) * 4096;
     const uint32_t lanes = tmem + ((quad * 32u) << 16);
     const uint32_t empty0 = map_to_cta(smem_u32(&sh->acc_empty[0]), 0), overlap = map_to_cta(smem_u32(&sh->overlap), 0);
     uint32_t unit = 0;
     bool ok = true;
     for (int item = pair; item < items && ok; item += npairs) {
-      const Item it = pair_item<kFloat>(p, item);
+      const Item it = pair_item(p, item);
       const int m = it.m0 + rank * 128 + (int)quad * 32;
       if constexpr (kFloat) {
-        const int n = it.n0 + half * 64, row = m + lane;
+        const int n = it.n0 + part * 128, row = m + lane;
         const int b_begin = 4 * it.g_begin, b_end = min(4 * it.g_end, p.a.blocks);
-        float acc[64];
+        float acc[128];
 #pragma unroll
-        for (int e = 0; e < 64; ++e) acc[e] = 0.f;
-        float sa = scale_line_f32(p.a, row, b_begin), sb = scale_tile_f32(p.b, it.n0, b_begin);
+        for (int e = 0; e < 128; ++e) acc[e] = 0.f;
+        float sa = scale_line_f32(p.a, row, b_begin), sb = scale_tile_f32(p.b, n, b_begin);
         for (int b = b_begin; b < b_end; ++b, ++unit) {
           const uint32_t buf = unit % S::kBuffers;
           const float s = sa * sb;
-          if (b + 1 < b_end) sa = scale_line_f32(p.a, row, b + 1), sb = scale_tile_f32(p.b, it.n0, b + 1);
-          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x840))) {
+          if (b + 1 < b_end) sa = scale_line_f32(p.a, row, b + 1), sb = scale_tile_f32(p.b, n, b + 1);
+          if (!wait_warp(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x840)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          uint32_t d0[32], d1[32];
-          tmem_ld_32x32(lanes + buf * S::kBufferStep + half * 64, d0);
-          tmem_ld_32x32(lanes + buf * S::kBufferStep + half * 64 + 32, d1);
-          tmem_wait_ld();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(empty0 + buf * 8);
+          const uint32_t from = lanes + buf * S::kBufferStep + part * 128;
+          uint32_t d[2][32];   // 32 columns are multiplied while the next 32 are read
+          tmem_ld_32x32(from, d[0]);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[e] = fmaf(__uint_as_float(d0[e]), s, acc[e]), acc[32 + e] = fmaf(__uint_as_float(d1[e]), s, acc[32 + e]);
+          for (int c = 0; c < 4; ++c) {
+            tmem_wait_ld();
+            if (c < 3) {
+              tmem_ld_32x32(from + (c + 1) * 32, d[(c + 1) & 1]);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(empty0 + buf * 8);
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) acc[c * 32 + e] = fmaf(__uint_as_float(d[c & 1][e]), s, acc[c * 32 + e]);
+          }
         }
         if (!ok) break;
         uint32_t w[32];
-        if constexpr (kBf16) {
+        constexpr int kPieces = kBf16 ? 2 : 4;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) w[e] = pack_bf16(acc[2 * e], acc[2 * e + 1]);
-          store_box<true>(p.out, &map_c, box, lane, w, m, n, it.split, false);
-        } else {
+        for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(acc[32 * h + e]);
-            store_box<false>(p.out, &map_c, box, lane, w, m, n + 32 * h, it.split, p.out.add);
+          for (int e = 0; e < 32; ++e) {
+            if constexpr (kBf16) w[e] = pack_bf16(acc[64 * i + 2 * e], acc[64 * i + 2 * e + 1]); else w[e] = __float_as_uint(acc[32 * i + e]);
           }
+          store_box<kBf16>(p.out, &map_c, box, lane, w, m, n + i * (128 / kPieces), it.split, p.out.add);
         }
       } else {
-        const int n = it.n0 + half * 128;
+        const int n = it.n0 + part * 128;
         for (int g0 = it.g_begin; g0 < it.g_end; g0 += p.chunk_groups, ++unit) {
           const uint32_t buf = unit % S::kBuffers;
           const bool later = g0 > it.g_begin;   // a later range of the same tile is added to the earlier ones
           if (later && p.out.tma && lane == 0) bulk_wait();
-          if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x841))) {
+          if (!wait_warp(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x841)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t from = lanes + buf * S::kBufferStep + half * 128;
-          const bool shared_half = buf == 0 ? half == 1 : half == 0;   // holds the columns that the other accumulator shares
+          const uint32_t from = lanes + buf * S::kBufferStep + part * 128;
+          const bool shared_half = buf == 0 ? part == 1 : part == 0;   // holds the columns that the other accumulator shares
           constexpr int kPieces = kBf16 ? 2 : 4, kWidth = kBf16 ? 64 : 32;
 #pragma unroll
           for (int i = 0; i < kPieces; ++i) {
-            const int c = buf == 0 && half == 1 ? kPieces - 1 - i : i;   // those columns first
+            const int c = buf == 0 && part == 1 ? kPieces - 1 - i : i;   // those columns first
             uint32_t w[32];
             if constexpr (kBf16) {
               uint32_t d0[32], d1[32];
@@ -572,32 +596,33 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    {
       const int w_lines = p.b.contract_rows;
       const uint32_t w_step = operand_step(w_lines);
       const uint32_t idesc = kFloat ? idesc_f8(128, NT) : idesc_mxf8(128, NT, w_lines, 0);
-      bool ok = true;
       for (int b = b_begin; b < b_end; ++b) {
         const int i = b - b_begin, stage = i % S::kStages, buf = i % S::kBuffers, set = (i / 4) % S::kSets;
-        if (kFloat && !wait_bounded(smem_u32(&sh->acc_empty[buf]), ((uint32_t)(i / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x910)) { ok = false; break; }
-        if (!kFloat && i % 4 == 0 && !wait_bounded(smem_u32(&sh->sf_full[set]), (uint32_t)(i / 4 / S::kSets) & 1u, &sh->abort, p.status, 0x911)) { ok = false; break; }
-        if (!wait_bounded(smem_u32(&sh->full[stage]), (uint32_t)(i / S::kStages) & 1u, &sh->abort, p.status, 0x920 + stage)) { ok = false; break; }
+        if (kFloat && !wait_warp(smem_u32(&sh->acc_empty[buf]), ((uint32_t)(i / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x910)) break;
+        if (!kFloat && i % 4 == 0 && !wait_warp(smem_u32(&sh->sf_full[set]), (uint32_t)(i / 4 / S::kSets) & 1u, &sh->abort, p.status, 0x911)) break;
+        if (!wait_warp(smem_u32(&sh->full[stage]), (uint32_t)(i / S::kStages) & 1u, &sh->abort, p.status, 0x920 + stage)) break;
         tc_fence_after();
         const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
         const uint64_t dw = operand_desc(w_lines, base), dx = smem_desc_sw128(base + S::kWBytes);
+        if (elect_one()) {
 #pragma unroll
-        for (uint32_t ks = 0; ks < 4; ++ks) {
-          if constexpr (kFloat)
-            mma_f8(tmem + buf * NT, dw + ks * w_step, dx + ks * 2u, idesc, ks ? 1u : 0u);
-          else
-            mma_mxf8(tmem, dw + ks * w_step, dx + ks * 2u, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
+          for (uint32_t ks = 0; ks < 4; ++ks) {
+            if constexpr (kFloat)
+              mma_f8(tmem + buf * NT, dw + ks * w_step, dx + ks * 2u, idesc, ks ? 1u : 0u);
+            else
+              mma_mxf8(tmem, dw + ks * w_step, dx + ks * 2u, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
+          }
+          mma_commit(smem_u32(&sh->empty[stage]));
+          if (kFloat || b + 1 == b_end) mma_commit(smem_u32(&sh->acc_full[kFloat ? buf : 0]));
+          if (!kFloat && (i % 4 == 3 || b + 1 == b_end)) mma_commit(smem_u32(&sh->sf_empty[set]));
         }
-        mma_commit(smem_u32(&sh->empty[stage]));
-        if (kFloat) mma_commit(smem_u32(&sh->acc_full[buf]));
-        if (!kFloat && (i % 4 == 3 || b + 1 == b_end)) mma_commit(smem_u32(&sh->sf_empty[set]));
+        __syncwarp();
       }
-      if (!kFloat && ok) mma_commit(smem_u32(&sh->acc_full[0]));
-      if (sh->abort) {
+      if (sh->abort && elect_one()) {
         mma_commit(smem_u32(&sh->drained));
         const uint64_t t0 = global_timer_ns();
         while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
@@ -630,7 +655,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 #pragma unroll
           for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, lane + 32 * j, b + 1) : 0.f;
         }
-        if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[buf]), (uint32_t)(i / S::kBuffers) & 1u, &sh->abort, p.status, 0x930))) {
+        if (!wait_warp(smem_u32(&sh->acc_full[buf]), (uint32_t)(i / S::kBuffers) & 1u, &sh->abort, p.status, 0x930)) {
           ok = false;
           break;
         }
@@ -663,12 +688,9 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       for (int g = g_begin; g < g_end; ++g) {
         const int i = g - g_begin, set = i % S::kSets;
         uint32_t ww[4], wx[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          ww[c] = scale_word(p.b, n0 + c * 32 + lane, g);
-          wx[c] = c * 32 < NT ? scale_word(p.a, c * 32 + lane, g) : 0x7F7F7F7Fu;
-        }
-        if (!__all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->sf_empty[set]), ((uint32_t)(i / S::kSets) & 1u) ^ 1u, &sh->abort, p.status, 0x931))) {
+        scale_words<4>(p.b, n0, lane, g, ww);
+        scale_words<(NT + 31) / 32>(p.a, 0, lane, g, wx);
+        if (!wait_warp(smem_u32(&sh->sf_empty[set]), ((uint32_t)(i / S::kSets) & 1u) ^ 1u, &sh->abort, p.status, 0x931)) {
           ok = false;
           break;
         }
@@ -680,7 +702,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh->sf_full[set]));
       }
-      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_bounded(smem_u32(&sh->acc_full[0]), 0u, &sh->abort, p.status, 0x932));
+      if (ok) ok = wait_warp(smem_u32(&sh->acc_full[0]), 0u, &sh->abort, p.status, 0x932);
       if (ok) {
         tc_fence_after();
 #pragma unroll
@@ -757,12 +779,16 @@ bool output_map(CUtensorMap* map, const Output& o, bool bf16, int splits) {
 }
 
 constexpr int kMaxDevices = 64;
-// Raises a kernel's dynamic shared memory once per device.
+// Raises a kernel's dynamic shared memory once per device, and checks its registers.
 template <class K>
-bool raise_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices]) {
+bool raise_smem(K kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices], int registers = 0) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
   if (done[dev].load(std::memory_order_acquire)) return true;
+  if (registers) {   // the kernel redistributes this many registers per thread: a build with fewer would wait for them
+    cudaFuncAttributes a;
+    if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess || a.numRegs < registers) return false;
+  }
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
   done[dev].store(true, std::memory_order_release);
   return true;
@@ -772,8 +798,8 @@ template <bool kFloat, bool kBf16>
 bool launch_pair(const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_c, const ProductParams& p, int pairs, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
   auto kernel = product_pair_kernel<kFloat, kBf16>;
-  if (!raise_smem(kernel, PairShape<kFloat>::kSmem, done)) return false;
-  kernel<<<(unsigned)(2 * pairs), kPairThreads, PairShape<kFloat>::kSmem, st>>>(map_a, map_b, map_c, p);
+  if (!raise_smem(kernel, PairShape<kFloat>::kSmem, done, kFloat ? PairShape<kFloat>::kLaunchRegs : 0)) return false;
+  kernel<<<(unsigned)(2 * pairs), PairShape<kFloat>::kThreads, PairShape<kFloat>::kSmem, st>>>(map_a, map_b, map_c, p);
   return cudaGetLastError() == cudaSuccess;
 }
 
@@ -837,8 +863,7 @@ ozk_status run_rows(ProductParams p, int64_t K, bool floats, bool bf16, cudaStre
 }
 
 ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t* workspace, cudaStream_t st) {
-  const int tile_n = floats ? 128 : 256;
-  const int64_t tm = ceil_div(p.out.M, kTileM), tn = ceil_div(p.out.N, tile_n);
+  const int64_t tm = ceil_div(p.out.M, kTileM), tn = ceil_div(p.out.N, kTileN);
   if (tm * tn > INT32_MAX) return OZK_ERR_UNSUPPORTED;
   const int pairs = device_sm_count() / 2;
   if (pairs < 1) return OZK_ERR_CUDA;
@@ -859,7 +884,7 @@ ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t*
     if ((size_t)splits * c.M * p.out.ld * 4 + kGemmStatusBytes > kGemmWorkspace) return OZK_ERR_UNSUPPORTED;
   }
   CUtensorMap map_a, map_b, map_c;
-  if (!operand_map(&map_a, p.a, K, 128) || !operand_map(&map_b, p.b, K, tile_n / 2)) return OZK_ERR_CUDA;
+  if (!operand_map(&map_a, p.a, K, 128) || !operand_map(&map_b, p.b, K, kTileN / 2)) return OZK_ERR_CUDA;
   if (p.out.tma) {
     if (!output_map(&map_c, p.out, out_bf16, splits)) return OZK_ERR_CUDA;
   } else {

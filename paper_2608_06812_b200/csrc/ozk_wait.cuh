@@ -26,5 +26,9 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
     }
   }
 }
+// The same for all lanes of a converged warp, with one answer for all.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, StatusBlock* status, int where) {
+  return __all_sync(0xFFFFFFFFu, wait_bounded(bar, parity, abort, status, where));
+}
 
 }  // namespace ozk
