@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "ozk_fp8.cuh"
 
 namespace ozk {
@@ -9,7 +11,10 @@ namespace {
 
 using namespace fp8;
 
-constexpr int kChunk = 4096;        // elements per thread block: eight warps of four blocks of 128
+// A piece is what one warp works on at a time: four blocks of 128 elements.  All its loads are issued before the first result
+// is formed (with 8-bit states and FP32 parameters 6 to 8 KiB a warp), which is what keeps enough bytes in flight.
+constexpr int kPieceBlocks = 4;
+constexpr int kPiece = kPieceBlocks * kBlock;
 constexpr int kTableTensors = 448;  // tensors per launch: the table travels in the kernel's parameters (at most 32764 bytes)
 
 struct Entry {
@@ -25,11 +30,12 @@ struct Entry {
 struct Table {
   int count;
   uint32_t first_tensor;              // index in the caller's array of entry 0: part of the hash
+  uint32_t pieces;
   const float* grad_scale;
   const int* skip;
   float beta1, one_minus_beta1, beta2, one_minus_beta2, decay, step_size, root_bias, eps;
   uint32_t seed_key;                  // mix(seed)
-  uint32_t first_chunk[kTableTensors + 1];
+  uint32_t first_piece[kTableTensors + 1];
   Entry entry[kTableTensors];
 };
 static_assert(sizeof(Table) <= 32764, "kernel parameters");
@@ -42,33 +48,81 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// Four consecutive elements; zeros beyond `left`.
-__device__ __forceinline__ void load4(const float* p, bool vec, int64_t left, float (&x)[4]) {
-  if (vec) {
-    const float4 w = *reinterpret_cast<const float4*>(p);
-    x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i < left ? p[i] : 0.f;
+// Pairs of floats: each operation rounds both by itself, as the scalar one does, in one instruction.
+struct Pair {
+  uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ float2 both(Pair p) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+  return f;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
+// Four consecutive elements as they lie in memory, read ahead; `vec`: in one access.  Zeros beyond `left`.
+template <class T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 w;
+  __device__ __forceinline__ void load(const float* p, bool vec, int64_t left) {
+    if (vec) {
+      w = *reinterpret_cast<const float4*>(p);
+    } else {
+      w.x = left > 0 ? p[0] : 0.f, w.y = left > 1 ? p[1] : 0.f, w.z = left > 2 ? p[2] : 0.f, w.w = left > 3 ? p[3] : 0.f;
+    }
   }
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, bool vec, int64_t left, float (&x)[4]) {
-  if (vec) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i < left ? __bfloat162float(p[i]) : 0.f;
+  __device__ __forceinline__ Pair lo() const { return pair(w.x, w.y); }
+  __device__ __forceinline__ Pair hi() const { return pair(w.z, w.w); }
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint2 w;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec, int64_t left) {
+    if (vec) {
+      w = *reinterpret_cast<const uint2*>(p);
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+      w.x = (left > 0 ? q[0] : 0u) | (left > 1 ? (uint32_t)q[1] << 16 : 0u);
+      w.y = (left > 2 ? q[2] : 0u) | (left > 3 ? (uint32_t)q[3] << 16 : 0u);
+    }
   }
-}
-__device__ __forceinline__ uint32_t load4(const uint8_t* p, bool vec, int64_t left) {
-  if (vec) return *reinterpret_cast<const uint32_t*>(p);
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i < left) w |= (uint32_t)p[i] << (8 * i);
-  return w;
-}
+  __device__ __forceinline__ Pair lo() const { return pair(bf16_lo(w.x), bf16_hi(w.x)); }
+  __device__ __forceinline__ Pair hi() const { return pair(bf16_lo(w.y), bf16_hi(w.y)); }
+};
+template <>
+struct Raw<uint8_t> {   // E4M3 codes
+  uint32_t w;
+  __device__ __forceinline__ void load(const uint8_t* p, bool vec, int64_t left) {
+    if (vec) {
+      w = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w = (left > 0 ? p[0] : 0u) | (left > 1 ? (uint32_t)p[1] << 8 : 0u) | (left > 2 ? (uint32_t)p[2] << 16 : 0u) | (left > 3 ? (uint32_t)p[3] << 24 : 0u);
+    }
+  }
+  __device__ __forceinline__ Pair lo() const {
+    const float2 f = unpack2(w & 0xFFFFu);
+    return pair(f.x, f.y);
+  }
+  __device__ __forceinline__ Pair hi() const {
+    const float2 f = unpack2(w >> 16);
+    return pair(f.x, f.y);
+  }
+};
 __device__ __forceinline__ void store4(float* p, bool vec, int64_t left, const float (&x)[4]) {
   if (vec) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -98,98 +152,139 @@ __device__ __forceinline__ void store4(uint8_t* p, bool vec, int64_t left, uint3
   }
 }
 
-// Root y = r / scale (0 <= y <= 448, or not finite) on the E4M3 grid, at least its least step 2^-9 unless y = 0.
+// Root y = r / scale, 0 <= y <= 448, on the E4M3 grid, at least its least step 2^-9 unless y = 0.
 // Stochastic: 16 random bits are added below the three fraction bits and the rest is cut off; below 2^-6, where the
 // grid is even, the same is done at y + 2^-6, whose unit is that grid's.
 template <bool kStochastic>
-__device__ __forceinline__ float root_on_grid(float y, uint32_t noise16) {
+__device__ __forceinline__ float root_on_grid(float y, uint32_t noise) {
+  float q = y;
   if constexpr (kStochastic) {
-    const bool low = y < 0.015625f;
-    const float z = low ? y + 0.015625f : y;
-    const float w = __uint_as_float((__float_as_uint(z) + (noise16 << 4)) & 0xFFF00000u);
-    const float q = low ? w - 0.015625f : w;
-    return y > 0.f ? (y <= 448.f ? fmaxf(q, 0.001953125f) : y - y + __uint_as_float(0x7FC00000u)) : y;
-  } else {
-    return y > 0.f ? (y <= 448.f ? fmaxf(y, 0.001953125f) : __uint_as_float(0x7FC00000u)) : y;
+    const float base = y < 0.015625f ? 0.015625f : 0.f;
+    q = __uint_as_float((__float_as_uint(y + base) + ((noise >> 16) << 4)) & 0xFFF00000u) - base;
   }
+  return y > 0.f ? fmaxf(q, 0.001953125f) : y;
 }
 // BF16 by adding 16 random bits below it and cutting off the rest; what is not finite stays.
-__device__ __forceinline__ float bf16_stochastic(float p, uint32_t noise16) {
+__device__ __forceinline__ float bf16_stochastic(float p, uint32_t noise) {
   const uint32_t u = __float_as_uint(p);
-  return (u & 0x7F800000u) == 0x7F800000u ? p : __uint_as_float((u + noise16) & 0xFFFF0000u);
+  return (u & 0x7F800000u) == 0x7F800000u ? p : __uint_as_float((u + (noise & 0xFFFFu)) & 0xFFFF0000u);
+}
+
+template <class P, class G, bool kEight>
+struct Block {
+  using State = typename std::conditional<kEight, uint8_t, float>::type;
+  Raw<P> p;
+  Raw<G> g;
+  Raw<State> m, v;
+  uint32_t m_scale, v_scale;
+  __device__ __forceinline__ void load(const Entry& e, int64_t at, int lane, bool vec, int64_t n) {
+    const int64_t i0 = at + lane * 4, left = n - i0;
+    p.load(static_cast<const P*>(e.param) + i0, vec, left);
+    g.load(static_cast<const G*>(e.grad) + i0, vec, left);
+    m.load(static_cast<const State*>(e.m) + i0, vec, left);
+    v.load(static_cast<const State*>(e.v) + i0, vec, left);
+    if constexpr (kEight) m_scale = e.m_scale[at / kBlock], v_scale = e.v_scale[at / kBlock];
+  }
+};
+
+template <class P, class G, bool kEight, bool kStochastic>
+__device__ __forceinline__ void update(const Table& t, const Entry& e, const Block<P, G, kEight>& x, int64_t at, int lane, bool vec, int64_t n, float clip, uint32_t key) {
+  using State = typename Block<P, G, kEight>::State;
+  const int64_t i0 = at + lane * 4, left = n - i0;
+  const Pair clip2 = pair(clip, clip), b1 = pair(t.beta1, t.beta1), c1 = pair(t.one_minus_beta1, t.one_minus_beta1), b2 = pair(t.beta2, t.beta2),
+             c2 = pair(t.one_minus_beta2, t.one_minus_beta2);
+  float p[4], m[4], v[4], r[4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const Pair g = (h ? x.g.hi() : x.g.lo()) * clip2;
+    Pair m2 = h ? x.m.hi() : x.m.lo(), v2 = h ? x.v.hi() : x.v.lo();
+    if constexpr (kEight) {
+      const float sm = scale_value(x.m_scale), sv = scale_value(x.v_scale);
+      m2 = m2 * pair(sm, sm), v2 = v2 * pair(sv, sv);
+      v2 = v2 * v2;   // the state is the root
+    }
+    // every product and sum is rounded by itself: the rounding to 8 bits after it then does not hang on a contraction
+    m2 = m2 * b1 + g * c1;
+    v2 = v2 * b2 + (g * c2) * g;
+    const float2 mf = both(m2), vf = both(v2), pf = both(h ? x.p.hi() : x.p.lo());
+    m[2 * h] = mf.x, m[2 * h + 1] = mf.y, v[2 * h] = vf.x, v[2 * h + 1] = vf.y, p[2 * h] = pf.x, p[2 * h + 1] = pf.y;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = __fsqrt_rn(v[i]);   // rounded correctly: the block's scale is read off it
+    // the quotient is only added to a parameter: two units in the last place of the step
+    p[i] = fmaf(p[i], t.decay, -t.step_size * __fdividef(m[i], fmaf(r[i], t.root_bias, t.eps)));
+  }
+  uint32_t noise[4] = {};
+  if constexpr (kStochastic) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) noise[i] = mix((uint32_t)(i0 + i) ^ key);
+  }
+  if constexpr (kStochastic && sizeof(P) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = bf16_stochastic(p[i], noise[i]);
+  }
+  store4(static_cast<P*>(e.param) + i0, vec, left, p);
+  if (sizeof(P) == 4 && e.copy) store4(e.copy + i0, vec, left, p);
+  if constexpr (kEight) {
+    uint32_t top_m = max(max(__float_as_uint(m[0]) & 0x7FFFFFFFu, __float_as_uint(m[1]) & 0x7FFFFFFFu), max(__float_as_uint(m[2]) & 0x7FFFFFFFu, __float_as_uint(m[3]) & 0x7FFFFFFFu));
+    uint32_t top_r = max(max(__float_as_uint(r[0]) & 0x7FFFFFFFu, __float_as_uint(r[1]) & 0x7FFFFFFFu), max(__float_as_uint(r[2]) & 0x7FFFFFFFu, __float_as_uint(r[3]) & 0x7FFFFFFFu));
+    top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
+    if (max(top_m, top_r) >= 0x7F800000u) {
+      // something is not finite (the same for the whole warp): it becomes NaN and stays out of the scales
+      top_m = max(max(finite_bits(m[0]), finite_bits(m[1])), max(finite_bits(m[2]), finite_bits(m[3])));
+      top_r = max(max(finite_bits(r[0]), finite_bits(r[1])), max(finite_bits(r[2]), finite_bits(r[3])));
+      top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] += m[i] - m[i], r[i] += r[i] - r[i];
+    }
+    const uint32_t code_m = scale_code(top_m), code_r = scale_code(top_r);
+    const float im = scale_recip(code_m), ir = scale_recip(code_r);
+    store4(static_cast<State*>(e.m) + i0, vec, left, pack4(m[0] * im, m[1] * im, m[2] * im, m[3] * im));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = root_on_grid<kStochastic>(r[i] * ir, noise[i]);
+    store4(static_cast<State*>(e.v) + i0, vec, left, pack4(r[0], r[1], r[2], r[3]));
+    if (lane == 0) e.m_scale[at / kBlock] = (uint8_t)code_m, e.v_scale[at / kBlock] = (uint8_t)code_r;
+  } else {
+    store4(static_cast<State*>(e.m) + i0, vec, left, m);
+    store4(static_cast<State*>(e.v) + i0, vec, left, v);
+  }
 }
 
 template <class P, class G, bool kEight, bool kStochastic>
 __global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ Table t) {
   if (t.skip && *t.skip) return;
-  // the tensor whose chunks hold this one
-  int lo = 0, hi = t.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (t.first_chunk[mid] <= blockIdx.x) lo = mid; else hi = mid;
-  }
-  const Entry& e = t.entry[lo];
-  const bool aligned = e.n > 0;
-  const int64_t n = aligned ? e.n : -e.n;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t base = (int64_t)(blockIdx.x - t.first_chunk[lo]) * kChunk + warp * (kChunk / 8);
   const float clip = t.grad_scale ? *t.grad_scale : 1.f;
-  const uint32_t key = mix(t.first_tensor + (uint32_t)lo + 1u) ^ t.seed_key;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  // each thread block takes a run of pieces, its warps one after another: the tensor is searched once and then followed
+  const uint32_t begin = (uint32_t)((uint64_t)t.pieces * blockIdx.x / gridDim.x), end = (uint32_t)((uint64_t)t.pieces * (blockIdx.x + 1) / gridDim.x);
+  uint32_t piece = begin + warp;
+  if (piece >= end) return;
+  int at_tensor = 0, hi = t.count;
+  while (hi - at_tensor > 1) {
+    const int mid = (at_tensor + hi) / 2;
+    if (t.first_piece[mid] <= piece) at_tensor = mid; else hi = mid;
+  }
+  for (; piece < end; piece += 8) {
+    while (t.first_piece[at_tensor + 1] <= piece) ++at_tensor;
+    const Entry& e = t.entry[at_tensor];
+    const bool aligned = e.n > 0;
+    const int64_t n = aligned ? e.n : -e.n, at = (int64_t)(piece - t.first_piece[at_tensor]) * kPiece;
+    const uint32_t key = mix(t.first_tensor + (uint32_t)at_tensor + 1u) ^ t.seed_key;
+    if (aligned && at + kPiece <= n) {
+      Block<P, G, kEight> x[kPieceBlocks];
 #pragma unroll
-  for (int b = 0; b < kChunk / 8 / kBlock; ++b) {
-    const int64_t at = base + b * kBlock;
-    if (at >= n) break;
-    const int64_t i0 = at + lane * 4, left = n - i0;
-    const bool vec = aligned && at + kBlock <= n;
-    float p[4], g[4], m[4], v[4], r[4];
-    load4(static_cast<const P*>(e.param) + i0, vec, left, p);
-    load4(static_cast<const G*>(e.grad) + i0, vec, left, g);
-    if constexpr (kEight) {
-      const uint32_t cm = load4(static_cast<const uint8_t*>(e.m) + i0, vec, left), cv = load4(static_cast<const uint8_t*>(e.v) + i0, vec, left);
-      const float sm = scale_value(e.m_scale[at / kBlock]), sv = scale_value(e.v_scale[at / kBlock]);
-      const float2 m01 = unpack2(cm & 0xFFFF), m23 = unpack2(cm >> 16), v01 = unpack2(cv & 0xFFFF), v23 = unpack2(cv >> 16);
-      m[0] = m01.x * sm, m[1] = m01.y * sm, m[2] = m23.x * sm, m[3] = m23.y * sm;
-      v[0] = v01.x * sv, v[1] = v01.y * sv, v[2] = v23.x * sv, v[3] = v23.y * sv;
+      for (int b = 0; b < kPieceBlocks; ++b) x[b].load(e, at + b * kBlock, lane, true, n);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], v[i]);
+      for (int b = 0; b < kPieceBlocks; ++b) update<P, G, kEight, kStochastic>(t, e, x[b], at + b * kBlock, lane, true, n, clip, key);
     } else {
-      load4(static_cast<const float*>(e.m) + i0, vec, left, m);
-      load4(static_cast<const float*>(e.v) + i0, vec, left, v);
-    }
-    uint32_t top_m = 0, top_r = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      // every product and sum rounded by itself: the rounding to 8 bits after it then does not hang on a contraction
-      const float gs = __fmul_rn(g[i], clip);
-      m[i] = __fadd_rn(__fmul_rn(m[i], t.beta1), __fmul_rn(gs, t.one_minus_beta1));
-      v[i] = __fadd_rn(__fmul_rn(v[i], t.beta2), __fmul_rn(__fmul_rn(gs, t.one_minus_beta2), gs));
-      r[i] = __fsqrt_rn(v[i]);
-      const float u = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(r[i], t.root_bias), t.eps));
-      p[i] = __fsub_rn(__fmul_rn(p[i], t.decay), __fmul_rn(u, t.step_size));
-      if constexpr (kEight) top_m = max(top_m, finite_bits(m[i])), top_r = max(top_r, finite_bits(r[i]));
-    }
-    uint32_t noise[4] = {};
-    if constexpr (kStochastic) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) noise[i] = mix((uint32_t)(i0 + i) ^ key);
-    }
-    if constexpr (kStochastic && sizeof(P) == 2) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = bf16_stochastic(p[i], noise[i] & 0xFFFFu);
-    }
-    store4(static_cast<P*>(e.param) + i0, vec, left, p);
-    if (e.copy) store4(e.copy + i0, vec, left, p);
-    if constexpr (kEight) {
-      const uint32_t code_m = scale_code(__reduce_max_sync(0xFFFFFFFFu, top_m)), code_r = scale_code(__reduce_max_sync(0xFFFFFFFFu, top_r));
-      const float im = scale_recip(code_m), ir = scale_recip(code_r);
-      store4(static_cast<uint8_t*>(e.m) + i0, vec, left, pack4(scaled(m[0], im), scaled(m[1], im), scaled(m[2], im), scaled(m[3], im)));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = root_on_grid<kStochastic>(__fmul_rn(r[i], ir), noise[i] >> 16);
-      store4(static_cast<uint8_t*>(e.v) + i0, vec, left, pack4(r[0], r[1], r[2], r[3]));
-      if (lane == 0) e.m_scale[at / kBlock] = (uint8_t)code_m, e.v_scale[at / kBlock] = (uint8_t)code_r;
-    } else {
-      store4(static_cast<float*>(e.m) + i0, vec, left, m);
-      store4(static_cast<float*>(e.v) + i0, vec, left, v);
+#pragma unroll 1
+      for (int64_t a = at; a < n && a < at + kPiece; a += kBlock) {
+        const bool vec = aligned && a + kBlock <= n;
+        Block<P, G, kEight> x;
+        x.load(e, a, lane, vec, n);
+        update<P, G, kEight, kStochastic>(t, e, x, a, lane, vec, n, clip, key);
+      }
     }
   }
 }
@@ -227,7 +322,7 @@ extern "C" ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t co
       return OZK_ERR_INVALID_ARG;
     if (o->state_bits == 8 && (!x.m_scale || !x.v_scale)) return OZK_ERR_INVALID_ARG;
     if (x.copy && (o->param_type != OZK_F32 || !aligned_to(x.copy, 2))) return OZK_ERR_INVALID_ARG;
-    if (ceil_div(x.n, kChunk) > INT32_MAX / kTableTensors) return OZK_ERR_UNSUPPORTED;   // chunks of a launch are counted in 31 bits
+    if (ceil_div(x.n, kPiece) > INT32_MAX / kTableTensors) return OZK_ERR_UNSUPPORTED;   // the pieces of a launch are counted in 31 bits
   }
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -244,23 +339,27 @@ extern "C" ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t co
   for (int64_t first = 0; first < count; first += kTableTensors) {
     t.count = (int)(count - first < kTableTensors ? count - first : kTableTensors);
     t.first_tensor = (uint32_t)first;
-    uint32_t chunks = 0;
+    uint32_t pieces = 0;
     for (int i = 0; i < t.count; ++i) {
       const ozk_adamw_tensor& x = tensors[first + i];
       const bool vec = aligned_to(x.param, 4 * ps) && aligned_to(x.grad, 4 * gs) && aligned_to(x.m, 4 * ss) && aligned_to(x.v, 4 * ss) && aligned_to(x.copy, 8);
       t.entry[i] = Entry{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, static_cast<__nv_bfloat16*>(x.copy), vec ? x.n : -x.n};
-      t.first_chunk[i] = chunks;
-      chunks += (uint32_t)ceil_div(x.n, kChunk);
+      t.first_piece[i] = pieces;
+      pieces += (uint32_t)ceil_div(x.n, kPiece);
     }
-    t.first_chunk[t.count] = chunks;
-    if (chunks == 0) continue;
+    t.first_piece[t.count] = pieces;
+    t.pieces = pieces;
+    if (pieces == 0) continue;
+    // small steps: a warp for every piece; large ones: as many thread blocks as run at a time, several times over
+    const int64_t most = (int64_t)device_sm_count() * 16, wanted = ceil_div(pieces, 8);
+    const unsigned blocks = (unsigned)(wanted < most ? wanted : most);
     const bool eight = o->state_bits == 8, stochastic = o->stochastic && (eight || o->param_type == OZK_BF16);
     cudaError_t e;
     if (o->param_type == OZK_F32)
-      e = o->grad_type == OZK_F32 ? launch<float, float>(t, eight, stochastic, chunks, st) : launch<float, __nv_bfloat16>(t, eight, stochastic, chunks, st);
+      e = o->grad_type == OZK_F32 ? launch<float, float>(t, eight, stochastic, blocks, st) : launch<float, __nv_bfloat16>(t, eight, stochastic, blocks, st);
     else
-      e = o->grad_type == OZK_F32 ? launch<__nv_bfloat16, float>(t, eight, stochastic, chunks, st)
-                                  : launch<__nv_bfloat16, __nv_bfloat16>(t, eight, stochastic, chunks, st);
+      e = o->grad_type == OZK_F32 ? launch<__nv_bfloat16, float>(t, eight, stochastic, blocks, st)
+                                  : launch<__nv_bfloat16, __nv_bfloat16>(t, eight, stochastic, blocks, st);
     if (e != cudaSuccess) return OZK_ERR_CUDA;
   }
   return OZK_OK;

@@ -109,8 +109,8 @@ struct PairShape {
   static constexpr int kEpilogueWarps = 8;
   static constexpr int kThreads = 32 * (kFirstEpilogue + kEpilogueWarps);
   // FP32 scales: an epilogue thread keeps its 128 sums in registers.  384 threads are launched with 168 each (64512); the
-  // first four warps keep 40 of them, so that the eight of the epilogue may have 232 (5120 + 59392).
-  [[maybe_unused]] static constexpr int kLaunchRegs = 168, kFewRegs = 40, kEpilogueRegs = 232;
+  // first four warps keep 56 of them, so that the eight of the epilogue may have 224 (7168 + 57344).
+  [[maybe_unused]] static constexpr int kLaunchRegs = 168, kFewRegs = 56, kEpilogueRegs = 224;
   static constexpr int kABytes = 128 * kBlock;             // this CTA's 128 lines of A
   static constexpr int kBBytes = kTileN / 2 * kBlock;      // and half of the lines of B
   static constexpr int kStageBytes = kABytes + kBBytes;
@@ -387,20 +387,23 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
       if constexpr (kFloat) {
         const int n = it.n0 + part * 128, row = m + lane;
         const int b_begin = 4 * it.g_begin, b_end = min(4 * it.g_end, p.a.blocks);
-        float acc[128];
+        uint64_t acc[64];
 #pragma unroll
-        for (int e = 0; e < 128; ++e) acc[e] = 0.f;
-        float sa = scale_line_f32(p.a, row, b_begin), sb = scale_tile_f32(p.b, n, b_begin);
+        for (int e = 0; e < 64; ++e) acc[e] = 0;
+        float sa = scale_line_f32(p.a, row, b_begin), sb = scale_tile_f32(p.b, n, b_begin), sa1 = sa, sb1 = sb;
+        if (b_begin + 1 < b_end) sa1 = scale_line_f32(p.a, row, b_begin + 1), sb1 = scale_tile_f32(p.b, n, b_begin + 1);
         for (int b = b_begin; b < b_end; ++b, ++unit) {
           const uint32_t buf = unit % S::kBuffers;
           const float s = sa * sb;
-          if (b + 1 < b_end) sa = scale_line_f32(p.a, row, b + 1), sb = scale_tile_f32(p.b, n, b + 1);
+          sa = sa1, sb = sb1;
+          if (b + 2 < b_end) sa1 = scale_line_f32(p.a, row, b + 2), sb1 = scale_tile_f32(p.b, n, b + 2);
           if (!wait_warp(smem_u32(&sh->acc_full[buf]), (unit / S::kBuffers) & 1u, &sh->abort, p.status, 0x840)) {
             ok = false;
             break;
           }
           tc_fence_after();
           const uint32_t from = lanes + buf * S::kBufferStep + part * 128;
+          const uint64_t s2 = pack_f32x2(s, s);
           uint32_t d[2][32];   // 32 columns are multiplied while the next 32 are read
           tmem_ld_32x32(from, d[0]);
 #pragma unroll
@@ -414,7 +417,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
               if (lane == 0) mbar_arrive_cluster(empty0 + buf * 8);
             }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) acc[c * 32 + e] = fmaf(__uint_as_float(d[c & 1][e]), s, acc[c * 32 + e]);
+            for (int e = 0; e < 32; e += 2) fma_f32x2(acc[c * 16 + e / 2], pack_f32x2(__uint_as_float(d[c & 1][e]), __uint_as_float(d[c & 1][e + 1])), s2);
           }
         }
         if (!ok) break;
@@ -424,7 +427,14 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
-            if constexpr (kBf16) w[e] = pack_bf16(acc[64 * i + 2 * e], acc[64 * i + 2 * e + 1]); else w[e] = __float_as_uint(acc[32 * i + e]);
+            float lo, hi;
+            if constexpr (kBf16) {
+              unpack_f32x2(acc[32 * i + e], lo, hi);
+              w[e] = pack_bf16(lo, hi);
+            } else {
+              unpack_f32x2(acc[16 * i + e / 2], lo, hi);
+              w[e] = __float_as_uint(e % 2 ? hi : lo);
+            }
           }
           store_box<kBf16>(p.out, &map_c, box, lane, w, m, n + i * (128 / kPieces), it.split, p.out.add);
         }

@@ -77,94 +77,206 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
   if (lane == 0) S[(int64_t)g * rows + r] = word;
 }
 
-// A 128 x 128 tile per block: thread (t / 8, t % 8) holds 16 columns of rows t / 8 + 32 i.
+// ---- 128 x 128 tiles ------------------------------------------------------------------
+// A tile per thread block, held in registers as it lies in memory: it is read once for both orientations.  Thread t has, of
+// rows t / 8 + 32 i, the 16 bytes from byte (t % 8) * 16 of every 128: eight lanes read whole 128-byte lines.
+// Magnitudes are compared as integers, two BF16 at a time; what is not finite shows as the largest of them, and then the
+// block looks again without it.
+template <class T>
+struct Words;
+template <>
+struct Words<__nv_bfloat16> {
+  static constexpr int kPiece = 8, kPieces = 2, kWords = 4;   // elements and words per 16 bytes, pieces per row of the tile
+  __device__ static __forceinline__ uint32_t magnitude(uint32_t w) { return w & 0x7FFF7FFFu; }
+  __device__ static __forceinline__ uint32_t finite_magnitude(uint32_t w) {
+    const uint32_t a = w & 0x7FFF7FFFu;
+    return ((a & 0xFFFFu) < 0x7F80u ? a & 0xFFFFu : 0u) | (a < 0x7F800000u ? a & 0xFFFF0000u : 0u);
+  }
+  __device__ static __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ static __forceinline__ uint32_t float_bits(uint32_t m, int i) { return i ? m & 0xFFFF0000u : m << 16; }   // element i of a word
+  __device__ static __forceinline__ uint32_t largest(uint32_t m) { return max(m << 16, m & 0xFFFF0000u); }
+  __device__ static __forceinline__ float value(const uint32_t* w, int e) { return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]); }
+};
+template <>
+struct Words<float> {
+  static constexpr int kPiece = 4, kPieces = 4, kWords = 4;
+  __device__ static __forceinline__ uint32_t magnitude(uint32_t w) { return w & 0x7FFFFFFFu; }
+  __device__ static __forceinline__ uint32_t finite_magnitude(uint32_t w) { return finite_bits(__uint_as_float(w)); }
+  __device__ static __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+  __device__ static __forceinline__ uint32_t float_bits(uint32_t m, int) { return m; }
+  __device__ static __forceinline__ uint32_t largest(uint32_t m) { return m; }
+  __device__ static __forceinline__ float value(const uint32_t* w, int e) { return __uint_as_float(w[e]); }
+};
+
+// 16 bytes of a row, zeros beyond `left` elements.
+template <class T, bool kVec>
+__device__ __forceinline__ void load_piece(const T* p, int left, uint32_t* w) {
+  constexpr int kPiece = Words<T>::kPiece;
+  if (kVec && left >= kPiece) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else {
+    w[0] = w[1] = w[2] = w[3] = 0;
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) {
+      if (i >= left) continue;
+      if constexpr (sizeof(T) == 2) w[i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
+      else w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+  }
+}
+// Its codes: x times a reciprocal that may differ from column to column, `bad`: NaN for what is not finite.
+template <class T>
+__device__ __forceinline__ void store_piece(uint8_t* q, int left, const uint32_t* w, const float* recip, int step, bool bad) {
+  constexpr int kPiece = Words<T>::kPiece;
+  uint32_t out[kPiece / 4];
+#pragma unroll
+  for (int k = 0; k < kPiece / 4; ++k) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = Words<T>::value(w, 4 * k + i) * recip[(4 * k + i) * step];
+    if (bad) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = scaled(Words<T>::value(w, 4 * k + i), recip[(4 * k + i) * step]);
+    }
+    out[k] = pack4(y[0], y[1], y[2], y[3]);
+  }
+  if (left >= kPiece) {
+    if constexpr (kPiece == 8) *reinterpret_cast<uint2*>(q) = make_uint2(out[0], out[1]); else *reinterpret_cast<uint32_t*>(q) = out[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i)
+      if (i < left) q[i] = (uint8_t)(out[i / 4] >> (8 * (i % 4)));
+  }
+}
+
 template <class T, bool kVec, bool kRows, bool kCols, bool kTiles>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
                                                             uint8_t* Qc, int64_t ldc, uint8_t* Sc) {
-  __shared__ uint32_t part[8][kBlock], tile_top[4];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  using W = Words<T>;
+  constexpr int kPiece = W::kPiece, kPieces = W::kPieces, kWords = W::kWords, kRowWords = kPieces * kWords;   // words per thread and row
+  constexpr int kTileWords = kRowWords * 8;
+  __shared__ uint32_t part[8][kCols ? kTileWords : 1];
+  __shared__ float column_recip[kCols ? kBlock : 1];
+  __shared__ uint32_t tile_top[8];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % 8;
   const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
   const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
-  const int r0 = tr * kBlock + threadIdx.x / 8, c0 = tc * kBlock + (threadIdx.x % 8) * 16;
-  float x[4][16];
+  const int r0 = tr * kBlock + threadIdx.x / 8, c0 = tc * kBlock + c * kPiece;
+  uint32_t x[4][kRowWords];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) load16<T, kVec>(X + (int64_t)(r0 + 32 * i) * ldx + c0, r0 + 32 * i < rows ? cols - c0 : 0, x[i]);
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int col = c0 + q * 8 * kPiece;
+      load_piece<T, kVec>(X + (int64_t)(r0 + 32 * i) * ldx + col, r0 + 32 * i < rows ? cols - col : 0, &x[i][q * kWords]);
+    }
+  // largest magnitudes of this thread's rows and columns
+  uint32_t row_top[4], col_top[kRowWords];
+  auto look = [&](auto magnitude) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t a[kRowWords];
+#pragma unroll
+      for (int k = 0; k < kRowWords; ++k) {
+        a[k] = magnitude(x[i][k]);
+        col_top[k] = i ? W::larger(col_top[k], a[k]) : a[k];
+      }
+      uint32_t top = a[0];
+#pragma unroll
+      for (int k = 1; k < kRowWords; ++k) top = W::larger(top, a[k]);
+      row_top[i] = W::largest(top);
+    }
+  };
+  look([](uint32_t w) { return W::magnitude(w); });
+  const bool bad = __syncthreads_or(max(max(row_top[0], row_top[1]), max(row_top[2], row_top[3])) >= 0x7F800000u);
+  if (bad) look([](uint32_t w) { return W::finite_magnitude(w); });
+
+  if constexpr (kCols) {
+#pragma unroll
+    for (int k = 0; k < kRowWords; ++k) {
+      col_top[k] = W::larger(col_top[k], __shfl_xor_sync(0xFFFFFFFFu, col_top[k], 8));
+      col_top[k] = W::larger(col_top[k], __shfl_xor_sync(0xFFFFFFFFu, col_top[k], 16));
+    }
+    if (lane < 8) {
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        *reinterpret_cast<uint4*>(&part[warp][(q * 8 + c) * kWords]) = make_uint4(col_top[q * 4], col_top[q * 4 + 1], col_top[q * 4 + 2], col_top[q * 4 + 3]);
+    }
+  }
+  if constexpr (kTiles) {
+    const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, max(max(row_top[0], row_top[1]), max(row_top[2], row_top[3])));
+    if (lane == 0) tile_top[warp] = t;
+  }
   if constexpr (kRows) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) top = max(top, finite_bits(x[i][j]));
+      uint32_t top = row_top[i];
 #pragma unroll
       for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
       const int r = r0 + 32 * i;
       if (r >= rows) continue;
-      const uint32_t c = scale_code(top);
-      const float recip = scale_recip(c);
-      if (cols > c0) {
-        uint32_t w[4];
+      const uint32_t code = scale_code(top);
+      const float recip = scale_recip(code);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = pack4(scaled(x[i][4 * j], recip), scaled(x[i][4 * j + 1], recip), scaled(x[i][4 * j + 2], recip), scaled(x[i][4 * j + 3], recip));
-        store16(Qr + (int64_t)r * ldr + c0, cols - c0, w);
+      for (int q = 0; q < kPieces; ++q) {
+        const int col = c0 + q * 8 * kPiece;
+        if (col < cols) store_piece<T>(Qr + (int64_t)r * ldr + col, cols - col, &x[i][q * kWords], &recip, 0, bad);
       }
-      if (lane % 8 == 0) {
+      if (c == 0) {
         uint8_t* s = Sr + ((int64_t)(tc / 4) * rows + r) * 4;
-        s[tc % 4] = (uint8_t)c;
+        s[tc % 4] = (uint8_t)code;
         if (tc + 1 == tiles_c)
           for (int b = tc % 4 + 1; b < 4; ++b) s[b] = 127;
       }
     }
   }
   if constexpr (kCols || kTiles) {
-    uint32_t top[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      top[j] = max(max(finite_bits(x[0][j]), finite_bits(x[1][j])), max(finite_bits(x[2][j]), finite_bits(x[3][j])));
-      top[j] = max(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], 8));
-      top[j] = max(top[j], __shfl_xor_sync(0xFFFFFFFFu, top[j], 16));
-    }
-    if (lane < 8) {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) part[warp][lane * 16 + j] = top[j];
-    }
     __syncthreads();
-    if (threadIdx.x < kBlock) {
-      uint32_t t = part[0][threadIdx.x];
-#pragma unroll
-      for (int w = 1; w < 8; ++w) t = max(t, part[w][threadIdx.x]);
-      if constexpr (kTiles) {
-        t = __reduce_max_sync(0xFFFFFFFFu, t);
-        if (lane == 0) tile_top[warp] = t;
-      } else {
-        part[0][threadIdx.x] = scale_code(t);
-      }
-    }
-    __syncthreads();
-    uint32_t tile_code = 0;
+    float tile_recip = 0.f;
     if constexpr (kTiles) {
-      tile_code = scale_code(max(max(tile_top[0], tile_top[1]), max(tile_top[2], tile_top[3])));
-      if (threadIdx.x == 0) Sc[(int64_t)tr * tiles_c + tc] = (uint8_t)tile_code;
-    } else if (threadIdx.x < kBlock && tc * kBlock + threadIdx.x < cols) {
-      uint8_t* s = Sc + ((int64_t)(tr / 4) * cols + tc * kBlock + threadIdx.x) * 4;
-      s[tr % 4] = (uint8_t)part[0][threadIdx.x];
-      if (tr + 1 == tiles_r)
-        for (int b = tr % 4 + 1; b < 4; ++b) s[b] = 127;
-    }
-    if (cols > c0) {
-      float recip[16];
+      uint32_t t = tile_top[0];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) recip[j] = scale_recip(kTiles ? tile_code : part[0][c0 - tc * kBlock + j]);
+      for (int w = 1; w < 8; ++w) t = max(t, tile_top[w]);
+      const uint32_t code = scale_code(t);
+      tile_recip = scale_recip(code);
+      if (threadIdx.x == 0) Sc[(int64_t)tr * tiles_c + tc] = (uint8_t)code;
+    } else {
+      if (threadIdx.x < kTileWords) {
+        constexpr int kPerWord = kPiece / kWords;
+        uint32_t t = part[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) t = W::larger(t, part[w][threadIdx.x]);
+#pragma unroll
+        for (int k = 0; k < kPerWord; ++k) {
+          const int col = (int)threadIdx.x * kPerWord + k;
+          const uint32_t code = scale_code(W::float_bits(t, k));
+          column_recip[col] = scale_recip(code);
+          if (tc * kBlock + col < cols) {
+            uint8_t* s = Sc + ((int64_t)(tr / 4) * cols + tc * kBlock + col) * 4;
+            s[tr % 4] = (uint8_t)code;
+            if (tr + 1 == tiles_r)
+              for (int b = tr % 4 + 1; b < 4; ++b) s[b] = 127;
+          }
+        }
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int col = c0 + q * 8 * kPiece;
+      float recip[kPiece];
+#pragma unroll
+      for (int k = 0; k < kPiece; ++k) recip[k] = kTiles ? tile_recip : column_recip[col - tc * kBlock + k];
+      if (col >= cols) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = r0 + 32 * i;
-        if (r >= rows) break;
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = pack4(scaled(x[i][4 * j], recip[4 * j]), scaled(x[i][4 * j + 1], recip[4 * j + 1]), scaled(x[i][4 * j + 2], recip[4 * j + 2]),
-                       scaled(x[i][4 * j + 3], recip[4 * j + 3]));
-        store16(Qc + (int64_t)r * ldc + c0, cols - c0, w);
+        if (r < rows) store_piece<T>(Qc + (int64_t)r * ldc + col, cols - col, &x[i][q * kWords], recip, 1, bad);
       }
     }
   }
