@@ -152,6 +152,25 @@ __device__ __forceinline__ void store4(uint8_t* p, bool vec, int64_t left, uint3
   }
 }
 
+// sqrt.approx and rcp.approx are off by at most one unit in the last place; below FP32's normal range they read zero.
+__device__ __forceinline__ float root(float v) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// scale_code() of the root of v, from v itself, so that it does not hang on the root's rounding: r <= 1.75 2^k exactly where
+// v <= 3.0625 4^k (a square that FP32 holds, and the next larger v has a root that rounds to more than 1.75 2^k).  With
+// v = f 2^E: k = floor(E / 2), one more where E is odd and 2 f > 3.0625.
+__device__ __forceinline__ uint32_t root_scale_code(uint32_t v_bits) {
+  const uint32_t e = v_bits >> 23;
+  return e == 0 ? 127u : (e + 1) / 2 + 55u + ((e & 1u) == 0 && (v_bits & 0x7FFFFFu) > 0x440000u ? 1u : 0u);
+}
+
 // Root y = r / scale, 0 <= y <= 448, on the E4M3 grid, at least its least step 2^-9 unless y = 0.
 // Stochastic: 16 random bits are added below the three fraction bits and the rest is cut off; below 2^-6, where the
 // grid is even, the same is done at y + 2^-6, whose unit is that grid's.
@@ -211,9 +230,9 @@ __device__ __forceinline__ void update(const Table& t, const Entry& e, const Blo
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    r[i] = __fsqrt_rn(v[i]);   // rounded correctly: the block's scale is read off it
-    // the quotient is only added to a parameter: two units in the last place of the step
-    p[i] = fmaf(p[i], t.decay, -t.step_size * __fdividef(m[i], fmaf(r[i], t.root_bias, t.eps)));
+    r[i] = root(v[i]);
+    // a few units in the last place of the step, which is small beside the parameter
+    p[i] = fmaf(p[i], t.decay, -t.step_size * m[i] * reciprocal(fmaf(r[i], t.root_bias, t.eps)));
   }
   uint32_t noise[4] = {};
   if constexpr (kStochastic) {
@@ -228,17 +247,17 @@ __device__ __forceinline__ void update(const Table& t, const Entry& e, const Blo
   if (sizeof(P) == 4 && e.copy) store4(e.copy + i0, vec, left, p);
   if constexpr (kEight) {
     uint32_t top_m = max(max(__float_as_uint(m[0]) & 0x7FFFFFFFu, __float_as_uint(m[1]) & 0x7FFFFFFFu), max(__float_as_uint(m[2]) & 0x7FFFFFFFu, __float_as_uint(m[3]) & 0x7FFFFFFFu));
-    uint32_t top_r = max(max(__float_as_uint(r[0]) & 0x7FFFFFFFu, __float_as_uint(r[1]) & 0x7FFFFFFFu), max(__float_as_uint(r[2]) & 0x7FFFFFFFu, __float_as_uint(r[3]) & 0x7FFFFFFFu));
-    top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
-    if (max(top_m, top_r) >= 0x7F800000u) {
+    uint32_t top_v = max(max(__float_as_uint(v[0]) & 0x7FFFFFFFu, __float_as_uint(v[1]) & 0x7FFFFFFFu), max(__float_as_uint(v[2]) & 0x7FFFFFFFu, __float_as_uint(v[3]) & 0x7FFFFFFFu));
+    top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
+    if (max(top_m, top_v) >= 0x7F800000u) {
       // something is not finite (the same for the whole warp): it becomes NaN and stays out of the scales
       top_m = max(max(finite_bits(m[0]), finite_bits(m[1])), max(finite_bits(m[2]), finite_bits(m[3])));
-      top_r = max(max(finite_bits(r[0]), finite_bits(r[1])), max(finite_bits(r[2]), finite_bits(r[3])));
-      top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_r = __reduce_max_sync(0xFFFFFFFFu, top_r);
+      top_v = max(max(finite_bits(v[0]), finite_bits(v[1])), max(finite_bits(v[2]), finite_bits(v[3])));
+      top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) m[i] += m[i] - m[i], r[i] += r[i] - r[i];
     }
-    const uint32_t code_m = scale_code(top_m), code_r = scale_code(top_r);
+    const uint32_t code_m = scale_code(top_m), code_r = root_scale_code(top_v);
     const float im = scale_recip(code_m), ir = scale_recip(code_r);
     store4(static_cast<State*>(e.m) + i0, vec, left, pack4(m[0] * im, m[1] * im, m[2] * im, m[3] * im));
 #pragma unroll
@@ -252,21 +271,18 @@ __device__ __forceinline__ void update(const Table& t, const Entry& e, const Blo
 }
 
 template <class P, class G, bool kEight, bool kStochastic>
-__global__ void __launch_bounds__(256) adamw_kernel(const __grid_constant__ Table t) {
+__global__ void __launch_bounds__(256, kEight ? 4 : 2) adamw_kernel(const __grid_constant__ Table t) {
   if (t.skip && *t.skip) return;
   const float clip = t.grad_scale ? *t.grad_scale : 1.f;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  // each thread block takes a run of pieces, its warps one after another: the tensor is searched once and then followed
-  const uint32_t begin = (uint32_t)((uint64_t)t.pieces * blockIdx.x / gridDim.x), end = (uint32_t)((uint64_t)t.pieces * (blockIdx.x + 1) / gridDim.x);
-  uint32_t piece = begin + warp;
-  if (piece >= end) return;
-  int at_tensor = 0, hi = t.count;
-  while (hi - at_tensor > 1) {
-    const int mid = (at_tensor + hi) / 2;
-    if (t.first_piece[mid] <= piece) at_tensor = mid; else hi = mid;
-  }
-  for (; piece < end; piece += 8) {
-    while (t.first_piece[at_tensor + 1] <= piece) ++at_tensor;
+  // the warps of the whole grid sweep the pieces together: what is read and written at one time lies close together
+  int at_tensor = 0;
+  for (uint32_t piece = blockIdx.x * 8 + warp; piece < t.pieces; piece += gridDim.x * 8) {
+    int hi = t.count;   // the tensor whose pieces hold this one: not before the last one's
+    while (hi - at_tensor > 1) {
+      const int mid = (at_tensor + hi) / 2;
+      if (t.first_piece[mid] <= piece) at_tensor = mid; else hi = mid;
+    }
     const Entry& e = t.entry[at_tensor];
     const bool aligned = e.n > 0;
     const int64_t n = aligned ? e.n : -e.n, at = (int64_t)(piece - t.first_piece[at_tensor]) * kPiece;
