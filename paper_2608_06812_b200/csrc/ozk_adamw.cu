@@ -164,12 +164,9 @@ __device__ __forceinline__ float reciprocal(float x) {
   return r;
 }
 // scale_code() of the root of v, from v itself, so that it does not hang on the root's rounding: r <= 1.75 2^k exactly where
-// v <= 3.0625 4^k (a square that FP32 holds, and the next larger v has a root that rounds to more than 1.75 2^k).  With
-// v = f 2^E: k = floor(E / 2), one more where E is odd and 2 f > 3.0625.
-__device__ __forceinline__ uint32_t root_scale_code(uint32_t v_bits) {
-  const uint32_t e = v_bits >> 23;
-  return e == 0 ? 127u : (e + 1) / 2 + 55u + ((e & 1u) == 0 && (v_bits & 0x7FFFFFu) > 0x440000u ? 1u : 0u);
-}
+// v <= 3.0625 4^k (a square that FP32 holds, and the next larger v has a root that rounds to more than 1.75 2^k).  3.0625 4^k
+// has the bits ((2 k + 128) << 23) + 0x440000, so the least such k is ((bits - 0x440001) >> 24) - 63, and the code 119 + k.
+__device__ __forceinline__ uint32_t root_scale_code(uint32_t v_bits) { return v_bits < 0x00800000u ? 127u : ((v_bits - 0x440001u) >> 24) + 56u; }
 
 // Root y = r / scale, 0 <= y <= 448, on the E4M3 grid, at least its least step 2^-9 unless y = 0.
 // Stochastic: 16 random bits are added below the three fraction bits and the rest is cut off; below 2^-6, where the
@@ -183,33 +180,49 @@ __device__ __forceinline__ float root_on_grid(float y, uint32_t noise) {
   }
   return y > 0.f ? fmaxf(q, 0.001953125f) : y;
 }
-// BF16 by adding 16 random bits below it and cutting off the rest; what is not finite stays.
+// BF16 by adding 16 random bits below it and cutting off the rest; infinities stay as they are, NaN is kept from the carry.
 __device__ __forceinline__ float bf16_stochastic(float p, uint32_t noise) {
-  const uint32_t u = __float_as_uint(p);
-  return (u & 0x7F800000u) == 0x7F800000u ? p : __uint_as_float((u + (noise & 0xFFFFu)) & 0xFFFF0000u);
+  const float q = __uint_as_float((__float_as_uint(p) + (noise & 0xFFFFu)) & 0xFFFF0000u);
+  return p == p ? q : p;
 }
 
+// One lane's four elements of a block, by pointers to them: the blocks of a piece lie at fixed distances.
+template <class P, class G, bool kEight>
+struct Lane {
+  using State = typename std::conditional<kEight, uint8_t, float>::type;
+  P* p;
+  const G* g;
+  State *m, *v;
+  __nv_bfloat16* copy;   // may be NULL
+  uint8_t *m_scale, *v_scale;
+  uint32_t index;        // of the first element, modulo 2^32: part of the hash
+  __device__ __forceinline__ Lane(const Entry& e, int64_t at, int lane) {
+    const int64_t i = at + lane * 4;
+    p = static_cast<P*>(e.param) + i, g = static_cast<const G*>(e.grad) + i, m = static_cast<State*>(e.m) + i, v = static_cast<State*>(e.v) + i;
+    copy = sizeof(P) == 4 && e.copy ? e.copy + i : nullptr;
+    if constexpr (kEight) m_scale = e.m_scale + at / kBlock, v_scale = e.v_scale + at / kBlock;
+    index = (uint32_t)i;
+  }
+};
 template <class P, class G, bool kEight>
 struct Block {
-  using State = typename std::conditional<kEight, uint8_t, float>::type;
+  using L = Lane<P, G, kEight>;
   Raw<P> p;
   Raw<G> g;
-  Raw<State> m, v;
+  Raw<typename L::State> m, v;
   uint32_t m_scale, v_scale;
-  __device__ __forceinline__ void load(const Entry& e, int64_t at, int lane, bool vec, int64_t n) {
-    const int64_t i0 = at + lane * 4, left = n - i0;
-    p.load(static_cast<const P*>(e.param) + i0, vec, left);
-    g.load(static_cast<const G*>(e.grad) + i0, vec, left);
-    m.load(static_cast<const State*>(e.m) + i0, vec, left);
-    v.load(static_cast<const State*>(e.v) + i0, vec, left);
-    if constexpr (kEight) m_scale = e.m_scale[at / kBlock], v_scale = e.v_scale[at / kBlock];
+  __device__ __forceinline__ void load(const L& l, int b, bool vec, int64_t left) {
+    p.load(l.p + b * kBlock, vec, left);
+    g.load(l.g + b * kBlock, vec, left);
+    m.load(l.m + b * kBlock, vec, left);
+    v.load(l.v + b * kBlock, vec, left);
+    if constexpr (kEight) m_scale = l.m_scale[b], v_scale = l.v_scale[b];
   }
 };
 
 template <class P, class G, bool kEight, bool kStochastic>
-__device__ __forceinline__ void update(const Table& t, const Entry& e, const Block<P, G, kEight>& x, int64_t at, int lane, bool vec, int64_t n, float clip, uint32_t key) {
-  using State = typename Block<P, G, kEight>::State;
-  const int64_t i0 = at + lane * 4, left = n - i0;
+__device__ __forceinline__ void update(const Table& t, const Lane<P, G, kEight>& l, const Block<P, G, kEight>& x, int b, int lane, bool vec, int64_t left, float clip,
+                                       uint32_t key) {
   const Pair clip2 = pair(clip, clip), b1 = pair(t.beta1, t.beta1), c1 = pair(t.one_minus_beta1, t.one_minus_beta1), b2 = pair(t.beta2, t.beta2),
              c2 = pair(t.one_minus_beta2, t.one_minus_beta2);
   float p[4], m[4], v[4], r[4];
@@ -237,16 +250,18 @@ __device__ __forceinline__ void update(const Table& t, const Entry& e, const Blo
   uint32_t noise[4] = {};
   if constexpr (kStochastic) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) noise[i] = mix((uint32_t)(i0 + i) ^ key);
+    for (int i = 0; i < 4; ++i) noise[i] = mix((l.index + (uint32_t)(b * kBlock + i)) ^ key);
   }
   if constexpr (kStochastic && sizeof(P) == 2) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = bf16_stochastic(p[i], noise[i]);
   }
-  store4(static_cast<P*>(e.param) + i0, vec, left, p);
-  if (sizeof(P) == 4 && e.copy) store4(e.copy + i0, vec, left, p);
+  store4(l.p + b * kBlock, vec, left, p);
+  if (sizeof(P) == 4 && l.copy) store4(l.copy + b * kBlock, vec, left, p);
   if constexpr (kEight) {
-    uint32_t top_m = max(max(__float_as_uint(m[0]) & 0x7FFFFFFFu, __float_as_uint(m[1]) & 0x7FFFFFFFu), max(__float_as_uint(m[2]) & 0x7FFFFFFFu, __float_as_uint(m[3]) & 0x7FFFFFFFu));
+    // The maxima pass over NaN (m) or show what is not finite as larger than all else (v, whose bits are compared).  An m that is not
+    // finite without its v being so can only be a NaN that was there before.
+    uint32_t top_m = __float_as_uint(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))) & 0x7FFFFFFFu;
     uint32_t top_v = max(max(__float_as_uint(v[0]) & 0x7FFFFFFFu, __float_as_uint(v[1]) & 0x7FFFFFFFu), max(__float_as_uint(v[2]) & 0x7FFFFFFFu, __float_as_uint(v[3]) & 0x7FFFFFFFu));
     top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
     if (max(top_m, top_v) >= 0x7F800000u) {
@@ -259,14 +274,14 @@ __device__ __forceinline__ void update(const Table& t, const Entry& e, const Blo
     }
     const uint32_t code_m = scale_code(top_m), code_r = root_scale_code(top_v);
     const float im = scale_recip(code_m), ir = scale_recip(code_r);
-    store4(static_cast<State*>(e.m) + i0, vec, left, pack4(m[0] * im, m[1] * im, m[2] * im, m[3] * im));
+    store4(l.m + b * kBlock, vec, left, pack4(m[0] * im, m[1] * im, m[2] * im, m[3] * im));
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = root_on_grid<kStochastic>(r[i] * ir, noise[i]);
-    store4(static_cast<State*>(e.v) + i0, vec, left, pack4(r[0], r[1], r[2], r[3]));
-    if (lane == 0) e.m_scale[at / kBlock] = (uint8_t)code_m, e.v_scale[at / kBlock] = (uint8_t)code_r;
+    store4(l.v + b * kBlock, vec, left, pack4(r[0], r[1], r[2], r[3]));
+    if (lane == 0) l.m_scale[b] = (uint8_t)code_m, l.v_scale[b] = (uint8_t)code_r;
   } else {
-    store4(static_cast<State*>(e.m) + i0, vec, left, m);
-    store4(static_cast<State*>(e.v) + i0, vec, left, v);
+    store4(l.m + b * kBlock, vec, left, m);
+    store4(l.v + b * kBlock, vec, left, v);
   }
 }
 
@@ -288,18 +303,21 @@ __global__ void __launch_bounds__(256, kEight ? 4 : 2) adamw_kernel(const __grid
     const int64_t n = aligned ? e.n : -e.n, at = (int64_t)(piece - t.first_piece[at_tensor]) * kPiece;
     const uint32_t key = mix(t.first_tensor + (uint32_t)at_tensor + 1u) ^ t.seed_key;
     if (aligned && at + kPiece <= n) {
+      const Lane<P, G, kEight> l(e, at, lane);
       Block<P, G, kEight> x[kPieceBlocks];
 #pragma unroll
-      for (int b = 0; b < kPieceBlocks; ++b) x[b].load(e, at + b * kBlock, lane, true, n);
+      for (int b = 0; b < kPieceBlocks; ++b) x[b].load(l, b, true, 4);
 #pragma unroll
-      for (int b = 0; b < kPieceBlocks; ++b) update<P, G, kEight, kStochastic>(t, e, x[b], at + b * kBlock, lane, true, n, clip, key);
+      for (int b = 0; b < kPieceBlocks; ++b) update<P, G, kEight, kStochastic>(t, l, x[b], b, lane, true, 4, clip, key);
     } else {
 #pragma unroll 1
       for (int64_t a = at; a < n && a < at + kPiece; a += kBlock) {
         const bool vec = aligned && a + kBlock <= n;
+        const int64_t left = n - a - lane * 4;
+        const Lane<P, G, kEight> l(e, a, lane);
         Block<P, G, kEight> x;
-        x.load(e, a, lane, vec, n);
-        update<P, G, kEight, kStochastic>(t, e, x, a, lane, vec, n, clip, key);
+        x.load(l, 0, vec, left);
+        update<P, G, kEight, kStochastic>(t, l, x, 0, lane, vec, left, clip, key);
       }
     }
   }

@@ -34,13 +34,12 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
   return u < 0x7F800000u ? u : 0u;
 }
 // UE8M0 code of the least power of two 2^e >= 2^-127 with amax <= 448 * 2^e (127, i.e. 1, for a block of zeros).
-// With amax = f 2^E, 1 <= f < 2, and 448 = 1.75 * 2^8: e = E - 8 + (f > 1.75).
+// With amax = f 2^E, 1 <= f < 2, and 448 = 1.75 * 2^8: e = E - 8 + (f > 1.75), the last by a carry out of the fraction bits.
 __device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits) {
-  const int c = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  return amax_bits == 0 ? 127u : (uint32_t)max(c, 0);
+  return amax_bits == 0 ? 127u : (uint32_t)max((int)((amax_bits + 0x1FFFFFu) >> 23) - 8, 0);
 }
 // 2^(c - 127) and its reciprocal; c = 0 is the subnormal 2^-127.
-__device__ __forceinline__ float scale_value(uint32_t c) { return __uint_as_float(c ? c << 23 : 1u << 22); }
+__device__ __forceinline__ float scale_value(uint32_t c) { return __uint_as_float(max(c << 23, 1u << 22)); }
 __device__ __forceinline__ float scale_recip(uint32_t c) { return __uint_as_float((254u - c) << 23); }   // c <= 247 from scale_code
 // x / scale where x is finite, else NaN: x - x is 0 or NaN.
 __device__ __forceinline__ float scaled(float x, float recip) { return fmaf(x, recip, x - x); }
