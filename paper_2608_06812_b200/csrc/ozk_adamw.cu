@@ -220,9 +220,9 @@ struct Block {
   }
 };
 
+// One block; returns the codes of its new scales (m in the low half, v in the high half).
 template <class P, class G, bool kEight, bool kStochastic>
-__device__ __forceinline__ void update(const Table& t, const Lane<P, G, kEight>& l, const Block<P, G, kEight>& x, int b, int lane, bool vec, int64_t left, float clip,
-                                       uint32_t key) {
+__device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEight>& l, const Block<P, G, kEight>& x, int b, bool vec, int64_t left, float clip, uint32_t key) {
   const Pair clip2 = pair(clip, clip), b1 = pair(t.beta1, t.beta1), c1 = pair(t.one_minus_beta1, t.one_minus_beta1), b2 = pair(t.beta2, t.beta2),
              c2 = pair(t.one_minus_beta2, t.one_minus_beta2);
   float p[4], m[4], v[4], r[4];
@@ -278,15 +278,16 @@ __device__ __forceinline__ void update(const Table& t, const Lane<P, G, kEight>&
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = root_on_grid<kStochastic>(r[i] * ir, noise[i]);
     store4(l.v + b * kBlock, vec, left, pack4(r[0], r[1], r[2], r[3]));
-    if (lane == 0) l.m_scale[b] = (uint8_t)code_m, l.v_scale[b] = (uint8_t)code_r;
+    return code_m | code_r << 16;
   } else {
     store4(l.m + b * kBlock, vec, left, m);
     store4(l.v + b * kBlock, vec, left, v);
+    return 0;
   }
 }
 
 template <class P, class G, bool kEight, bool kStochastic>
-__global__ void __launch_bounds__(256, kEight ? 4 : 2) adamw_kernel(const __grid_constant__ Table t) {
+__global__ void __launch_bounds__(256, !kEight ? 2 : sizeof(P) == 4 ? 3 : 4) adamw_kernel(const __grid_constant__ Table t) {
   if (t.skip && *t.skip) return;
   const float clip = t.grad_scale ? *t.grad_scale : 1.f;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -305,10 +306,16 @@ __global__ void __launch_bounds__(256, kEight ? 4 : 2) adamw_kernel(const __grid
     if (aligned && at + kPiece <= n) {
       const Lane<P, G, kEight> l(e, at, lane);
       Block<P, G, kEight> x[kPieceBlocks];
+      uint32_t codes = 0;
 #pragma unroll
       for (int b = 0; b < kPieceBlocks; ++b) x[b].load(l, b, true, 4);
 #pragma unroll
-      for (int b = 0; b < kPieceBlocks; ++b) update<P, G, kEight, kStochastic>(t, l, x[b], b, lane, true, 4, clip, key);
+      for (int b = 0; b < kPieceBlocks; ++b) {
+        const uint32_t c = update<P, G, kEight, kStochastic>(t, l, x[b], b, true, 4, clip, key);
+        if (lane == b) codes = c;
+      }
+      // the scales of the four blocks in one request each: single bytes, one request at a time, cost 0.28 of 0.97 ms over 256 M parameters
+      if (kEight && lane < kPieceBlocks) l.m_scale[lane] = (uint8_t)codes, l.v_scale[lane] = (uint8_t)(codes >> 16);
     } else {
 #pragma unroll 1
       for (int64_t a = at; a < n && a < at + kPiece; a += kBlock) {
@@ -317,7 +324,8 @@ __global__ void __launch_bounds__(256, kEight ? 4 : 2) adamw_kernel(const __grid
         const Lane<P, G, kEight> l(e, a, lane);
         Block<P, G, kEight> x;
         x.load(l, 0, vec, left);
-        update<P, G, kEight, kStochastic>(t, l, x, 0, lane, vec, left, clip, key);
+        const uint32_t c = update<P, G, kEight, kStochastic>(t, l, x, 0, vec, left, clip, key);
+        if (kEight && lane == 0) *l.m_scale = (uint8_t)c, *l.v_scale = (uint8_t)(c >> 16);
       }
     }
   }
@@ -384,8 +392,8 @@ extern "C" ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t co
     t.first_piece[t.count] = pieces;
     t.pieces = pieces;
     if (pieces == 0) continue;
-    // small steps: a warp for every piece; large ones: as many thread blocks as run at a time, several times over
-    const int64_t most = (int64_t)device_sm_count() * 16, wanted = ceil_div(pieces, 8);
+    // a warp for every piece; from 32 thread blocks per multiprocessor on (eight times what runs at a time) each takes several
+    const int64_t most = (int64_t)device_sm_count() * 32, wanted = ceil_div(pieces, 8);
     const unsigned blocks = (unsigned)(wanted < most ? wanted : most);
     const bool eight = o->state_bits == 8, stochastic = o->stochastic && (eight || o->param_type == OZK_BF16);
     cudaError_t e;

@@ -27,8 +27,21 @@ def _up(n: int, m: int) -> int:
     return -(-n // m) * m
 
 
-def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream(index: int) -> int:
+    """The raw handle of the current stream of a device."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _call(index: int, name: str, *args) -> None:
+    """Calls the library with the device current, and raises its errors."""
+    fn = getattr(ozk.lib(), name)
+    if torch._C._cuda_getDevice() == index:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args)
+    if status != ozk.OZK_OK:
+        raise ozk.OzkError(status, name)
 
 
 def _type(t: torch.Tensor, what: str) -> int:
@@ -44,24 +57,25 @@ def _need_cuda(t: torch.Tensor, what: str) -> None:
 
 
 # The product's scratch, one for each device and stream (calls on one stream are ordered, calls on two may overlap).
-_workspaces: dict[tuple[int, int], torch.Tensor] = {}
+_workspaces: dict[tuple[int, int], tuple[int, int, torch.Tensor]] = {}
 
 
-def _workspace(device: torch.device, stream: int) -> torch.Tensor:
-    ws = _workspaces.get((device.index, stream))
+def _workspace(index: int, stream: int) -> tuple[int, int, torch.Tensor]:
+    """(address, bytes, tensor)"""
+    ws = _workspaces.get((index, stream))
     if ws is None:
-        ws = torch.zeros(ozk.ozk_fp8_gemm_workspace_bytes(), dtype=torch.uint8, device=device)
-        _workspaces[device.index, stream] = ws
+        size = ozk.ozk_fp8_gemm_workspace_bytes()
+        t = torch.zeros(size, dtype=torch.uint8, device=torch.device("cuda", index))
+        ws = _workspaces[index, stream] = (t.data_ptr(), size, t)
     return ws
 
 
-def check_async(device: torch.device | None = None) -> None:
+def check_async(device: torch.device | int | None = None) -> None:
     """Waits for the current stream and raises OzkError if a wait inside a product kernel on it had run out."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
-    stream = _stream(device)
-    if (device.index, stream) in _workspaces:
-        with torch.cuda.device(device):
-            ozk.check(ozk.ozk_get_workspace_status(_workspaces[device.index, stream].data_ptr(), stream), "product")
+    index = torch.cuda.current_device() if device is None else torch.device("cuda", device).index if isinstance(device, int) else device.index
+    stream = _stream(index)
+    if (index, stream) in _workspaces:
+        _call(index, "ozk_get_workspace_status", _workspaces[index, stream][0], stream)
 
 
 class Fp8Matrix:
@@ -92,6 +106,10 @@ class Fp8Matrix:
         if (not floats and scales.dtype != torch.uint8) or scales.device != codes.device or not scales.is_contiguous() or want is None or tuple(scales.shape) != want:
             raise ValueError(f"scales of {rows} x {cols} by {kind}: {scales.dtype} {tuple(scales.shape)}, wanted {want} on {codes.device}")
         self.codes, self.scales, self.rows, self.cols, self.kind = codes, scales, rows, cols, kind
+        self.index = codes.device.index
+        # what the quantisers are given, and what a matrix to be written is compared with
+        self._target = (codes.data_ptr(), ld, scales.data_ptr())
+        self._form = (rows, cols, kind, floats, self.index)
         if floats:
             code = ozk.OZK_SCALE_LINES_F32 if kind == ROWS else ozk.OZK_SCALE_TILES_F32
         else:
@@ -99,6 +117,7 @@ class Fp8Matrix:
         self.ld = ld
         # the operand summed over its columns, and over its rows
         self._operand = [ozk.ozk_fp8_operand(codes.data_ptr(), ld, scales.data_ptr(), code, over) for over in (0, 1)]
+        self._at = [ctypes.addressof(o) for o in self._operand]
 
     @classmethod
     def empty(cls, rows: int, cols: int, kind: str, device: torch.device | str = "cuda") -> "Fp8Matrix":
@@ -128,48 +147,50 @@ class Fp8Matrix:
         return self.values8().float() * full
 
 
+_NONE = (None, 0, None)
+
+
 def _input(x: torch.Tensor) -> tuple[int, int, int, int]:
-    _need_cuda(x, "x")
-    if x.dim() != 2:
+    kind = _TYPES.get(x.dtype)
+    if kind is None:
+        _type(x, "x")
+    if not x.is_cuda or x.dim() != 2:
+        _need_cuda(x, "x")
         raise ValueError(f"x has two dimensions, not {x.dim()}")
     rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    ld, step = x.stride()
+    if cols > 1 and step != 1:
         raise ValueError("the rows of x are contiguous")
-    return rows, cols, _type(x, "x"), x.stride(0) if rows > 1 else max(cols, 1)
+    return rows, cols, kind, ld if rows > 1 else max(cols, 1)
 
 
-def _output(q: Fp8Matrix, x: torch.Tensor, kind: str) -> None:
-    if (q.rows, q.cols, q.kind) != (*x.shape, kind) or q.scales.dtype != torch.uint8 or q.codes.device != x.device:
-        raise ValueError(f"out is a {x.shape[0]} x {x.shape[1]} Fp8Matrix by {kind} with UE8M0 scales on {x.device}")
+def _output(q: Fp8Matrix, rows: int, cols: int, kind: str, index: int) -> tuple:
+    if q._form != (rows, cols, kind, False, index):
+        raise ValueError(f"out is a {rows} x {cols} Fp8Matrix by {kind} with UE8M0 scales on GPU {index}")
+    return q._target
 
 
 def quantize_lines(x: torch.Tensor, rows: "bool | Fp8Matrix | None" = True, cols: "bool | Fp8Matrix | None" = False):
     """x [rows, cols] (float32 or bfloat16) by 1 x 128 blocks, by 128 x 1 blocks, or both in one pass over x.
     `rows`, `cols`: whether that form is wanted, or an Fp8Matrix to write it to.  Returns the pair (None where not wanted)."""
     r, c, kind, ld = _input(x)
+    index = x.get_device()
     by_rows = Fp8Matrix.empty(r, c, ROWS, x.device) if rows is True else rows or None
     by_cols = Fp8Matrix.empty(r, c, COLS, x.device) if cols is True else cols or None
     if by_rows is None and by_cols is None:
         raise ValueError("neither rows nor columns are wanted")
-    args = []
-    for q, k in ((by_rows, ROWS), (by_cols, COLS)):
-        if q is None:
-            args += [None, 0, None]
-        else:
-            _output(q, x, k)
-            args += [q.codes.data_ptr(), q.ld, q.scales.data_ptr()]
-    with torch.cuda.device(x.device):
-        ozk.check(ozk.ozk_fp8_quantize_lines(r, c, x.data_ptr(), kind, ld, *args, _stream(x.device)), "quantize_lines")
+    to_rows = _NONE if by_rows is None else _output(by_rows, r, c, ROWS, index)
+    to_cols = _NONE if by_cols is None else _output(by_cols, r, c, COLS, index)
+    _call(index, "ozk_fp8_quantize_lines", r, c, x.data_ptr(), kind, ld, *to_rows, *to_cols, _stream(index))
     return by_rows, by_cols
 
 
 def quantize_tiles(x: torch.Tensor, out: Fp8Matrix | None = None) -> Fp8Matrix:
     """x [rows, cols] (float32 or bfloat16) by 128 x 128 tiles."""
     r, c, kind, ld = _input(x)
+    index = x.get_device()
     q = Fp8Matrix.empty(r, c, TILES, x.device) if out is None else out
-    _output(q, x, TILES)
-    with torch.cuda.device(x.device):
-        ozk.check(ozk.ozk_fp8_quantize_tiles(r, c, x.data_ptr(), kind, ld, q.codes.data_ptr(), q.ld, q.scales.data_ptr(), _stream(x.device)), "quantize_tiles")
+    _call(index, "ozk_fp8_quantize_tiles", r, c, x.data_ptr(), kind, ld, *_output(q, r, c, TILES, index), _stream(index))
     return q
 
 
@@ -187,24 +208,21 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
     n, kb = (b.cols, b.rows) if b_over else (b.rows, b.cols)
     if k != kb:
         raise ValueError(f"the operands are summed over {k} and {kb} elements")
-    device = a.codes.device
-    if b.codes.device != device:
+    index = a.index
+    if b.index != index:
         raise ValueError("the operands are on two devices")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
         if dtype not in _TYPES:
             raise ValueError(f"the result is float32 or bfloat16, not {dtype}")
-        out = torch.empty(m, _up(n, 8), dtype=dtype, device=device)[:, :n]   # rows at 16-byte boundaries
-    elif out.shape != (m, n) or out.device != device or (n > 1 and out.stride(1) != 1):
-        raise ValueError(f"out is [{m}, {n}] on {device} with contiguous rows")
-    ctype = _type(out, "out")
-    stream = _stream(device)
-    ldc = out.stride(0) if m > 1 else max(n, 1)
-    with torch.cuda.device(device):
-        ws = _workspace(device, stream)
-        ozk.check(ozk.ozk_fp8_gemm(m, n, k, a._operand[a_over], b._operand[b_over], out.data_ptr(), ctype, ldc, 1 if accumulate else 0,
-                                   ws.data_ptr(), ws.numel(), stream), "matmul")
+        out = torch.empty(m, _up(n, 8), dtype=dtype, device=a.codes.device)[:, :n]   # rows at 16-byte boundaries
+    elif out.shape != (m, n) or out.get_device() != index or (n > 1 and out.stride(1) != 1):
+        raise ValueError(f"out is [{m}, {n}] on GPU {index} with contiguous rows")
+    stream = _stream(index)
+    ws, size, _ = _workspace(index, stream)
+    _call(index, "ozk_fp8_gemm", m, n, k, a._at[a_over], b._at[b_over], out.data_ptr(), _type(out, "out"), out.stride(0) if m > 1 else max(n, 1),
+          1 if accumulate else 0, ws, size, stream)
     return out
 
 
@@ -267,6 +285,7 @@ class AdamWTable:
         self.tensors, self.count = lists, count
         self._table = (ozk.ozk_adamw_tensor * max(count, 1))()
         self._options = ozk.ozk_adamw_options()
+        self._table_at, self._options_at = ctypes.addressof(self._table), ctypes.addressof(self._options)
         if count:
             self.device = lists["params"][0].device
             at = lambda name, i: None if lists[name] is None else lists[name][i].data_ptr()  # noqa: E731
@@ -300,5 +319,4 @@ class AdamWTable:
         o.lr, (o.beta1, o.beta2), o.eps, o.weight_decay, o.step = lr, betas, eps, weight_decay, step
         o.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
         o.skip = None if skip is None else skip.data_ptr()
-        with torch.cuda.device(self.device):
-            ozk.check(ozk.ozk_adamw_step(ctypes.byref(self._table), self.count, o, _stream(self.device)), "AdamW step")
+        _call(self.device.index, "ozk_adamw_step", self._table_at, self.count, self._options_at, _stream(self.device.index))
