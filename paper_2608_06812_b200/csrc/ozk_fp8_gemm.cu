@@ -516,6 +516,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float* part, int splits
 }
 
 // ---- few rows of C --------------------------------------------------------------------
+constexpr int kMaxCluster = 8;
 constexpr int kRowsThreads = 6 * 32;   // producer, issuer, 4 warps for scales and epilogue
 template <int NT, bool kFloat>
 struct RowsShape {
@@ -536,11 +537,12 @@ struct __align__(8) RowsShared {
 };
 static_assert(sizeof(RowsShared) <= 512, "room reserved behind the stages");
 
-__device__ __forceinline__ float load_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 load_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_size() {
   uint32_t n;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
@@ -736,17 +738,29 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     __syncwarp();
     tmem_dealloc(tmem, S::kCols);
   }
-  // each CTA of the cluster joins its share of the sums, in the order of the ranges
+  // each CTA of the cluster joins its share of the sums, in the order of the ranges, four columns a thread
   const uint32_t local = smem_u32(sums);
-  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < p.out.M * 128; e += size * kRowsThreads) {
-    const int n = n0 + e % 128;
-    if (n >= p.out.N) continue;
-    float sum = 0.f;
-    for (int r = 0; r < size; ++r) sum += load_cluster_f32(map_to_cta(local + (uint32_t)e * 4u, (uint32_t)r));
-    T* c = static_cast<T*>(p.out.ptr) + (int64_t)(e / 128) * p.out.ld + n;
-    store_element(c, p.out.add ? load_element(c) + sum : sum);
+  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < p.out.M * 32; e += size * kRowsThreads) {
+    const int n = n0 + e % 32 * 4, left = p.out.N - n;
+    if (left <= 0) continue;
+    float4 v[kMaxCluster];
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r)
+      if (r < size) v[r] = load_cluster_f32x4(map_to_cta(local + (uint32_t)e * 16u, (uint32_t)r));
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r)
+      if (r < size) sum[0] += v[r].x, sum[1] += v[r].y, sum[2] += v[r].z, sum[3] += v[r].w;
+    T* c = static_cast<T*>(p.out.ptr) + (int64_t)(e / 32) * p.out.ld + n;
+    if (sizeof(T) == 2 && p.out.tma && left >= 4) {
+      *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) store_element(c + k, p.out.add ? load_element(c + k) + sum[k] : sum[k]);
+    }
   }
-  cluster_arrive();   // no CTA leaves while another reads its sums
+  cluster_arrive_relaxed();   // no CTA leaves while another reads its sums; nothing was written that another waits for
   cluster_wait();
 }
 
@@ -860,7 +874,7 @@ ozk_status run_rows(ProductParams p, int64_t K, bool floats, bool bf16, cudaStre
   if (sms < 1) return OZK_ERR_CUDA;
   // two CTAs fit a multiprocessor: split K over a cluster while that fills them
   int cluster = 2 * sms / tiles;
-  cluster = cluster < 1 ? 1 : cluster > 8 ? 8 : cluster;
+  cluster = cluster < 1 ? 1 : cluster > kMaxCluster ? kMaxCluster : cluster;
   if (cluster > p.groups) cluster = p.groups;
   bool ok;
   switch (NT) {

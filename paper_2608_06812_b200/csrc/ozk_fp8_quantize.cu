@@ -9,74 +9,6 @@ namespace {
 
 using namespace fp8;
 
-// 16 consecutive elements of a row from column c on; zeros beyond `left` elements.
-template <class T, bool kVec>
-__device__ __forceinline__ void load16(const T* p, int left, float (&x)[16]) {
-  if (left <= 0) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-  } else if (kVec && left >= 16) {
-    if constexpr (sizeof(T) == 2) {
-      const uint4* q = reinterpret_cast<const uint4*>(p);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4 w = __ldg(q + h);
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[8 * h + 2 * i] = bf16_lo(v[i]), x[8 * h + 2 * i + 1] = bf16_hi(v[i]);
-      }
-    } else {
-      const float4* q = reinterpret_cast<const float4*>(p);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float4 w = __ldg(q + h);
-        x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i < left ? load_element(p + i) : 0.f;
-  }
-}
-// 16 codes at a 16-byte aligned address; only the first `left` of them inside the matrix.
-__device__ __forceinline__ void store16(uint8_t* p, int left, const uint32_t (&w)[4]) {
-  if (left >= 16) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < left) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
-  }
-}
-
-// By rows: one warp per 512 columns of a row (one word of scales).  Eight lanes of 16 elements hold a block.
-template <class T, bool kVec>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Q, int64_t ldq, uint32_t* S) {
-  const int64_t groups = (cols + 511) / 512;
-  const int64_t item = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-  if (item >= groups * rows) return;
-  const int g = (int)(item / rows), r = (int)(item % rows), lane = threadIdx.x % 32;
-  const int c0 = g * 512 + lane * 16;
-  float x[16];
-  load16<T, kVec>(X + (int64_t)r * ldx + c0, cols - c0, x);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, finite_bits(x[i]));
-#pragma unroll
-  for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  const uint32_t c = scale_code(top);
-  const float recip = scale_recip(c);
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = pack4(scaled(x[4 * i], recip), scaled(x[4 * i + 1], recip), scaled(x[4 * i + 2], recip), scaled(x[4 * i + 3], recip));
-  if (cols - c0 > 0) store16(Q + (int64_t)r * ldq + c0, cols - c0, w);
-  uint32_t word = c;
-  word |= __shfl_sync(0xFFFFFFFFu, c, 8) << 8;
-  word |= __shfl_sync(0xFFFFFFFFu, c, 16) << 16;
-  word |= __shfl_sync(0xFFFFFFFFu, c, 24) << 24;
-  if (lane == 0) S[(int64_t)g * rows + r] = word;
-}
-
 // ---- 128 x 128 tiles ------------------------------------------------------------------
 // A tile per thread block, held in registers as it lies in memory: it is read once for both orientations.  Thread t has, of
 // rows t / 8 + 32 i, the 16 bytes from byte (t % 8) * 16 of every 128: eight lanes read whole 128-byte lines.
@@ -154,6 +86,45 @@ __device__ __forceinline__ void store_piece(uint8_t* q, int left, const uint32_t
   }
 }
 
+// By rows: a warp takes 512 columns (one word of scales) of kR rows, all loaded before the first is reduced.  Each 16-byte
+// piece of a lane lies beside its neighbours'; 16 lanes (BF16) or all 32 (FP32) hold a block.  The warps of a thread block take
+// consecutive rows, whose words of scales are neighbours: single words far apart cost more than the codes.
+template <class T, bool kVec, int kR>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Q, int64_t ldq, uint32_t* S) {
+  using W = Words<T>;
+  constexpr int kPiece = W::kPiece, kPieces = 512 / (32 * kPiece), kLanes = kBlock / kPiece;
+  const int64_t strips = (rows + kR - 1) / kR, item = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+  const int g = (int)(item / strips), r0 = (int)(item % strips) * kR, lane = threadIdx.x % 32;
+  if ((int64_t)g * 512 >= cols) return;
+  const int c0 = g * 512 + lane * kPiece;
+  uint32_t x[kR][kPieces][4];
+#pragma unroll
+  for (int i = 0; i < kR; ++i)
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q)
+      load_piece<T, kVec>(X + (int64_t)(r0 + i) * ldx + c0 + q * 32 * kPiece, r0 + i < rows ? cols - c0 - q * 32 * kPiece : 0, x[i][q]);
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const uint32_t* w = x[i][q];
+      uint32_t top = W::largest(W::larger(W::larger(W::magnitude(w[0]), W::magnitude(w[1])), W::larger(W::magnitude(w[2]), W::magnitude(w[3]))));
+      const bool bad = __any_sync(0xFFFFFFFFu, top >= 0x7F800000u);
+      if (bad)
+        top = W::largest(W::larger(W::larger(W::finite_magnitude(w[0]), W::finite_magnitude(w[1])), W::larger(W::finite_magnitude(w[2]), W::finite_magnitude(w[3]))));
+#pragma unroll
+      for (int d = 1; d < kLanes; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      const uint32_t c = scale_code(top);
+      const float recip = scale_recip(c);
+      const int left = cols - c0 - q * 32 * kPiece;
+      if (left > 0 && r0 + i < rows) store_piece<T>(Q + (int64_t)(r0 + i) * ldq + c0 + q * 32 * kPiece, left, w, &recip, 0, bad);
+      if constexpr (kLanes == 16) word |= (c | __shfl_down_sync(0xFFFFFFFFu, c, 16) << 8) << (16 * q); else word |= c << (8 * q);
+    }
+    if (lane == 0 && r0 + i < rows) S[(int64_t)g * rows + r0 + i] = word;
+  }
+}
+
 template <class T, bool kVec, bool kRows, bool kCols, bool kTiles>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
                                                             uint8_t* Qc, int64_t ldc, uint8_t* Sc) {
@@ -162,7 +133,7 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t 
   constexpr int kTileWords = kRowWords * 8;
   __shared__ uint32_t part[8][kCols ? kTileWords : 1];
   __shared__ float column_recip[kCols ? kBlock : 1];
-  __shared__ uint32_t tile_top[8];
+  __shared__ uint32_t tile_top[8], row_code[kRows ? kBlock : 1];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % 8;
   const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
   const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
@@ -227,16 +198,20 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t 
         const int col = c0 + q * 8 * kPiece;
         if (col < cols) store_piece<T>(Qr + (int64_t)r * ldr + col, cols - col, &x[i][q * kWords], &recip, 0, bad);
       }
-      if (c == 0) {
-        uint8_t* s = Sr + ((int64_t)(tc / 4) * rows + r) * 4;
-        s[tc % 4] = (uint8_t)code;
-        if (tc + 1 == tiles_c)
-          for (int b = tc % 4 + 1; b < 4; ++b) s[b] = 127;
-      }
+      if (c == 0) row_code[threadIdx.x / 8 + 32 * i] = code;
+    }
+  }
+  __syncthreads();
+  if constexpr (kRows) {   // a warp's 32 scale bytes in one request
+    const int i = (int)threadIdx.x - kBlock, r = tr * kBlock + i;
+    if (i >= 0 && r < rows) {
+      uint8_t* s = Sr + ((int64_t)(tc / 4) * rows + r) * 4;
+      s[tc % 4] = (uint8_t)row_code[i];
+      if (tc + 1 == tiles_c)
+        for (int b = tc % 4 + 1; b < 4; ++b) s[b] = 127;
     }
   }
   if constexpr (kCols || kTiles) {
-    __syncthreads();
     float tile_recip = 0.f;
     if constexpr (kTiles) {
       uint32_t t = tile_top[0];
@@ -297,14 +272,23 @@ bool good_codes(const uint8_t* q, int64_t ld, int64_t cols, const void* scales, 
   return q && scales && aligned16(q) && ld % 16 == 0 && ld >= cols && (reinterpret_cast<uintptr_t>(scales) & (scale_align - 1)) == 0;
 }
 
+// Four rows a warp once that still leaves every multiprocessor 16 warps; one row a warp where there are few, for the latency.
+template <class T, bool kVec>
+cudaError_t launch_rows(int rows, int cols, const T* X, int64_t ldx, uint8_t* Q, int64_t ld, uint32_t* S, cudaStream_t st) {
+  const int64_t groups = ceil_div(cols, 512);
+  if (groups * ceil_div(rows, 4) >= (int64_t)device_sm_count() * 16)
+    quantize_rows_kernel<T, kVec, 4><<<(unsigned)ceil_div(groups * ceil_div(rows, 4), 8), 256, 0, st>>>(X, ldx, rows, cols, Q, ld, S);
+  else
+    quantize_rows_kernel<T, kVec, 1><<<(unsigned)ceil_div(groups * rows, 8), 256, 0, st>>>(X, ldx, rows, cols, Q, ld, S);
+  return cudaGetLastError();
+}
+
 template <class T, bool kVec>
 cudaError_t launch_lines(int rows, int cols, const T* X, int64_t ldx, uint8_t* Qr, int64_t ldr, uint8_t* Sr, uint8_t* Qc, int64_t ldc, uint8_t* Sc,
                          cudaStream_t st) {
   const int64_t tiles = ceil_div(rows, kBlock) * ceil_div(cols, kBlock);
-  if (!Qc)
-    quantize_rows_kernel<T, kVec><<<(unsigned)ceil_div((int64_t)rows * ceil_div(cols, 512), 8), 256, 0, st>>>(X, ldx, rows, cols, Qr, ldr,
-                                                                                                        reinterpret_cast<uint32_t*>(Sr));
-  else if (Qr)
+  if (!Qc) return launch_rows<T, kVec>(rows, cols, X, ldx, Qr, ldr, reinterpret_cast<uint32_t*>(Sr), st);
+  if (Qr)
     quantize_tile_kernel<T, kVec, true, true, false><<<(unsigned)tiles, 256, 0, st>>>(X, ldx, rows, cols, Qr, ldr, Sr, Qc, ldc, Sc);
   else
     quantize_tile_kernel<T, kVec, false, true, false><<<(unsigned)tiles, 256, 0, st>>>(X, ldx, rows, cols, nullptr, 0, nullptr, Qc, ldc, Sc);

@@ -107,6 +107,9 @@ class Fp8Matrix:
             raise ValueError(f"scales of {rows} x {cols} by {kind}: {scales.dtype} {tuple(scales.shape)}, wanted {want} on {codes.device}")
         self.codes, self.scales, self.rows, self.cols, self.kind = codes, scales, rows, cols, kind
         self.index = codes.device.index
+        # views that are asked for at every step
+        self._values8 = codes.view(torch.float8_e4m3fn)[:, :cols]
+        self._words = None if floats or kind == TILES else scales.transpose(1, 2)
         # what the quantisers are given, and what a matrix to be written is compared with
         self._target = (codes.data_ptr(), ld, scales.data_ptr())
         self._form = (rows, cols, kind, floats, self.index)
@@ -127,14 +130,16 @@ class Fp8Matrix:
 
     def values8(self) -> torch.Tensor:
         """The codes as torch's 8-bit type, [rows, cols], without the scales."""
-        return self.codes.view(torch.float8_e4m3fn)[:, :self.cols]
+        return self._values8
 
     def scale_codes(self) -> torch.Tensor:
         """Scales by stored block: [rows, blocks] (ROWS), [blocks, cols] (COLS), [row tiles, column tiles] (TILES)."""
-        if self.kind == TILES or self.scales.dtype == torch.float32:
+        if self._words is None:
             return self.scales
-        k = self.cols if self.kind == ROWS else self.rows
-        s = self.scales.permute(0, 2, 1).reshape(-1, self.scales.shape[1])[:-(-k // 128)]
+        k, lines = (self.cols, self.rows) if self.kind == ROWS else (self.rows, self.cols)
+        s = self._words.reshape(-1, lines)
+        if k % 512:
+            s = s[:-(-k // 128)]
         return s.T if self.kind == ROWS else s
 
     def dequantize(self) -> torch.Tensor:
