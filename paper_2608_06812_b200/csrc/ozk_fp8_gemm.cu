@@ -91,8 +91,6 @@ struct ProductParams {
   Operand a, b;
   Output out;          // C, or the partial sums [splits][M][ld] when splits > 1
   int tiles_m, tiles_n, splits, groups;   // groups = ceil(K / 512)
-  int whole;           // items before this one are whole tiles; from it on halves of 128 columns (UE8M0 kernel)
-  int items;
   int chunk_groups;    // groups summed in tensor memory before the sum is added to C in FP32
   StatusBlock* status;
 };
@@ -136,19 +134,17 @@ struct __align__(8) PairShared {
 static_assert(sizeof(PairShared) <= 512, "room reserved behind the stages");
 
 struct Item {
-  int m0, n0, width, split, g_begin, g_end;   // width: 256 columns, or 128
+  int m0, n0, split, g_begin, g_end;
 };
 __device__ __forceinline__ Item pair_item(const ProductParams& p, int item) {
   // Bands of kBand row tiles sweep the column tiles, so that the pairs at work at one time share few panels of A and B and each
   // panel of B is read from memory once a band.  8192^3, back to back: 455 us with bands of 8, 443 with 16, 454 with 24, 485 with 32.
   Item r;
-  const bool half = item >= p.whole;
-  const int j = item - p.whole, tile = half ? p.whole + j / 2 : item / p.splits;
-  r.split = half ? 0 : item - tile * p.splits;
-  r.width = half ? kTileN / 2 : kTileN;
+  const int tile = item / p.splits;
+  r.split = item - tile * p.splits;
   const int band = kBand * p.tiles_n, g = tile / band, rem = tile - g * band;
   const int rows = min(kBand, p.tiles_m - kBand * g);
-  r.n0 = rem / rows * kTileN + (half ? j % 2 * (kTileN / 2) : 0);
+  r.n0 = rem / rows * kTileN;
   r.m0 = (kBand * g + rem % rows) * kTileM;
   r.g_begin = (int)((int64_t)r.split * p.groups / p.splits);
   r.g_end = (int)((int64_t)(r.split + 1) * p.groups / p.splits);
@@ -210,7 +206,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
-  const int items = p.items;
+  const int items = p.tiles_m * p.tiles_n * p.splits;
 
   if (threadIdx.x == 0) {
     prefetch_tensormap(&map_a);
@@ -258,7 +254,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             int x, y;
             tile_at(p.a.contract_rows, it.m0 + rank * 128, b, x, y);
             tma_load_2d_pair(dst, &map_a, full, x, y);
-            tile_at(p.b.contract_rows, it.n0 + rank * (it.width / 2), b, x, y);   // 128 lines, of which a half tile uses 64
+            tile_at(p.b.contract_rows, it.n0 + rank * (kTileN / 2), b, x, y);
             tma_load_2d_pair(dst + S::kABytes, &map_b, full, x, y);
             ++issued;
             if (++stage == S::kStages) stage = 0, phase ^= 1u;
@@ -279,12 +275,10 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         uint32_t phase = 0, unit = 0, sf_unit = 0;
         const int a_lines = p.a.contract_rows, b_lines = p.b.contract_rows;
         const uint32_t a_step = operand_step(a_lines), b_step = operand_step(b_lines);
-        const uint32_t idesc_whole = kFloat ? idesc_f8(kTileM, kTileN) : idesc_mxf8(kTileM, kTileN, a_lines, b_lines);
-        [[maybe_unused]] const uint32_t idesc_half = idesc_mxf8(kTileM, kTileN / 2, a_lines, b_lines);
+        const uint32_t idesc = kFloat ? idesc_f8(kTileM, kTileN) : idesc_mxf8(kTileM, kTileN, a_lines, b_lines);
         bool ok = true;
         for (int item = pair; item < items && ok; item += npairs) {
           const Item it = pair_item(p, item);
-          const uint32_t idesc = kFloat || it.width == kTileN ? idesc_whole : idesc_half;
           for (int g0 = it.g_begin; g0 < it.g_end && ok; g0 += p.chunk_groups) {
             const int b_begin = 4 * g0, b_end = min(4 * min(it.g_end, g0 + p.chunk_groups), p.a.blocks);
             uint32_t acc = 0;
@@ -447,7 +441,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
           store_box<kBf16>(p.out, &map_c, box, lane, w, m, n + i * (128 / kPieces), it.split, p.out.add);
         }
       } else {
-        const int columns = it.width / 2, n = it.n0 + part * columns;   // of this warp
+        const int n = it.n0 + part * 128;
         for (int g0 = it.g_begin; g0 < it.g_end; g0 += p.chunk_groups, ++unit) {
           const uint32_t buf = unit % S::kBuffers;
           const bool later = g0 > it.g_begin;   // a later range of the same tile is added to the earlier ones
@@ -457,13 +451,12 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             break;
           }
           tc_fence_after();
-          const uint32_t from = lanes + buf * S::kBufferStep + part * columns;
+          const uint32_t from = lanes + buf * S::kBufferStep + part * 128;
           const bool shared_half = buf == 0 ? part == 1 : part == 0;   // holds the columns that the other accumulator shares
-          constexpr int kWidth = kBf16 ? 64 : 32;
-          const int pieces = columns / kWidth;
-#pragma unroll 1
-          for (int i = 0; i < pieces; ++i) {
-            const int c = buf == 0 && part == 1 ? pieces - 1 - i : i;   // those columns first
+          constexpr int kPieces = kBf16 ? 2 : 4, kWidth = kBf16 ? 64 : 32;
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            const int c = buf == 0 && part == 1 ? kPieces - 1 - i : i;   // those columns first
             uint32_t w[32];
             if constexpr (kBf16) {
               uint32_t d0[32], d1[32];
@@ -479,12 +472,12 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
               tmem_ld_32x32(from + c * 32, w);
               tmem_wait_ld();
             }
-            if ((i == 0 && shared_half) || i == pieces - 1) {
+            if ((i == 0 && shared_half) || i == kPieces - 1) {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) {
                 if (i == 0 && shared_half) mbar_arrive_cluster(overlap);
-                if (i == pieces - 1) mbar_arrive_cluster(empty0 + buf * 8);
+                if (i == kPieces - 1) mbar_arrive_cluster(empty0 + buf * 8);
               }
             }
             store_box<kBf16>(p.out, &map_c, box, lane, w, m, n + c * kWidth, it.split, p.out.add || later);
@@ -923,14 +916,8 @@ ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t*
   } else {
     map_c = map_a;   // not used
   }
-  int64_t items = tm * tn * splits;
-  p.whole = (int)items;
-  // A last round that would keep at most half of the pairs busy is given out in halves of 128 columns instead: half a round
-  // less.  4096^3: 256 tiles on 74 pairs, 4 rounds without and 3.5 with.
-  const int64_t rest = tm * tn % pairs;
-  if (!floats && splits == 1 && tm * tn > pairs && rest > 0 && 2 * rest <= pairs) p.whole = (int)(items - rest), items += rest;
+  const int64_t items = tm * tn * splits;
   if (items > INT32_MAX) return OZK_ERR_UNSUPPORTED;
-  p.items = (int)items;
   const int grid = (int)(items < pairs ? items : pairs);
   const bool ok = floats ? (out_bf16 ? launch_pair<true, true>(map_a, map_b, map_c, p, grid, st) : launch_pair<true, false>(map_a, map_b, map_c, p, grid, st))
                          : (out_bf16 ? launch_pair<false, true>(map_a, map_b, map_c, p, grid, st) : launch_pair<false, false>(map_a, map_b, map_c, p, grid, st));
