@@ -97,6 +97,7 @@ struct ProductParams {
 
 constexpr int kGroupK = 4 * kBlock;
 constexpr int kRangeGroups = 8192 / kGroupK;   // FP32 results: longest range summed by the tensor cores alone
+constexpr int kRowsRangeGroups = 8;            // the same in product_rows_kernel, where a shorter one is only a larger cluster
 
 // ---- CTA-pair kernel --------------------------------------------------------------------
 constexpr int kTileM = 256;
@@ -519,6 +520,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float* part, int splits
 
 // ---- few rows of C --------------------------------------------------------------------
 constexpr int kMaxCluster = 8;
+constexpr int kRowsMost = 128, kRowsMostFloat = 64;   // rows of C in one tile
 constexpr int kRowsThreads = 6 * 32;   // producer, issuer, 4 warps for scales and epilogue
 template <int NT, bool kFloat>
 struct RowsShape {
@@ -526,7 +528,7 @@ struct RowsShape {
   static constexpr int kStageBytes = kWBytes + NT * kBlock;
   static constexpr int kStages = NT == 128 ? 3 : 4;
   static constexpr int kSets = 4;                                   // scale words of four groups in flight (UE8M0)
-  static constexpr int kBuffers = kFloat ? (NT == 128 ? 2 : 4) : 1; // accumulators, one per block of 128 (FP32 scales)
+  static constexpr int kBuffers = kFloat ? 4 : 1;                   // accumulators, one per block of 128 (FP32 scales)
   static constexpr int kNeeded = kFloat ? kBuffers * NT : NT + kSets * 8;
   static constexpr int kCols = kNeeded <= 64 ? 64 : kNeeded <= 128 ? 128 : 256;
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 512 + 4 * 2 * NT * 4 + 1024;
@@ -551,7 +553,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
   return n;
 }
 
-// p.a: the few rows of C (lines of the instruction's column side), p.b: the lines that become its 128 rows.
+// p.a: the rows of C, NT at a time (the instruction's column side), p.b: the lines that become its 128 rows.
 template <int NT, bool kFloat, class T>
 __global__ void __launch_bounds__(kRowsThreads)
 product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ProductParams p) {
@@ -562,7 +564,9 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   float* block_scales = reinterpret_cast<float*>(tiles + S::kStages * S::kStageBytes + 512);   // [warp][2][NT]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank(), size = (int)cluster_size();
-  const int n0 = (int)(blockIdx.x / size) * 128;
+  // tiles of rows of C run fastest: the clusters that read the same lines of B do so at about the same time
+  const int tile = (int)(blockIdx.x / size), m0 = tile % p.tiles_m * NT, n0 = tile / p.tiles_m * 128;
+  const int rows = min(NT, p.out.M - m0);
   const int g_begin = (int)((int64_t)rank * p.groups / size), g_end = (int)((int64_t)(rank + 1) * p.groups / size);
   const int b_begin = 4 * g_begin, b_end = min(4 * g_end, p.a.blocks);
 
@@ -600,7 +604,8 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         int x, y;
         tile_at(p.b.contract_rows, n0, b, x, y);
         tma_load_2d(dst, &map_w, full, x, y);
-        tma_load_2d(dst + S::kWBytes, &map_x, full, b * kBlock, 0);
+        tile_at(p.a.contract_rows, m0, b, x, y);
+        tma_load_2d(dst + S::kWBytes, &map_x, full, x, y);
       }
       if (sh->abort) {   // copies in flight land before this CTA leaves
         const uint64_t t0 = global_timer_ns();
@@ -611,9 +616,9 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     }
   } else if (warp == 1) {
     {
-      const int w_lines = p.b.contract_rows;
-      const uint32_t w_step = operand_step(w_lines);
-      const uint32_t idesc = kFloat ? idesc_f8(128, NT) : idesc_mxf8(128, NT, w_lines, 0);
+      const int w_lines = p.b.contract_rows, x_lines = p.a.contract_rows;
+      const uint32_t w_step = operand_step(w_lines), x_step = operand_step(x_lines);
+      const uint32_t idesc = kFloat ? idesc_f8(128, NT) : idesc_mxf8(128, NT, w_lines, x_lines);
       for (int b = b_begin; b < b_end; ++b) {
         const int i = b - b_begin, stage = i % S::kStages, buf = i % S::kBuffers, set = (i / 4) % S::kSets;
         if (kFloat && !wait_warp(smem_u32(&sh->acc_empty[buf]), ((uint32_t)(i / S::kBuffers) & 1u) ^ 1u, &sh->abort, p.status, 0x910)) break;
@@ -621,14 +626,14 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         if (!wait_warp(smem_u32(&sh->full[stage]), (uint32_t)(i / S::kStages) & 1u, &sh->abort, p.status, 0x920 + stage)) break;
         tc_fence_after();
         const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
-        const uint64_t dw = operand_desc(w_lines, base), dx = smem_desc_sw128(base + S::kWBytes);
+        const uint64_t dw = operand_desc(w_lines, base), dx = operand_desc(x_lines, base + S::kWBytes);
         if (elect_one()) {
 #pragma unroll
           for (uint32_t ks = 0; ks < 4; ++ks) {
             if constexpr (kFloat)
-              mma_f8(tmem + buf * NT, dw + ks * w_step, dx + ks * 2u, idesc, ks ? 1u : 0u);
+              mma_f8(tmem + buf * NT, dw + ks * w_step, dx + ks * x_step, idesc, ks ? 1u : 0u);
             else
-              mma_mxf8(tmem, dw + ks * w_step, dx + ks * 2u, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
+              mma_mxf8(tmem, dw + ks * w_step, dx + ks * x_step, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
           }
           mma_commit(smem_u32(&sh->empty[stage]));
           if (kFloat || b + 1 == b_end) mma_commit(smem_u32(&sh->acc_full[kFloat ? buf : 0]));
@@ -656,7 +661,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
       constexpr int kPer = (NT + 31) / 32;
       float sx[kPer], sw = scale_tile_f32(p.b, n0, b_begin);
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, lane + 32 * j, b_begin) : 0.f;
+      for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, m0 + lane + 32 * j, b_begin) : 0.f;
       for (int b = b_begin; b < b_end; ++b) {
         const int i = b - b_begin, buf = i % S::kBuffers;
         float* s = mine + (i & 1) * NT;   // two, so that one barrier of the warp is enough
@@ -667,7 +672,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         if (b + 1 < b_end) {
           sw = scale_tile_f32(p.b, n0, b + 1);
 #pragma unroll
-          for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, lane + 32 * j, b + 1) : 0.f;
+          for (int j = 0; j < kPer; ++j) sx[j] = lane + 32 * j < NT ? scale_line_f32(p.a, m0 + lane + 32 * j, b + 1) : 0.f;
         }
         if (!wait_warp(smem_u32(&sh->acc_full[buf]), (uint32_t)(i / S::kBuffers) & 1u, &sh->abort, p.status, 0x930)) {
           ok = false;
@@ -703,7 +708,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int i = g - g_begin, set = i % S::kSets;
         uint32_t ww[4], wx[4];
         scale_words<4>(p.b, n0, lane, g, ww);
-        scale_words<(NT + 31) / 32>(p.a, 0, lane, g, wx);
+        scale_words<(NT + 31) / 32>(p.a, m0, lane, g, wx);
         if (!wait_warp(smem_u32(&sh->sf_empty[set]), ((uint32_t)(i / S::kSets) & 1u) ^ 1u, &sh->abort, p.status, 0x931)) {
           ok = false;
           break;
@@ -742,7 +747,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
   }
   // each CTA of the cluster joins its share of the sums, in the order of the ranges, four columns a thread
   const uint32_t local = smem_u32(sums);
-  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < p.out.M * 32; e += size * kRowsThreads) {
+  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < rows * 32; e += size * kRowsThreads) {
     const int n = n0 + e % 32 * 4, left = p.out.N - n;
     if (left <= 0) continue;
     float4 v[kMaxCluster];
@@ -753,7 +758,7 @@ product_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 #pragma unroll
     for (int r = 0; r < kMaxCluster; ++r)
       if (r < size) sum[0] += v[r].x, sum[1] += v[r].y, sum[2] += v[r].z, sum[3] += v[r].w;
-    T* c = static_cast<T*>(p.out.ptr) + (int64_t)(e / 32) * p.out.ld + n;
+    T* c = static_cast<T*>(p.out.ptr) + (int64_t)(m0 + e / 32) * p.out.ld + n;
     if (sizeof(T) == 2 && p.out.tma && left >= 4) {
       *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
     } else {
@@ -849,8 +854,10 @@ bool launch_rows(const CUtensorMap& map_x, const CUtensorMap& map_w, const Produ
 }
 template <int NT>
 bool launch_rows_as(bool floats, bool bf16, const CUtensorMap& map_x, const CUtensorMap& map_w, const ProductParams& p, int tiles, int cluster, cudaStream_t st) {
-  if (floats)
-    return bf16 ? launch_rows<NT, true, __nv_bfloat16>(map_x, map_w, p, tiles, cluster, st) : launch_rows<NT, true, float>(map_x, map_w, p, tiles, cluster, st);
+  if constexpr (NT <= kRowsMostFloat) {   // one accumulator a thread for each of the NT columns
+    if (floats)
+      return bf16 ? launch_rows<NT, true, __nv_bfloat16>(map_x, map_w, p, tiles, cluster, st) : launch_rows<NT, true, float>(map_x, map_w, p, tiles, cluster, st);
+  }
   return bf16 ? launch_rows<NT, false, __nv_bfloat16>(map_x, map_w, p, tiles, cluster, st) : launch_rows<NT, false, float>(map_x, map_w, p, tiles, cluster, st);
 }
 
@@ -867,23 +874,36 @@ bool check_operand(const ozk_fp8_operand* o, int64_t lines, int64_t k, Operand* 
 constexpr size_t kGemmStatusBytes = 1024;
 constexpr size_t kGemmWorkspace = 24u << 20;   // status, and the partial sums of at most one tile per CTA pair (74 x 256 KiB)
 
-// Few rows of C: the instruction's column side holds them, 16 to 128 at a time.
-ozk_status run_rows(ProductParams p, int64_t K, bool floats, bool bf16, cudaStream_t st) {
-  const int M = p.out.M, NT = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+// How product_rows_kernel would run: NT rows of C a tile, `cluster` CTAs along K.
+struct RowsPlan {
+  int NT, tiles_m, tiles_n, cluster;
+};
+RowsPlan rows_plan(const ProductParams& p, bool floats, bool f32_result, int sms) {
+  RowsPlan r;
+  const int most = floats ? kRowsMostFloat : kRowsMost;
+  // an A summed over its rows comes in rows of 128 lines
+  r.NT = p.a.contract_rows ? 128 : p.out.M <= 16 ? 16 : p.out.M <= 32 ? 32 : p.out.M <= 64 ? 64 : most;
+  r.tiles_m = (int)ceil_div(p.out.M, r.NT);
+  r.tiles_n = (int)ceil_div(p.out.N, 128);
+  // two CTAs fit a multiprocessor: K is split over a cluster while that fills them
+  const int64_t tiles = (int64_t)r.tiles_m * r.tiles_n;
+  int c = tiles >= 2 * sms ? 1 : (int)(2 * sms / tiles);
+  if (f32_result && c * kRowsRangeGroups < p.groups) c = (int)ceil_div(p.groups, kRowsRangeGroups);   // FP32 results: short ranges
+  if (c > p.groups) c = p.groups;
+  r.cluster = c > kMaxCluster ? kMaxCluster : c;
+  return r;
+}
+ozk_status run_rows(ProductParams p, const RowsPlan& r, int64_t K, bool floats, bool bf16, cudaStream_t st) {
   CUtensorMap map_x, map_w;
-  if (!operand_map(&map_x, p.a, K, NT) || !operand_map(&map_w, p.b, K, 128)) return OZK_ERR_CUDA;
-  const int tiles = (int)ceil_div(p.out.N, 128), sms = device_sm_count();
-  if (sms < 1) return OZK_ERR_CUDA;
-  // two CTAs fit a multiprocessor: split K over a cluster while that fills them
-  int cluster = 2 * sms / tiles;
-  cluster = cluster < 1 ? 1 : cluster > kMaxCluster ? kMaxCluster : cluster;
-  if (cluster > p.groups) cluster = p.groups;
+  if (!operand_map(&map_x, p.a, K, r.NT) || !operand_map(&map_w, p.b, K, 128)) return OZK_ERR_CUDA;
+  p.tiles_m = r.tiles_m, p.tiles_n = r.tiles_n;
+  const int tiles = r.tiles_m * r.tiles_n;
   bool ok;
-  switch (NT) {
-    case 16: ok = launch_rows_as<16>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
-    case 32: ok = launch_rows_as<32>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
-    case 64: ok = launch_rows_as<64>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
-    default: ok = launch_rows_as<128>(floats, bf16, map_x, map_w, p, tiles, cluster, st); break;
+  switch (r.NT) {
+    case 16: ok = launch_rows_as<16>(floats, bf16, map_x, map_w, p, tiles, r.cluster, st); break;
+    case 32: ok = launch_rows_as<32>(floats, bf16, map_x, map_w, p, tiles, r.cluster, st); break;
+    case 64: ok = launch_rows_as<64>(floats, bf16, map_x, map_w, p, tiles, r.cluster, st); break;
+    default: ok = launch_rows_as<128>(floats, bf16, map_x, map_w, p, tiles, r.cluster, st); break;
   }
   return ok ? OZK_OK : OZK_ERR_CUDA;
 }
@@ -974,9 +994,18 @@ ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* 
   p.splits = 1;
   p.groups = (int)ceil_div(K, kGroupK);
   p.status = static_cast<StatusBlock*>(workspace);
-  // Up to 128 rows the kernel for few rows reads B once with nothing to spare; an A summed over its rows has no 128-byte
-  // rows of k to serve as that kernel's column side.
-  if (M <= 128 && !a.contract_rows) return run_rows(p, K, floats, bf16, st);
+  const int sms = device_sm_count();
+  if (sms < 2) return OZK_ERR_CUDA;
+  const RowsPlan rows = rows_plan(p, floats, !bf16, sms);
+  // product_rows_kernel where it keeps more of the GPU busy than pairs of CTAs with 256 x 256 tiles would:
+  //   UE8M0: up to 128 rows, or while the pairs have tiles for half of them at most (and would split K and join).  Rows against pairs, us:
+  //     256 x 4096 x 4096 13.7 : 19.2, 512 x 4096 x 4096 17.9 : 24.9, 1024 x 2048 x 2048 13.7 : 21.4, but 384 x 8192 x 4096 (64 tiles) 26.4 : 18.3.
+  //   FP32 scales: one tile of rows, or at most 8 blocks a CTA, whose sums one CTA takes longer to scale than to form:
+  //     128 x 4096 x 4096 13.6 : 16.9, 512 x 1024 x 4096 12.9 : 15.6, but 512 x 2048 x 8192 (32 blocks) 33 : 23.
+  const int64_t pair_tiles = ceil_div(M, kTileM) * ceil_div(N, kTileN);
+  const bool few = floats ? rows.tiles_m == 1 || 4 * ceil_div(p.groups, rows.cluster) <= 8 : M <= kRowsMost || 2 * pair_tiles <= sms / 2;
+  const bool ranges_fit = bf16 || (int64_t)rows.cluster * kRowsRangeGroups >= p.groups;
+  if (few && ranges_fit) return run_rows(p, rows, K, floats, bf16, st);
   return run_pair(p, K, floats, bf16, static_cast<uint8_t*>(workspace), st);
 }
 

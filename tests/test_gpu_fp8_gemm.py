@@ -70,6 +70,7 @@ def check(c, a, b, over_rows, before=None):
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4], np.abs(got - want).max())
 
 
+# on both sides of every choice between the kernels, tile widths and splits of K
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 257, 300), (2, 130, 1024), (16, 64, 640), (17, 512, 384), (33, 200, 129), (64, 384, 2048), (61, 1000, 777), (100, 300, 520),
          (128, 128, 128), (129, 128, 640), (200, 264, 1000), (256, 256, 512), (257, 255, 1100), (300, 520, 2050), (700, 17, 260), (513, 1025, 96)]
 
@@ -103,7 +104,7 @@ def test_accumulate(way, m, n, k):
     lowbit.check_async()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (5, 8192, 512), (1024, 1024, 16384), (4096, 300, 256), (130, 4100, 8190), (2048, 2048, 9000)])
+@pytest.mark.parametrize("m,n,k", [(40, 100, 12000), (130, 700, 3000), (512, 512, 8192), (260, 256, 1024), (1, 4096, 4096), (5, 8192, 512), (1024, 1024, 16384), (4096, 300, 256), (130, 4100, 8190), (2048, 2048, 9000)])
 @pytest.mark.parametrize("way", ["forward", "dgrad", "wgrad"])
 def test_larger(way, m, n, k):
     a, b, over = operands(way, m, n, k, 3)
