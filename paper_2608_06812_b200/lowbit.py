@@ -64,6 +64,8 @@ def _workspace(index: int, stream: int) -> tuple[int, int, torch.Tensor]:
     """(address, bytes, tensor)"""
     ws = _workspaces.get((index, stream))
     if ws is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first product on a stream cannot be captured: make one before, for its workspace")
         size = ozk.ozk_fp8_gemm_workspace_bytes()
         t = torch.zeros(size, dtype=torch.uint8, device=torch.device("cuda", index))
         ws = _workspaces[index, stream] = (t.data_ptr(), size, t)
