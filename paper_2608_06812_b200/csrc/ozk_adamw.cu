@@ -2,7 +2,7 @@
 //
 // Every element is read and written once: 16.1 bytes with FP32 parameters, their BF16 copy, BF16 gradients and 8-bit states.  A warp
 // works on four blocks of 128 with a block's 128 elements over its lanes, so that a block's maximum is one warp reduction.
-// 256 M such parameters: 0.69 ms, 5.8 TB/s, bound by memory.  26 M BF16 parameters with 8-bit states (10.1 bytes): 74 us, 3.5 TB/s, bound
+// 256 M such parameters: 0.67 ms, 5.9 TB/s (0.75 ms in a long loop of them), bound by memory.  26 M BF16 parameters with 8-bit states (10.1 bytes): 71 us, 3.6 TB/s, bound
 // by the arithmetic, most of it the hash, the stochastic roundings and the maxima.  150 tensors of 5000: 6 us, and 7 us a step
 // of a loop, which the host needs to launch it.
 #include <math.h>
@@ -56,6 +56,19 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ (x >> 16);
 }
 
+// mix() of four consecutive numbers a, a ^ 1, a ^ 2, a ^ 3 (the first a multiple of four, XORed with anything): the low two bits do not
+// reach the first shift's result, so that step is done once.
+__device__ __forceinline__ void mix4(uint32_t a, uint32_t (&out)[4]) {
+  const uint32_t t = a ^ (a >> 16);
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    uint32_t x = (t ^ i) * 0x7feb352du;
+    x ^= x >> 15;
+    x *= 0x846ca68bu;
+    out[i] = x ^ (x >> 16);
+  }
+}
+
 // Pairs of floats, multiplied in one instruction; each operation rounds both by itself, as the scalar one does.
 struct Pair {
   uint64_t v;
@@ -73,6 +86,11 @@ __device__ __forceinline__ float2 both(Pair p) {
 __device__ __forceinline__ Pair operator*(Pair a, Pair b) {
   Pair r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair multiply_add(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
   return r;
 }
 // Sums one by one: a packed sum of packed products came out as if it had been contracted into multiply-adds (one in 400 moments,
@@ -187,7 +205,7 @@ __device__ __forceinline__ float root_on_grid(float y, uint32_t noise) {
   float q = y;
   if constexpr (kStochastic) {
     const float base = y < 0.015625f ? 0.015625f : 0.f;
-    q = __uint_as_float((__float_as_uint(y + base) + ((noise >> 16) << 4)) & 0xFFF00000u) - base;
+    q = __uint_as_float((__float_as_uint(y + base) + ((noise & 0xFFFF0000u) >> 12)) & 0xFFF00000u) - base;
   }
   return y > 0.f ? fmaxf(q, 0.001953125f) : y;
 }
@@ -249,19 +267,18 @@ __device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEig
     // every product and sum is rounded by itself: the rounding to 8 bits after it then does not hang on a contraction
     m2 = m2 * b1 + g * c1;
     v2 = v2 * b2 + (g * c2) * g;
-    const float2 mf = both(m2), vf = both(v2), pf = both(h ? x.p.hi() : x.p.lo());
-    m[2 * h] = mf.x, m[2 * h + 1] = mf.y, v[2 * h] = vf.x, v[2 * h + 1] = vf.y, p[2 * h] = pf.x, p[2 * h + 1] = pf.y;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[i] = root<kEight>(v[i]);
-    // a few units in the last place of the step, which is small beside the parameter
-    p[i] = fmaf(p[i], t.decay, -t.step_size * m[i] * reciprocal(fmaf(r[i], t.root_bias, t.eps)));
+    const float2 mf = both(m2), vf = both(v2);
+    m[2 * h] = mf.x, m[2 * h + 1] = mf.y, v[2 * h] = vf.x, v[2 * h + 1] = vf.y;
+    r[2 * h] = root<kEight>(vf.x), r[2 * h + 1] = root<kEight>(vf.y);
+    // the step is a few units in the last place off, which is little beside the parameter
+    const float2 d = both(multiply_add(pair(r[2 * h], r[2 * h + 1]), pair(t.root_bias, t.root_bias), pair(t.eps, t.eps)));
+    const Pair step = m2 * pair(-t.step_size, -t.step_size) * pair(reciprocal(d.x), reciprocal(d.y));
+    const float2 pf = both(multiply_add(h ? x.p.hi() : x.p.lo(), pair(t.decay, t.decay), step));
+    p[2 * h] = pf.x, p[2 * h + 1] = pf.y;
   }
   uint32_t noise[4] = {};
   if constexpr (kStochastic) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) noise[i] = mix((l.index + (uint32_t)(b * kBlock + i)) ^ key);
+    mix4((l.index + (uint32_t)(b * kBlock)) ^ key, noise);   // index is a multiple of four
   }
   if constexpr (kStochastic && sizeof(P) == 2) {
 #pragma unroll
