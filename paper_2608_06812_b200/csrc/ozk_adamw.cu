@@ -69,25 +69,6 @@ __device__ __forceinline__ void mix4(uint32_t a, uint32_t (&out)[4]) {
   }
 }
 
-// Pairs of floats, multiplied in one instruction; each operation rounds both by itself, as the scalar one does.
-struct Pair {
-  uint64_t v;
-};
-__device__ __forceinline__ Pair pair(float lo, float hi) {
-  Pair p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
-  return p;
-}
-__device__ __forceinline__ float2 both(Pair p) {
-  float2 f;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
-  return f;
-}
-__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
-  Pair r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
 __device__ __forceinline__ Pair multiply_add(Pair a, Pair b, Pair c) {
   Pair r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));

@@ -44,6 +44,26 @@ __device__ __forceinline__ float scale_recip(uint32_t c) { return __uint_as_floa
 // x / scale where x is finite, else NaN: x - x is 0 or NaN.
 __device__ __forceinline__ float scaled(float x, float recip) { return fmaf(x, recip, x - x); }
 
+// Pairs of floats, multiplied in one instruction; each operation rounds both by itself, as the scalar one does.
+struct Pair {
+  uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ float2 both(Pair p) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+  return f;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float load_element(const float* p) { return *p; }

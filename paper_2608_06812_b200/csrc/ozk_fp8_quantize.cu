@@ -3,8 +3,8 @@
 //   scale = 2^ceil(log2(amax / 448)), code = E4M3(x / scale): the division is exact, so both the scale and the code are
 //   determined bit for bit, whatever the order of the maximum.
 //
-// One pass over X for both orientations.  16384 x 8192 BF16 on one B200: by rows 73 us (5.5 TB/s), by columns 68 us (5.9), both 102 us
-// (5.3), by tiles 61 us (6.6); 8190 x 4100 FP32 by tiles 31 us (5.4).  Bound by memory, and with both orientations by instructions too.
+// One pass over X for both orientations.  16384 x 8192 BF16 on one B200: by rows 73 us (5.5 TB/s), by columns 69 us (5.9), both 100 us
+// (5.4), by tiles 61 us (6.6); 8190 x 4100 FP32 by tiles 31 us (5.4).  Bound by memory, and with both orientations by instructions too.
 #include "ozk_fp8.cuh"
 
 namespace ozk {
@@ -64,21 +64,22 @@ __device__ __forceinline__ void load_piece(const T* p, int left, uint32_t* w) {
     }
   }
 }
-// Its codes: x times a reciprocal that may differ from column to column, `bad`: NaN for what is not finite.
+// Its codes: x times reciprocals of scales, which may differ from column to column; `bad`: NaN for what is not finite.
 template <class T>
-__device__ __forceinline__ void store_piece(uint8_t* q, int left, const uint32_t* w, const float* recip, int step, bool bad) {
+__device__ __forceinline__ void store_piece(uint8_t* q, int left, const uint32_t* w, const Pair* recip, int step, bool bad) {
   constexpr int kPiece = Words<T>::kPiece;
   uint32_t out[kPiece / 4];
 #pragma unroll
   for (int k = 0; k < kPiece / 4; ++k) {
-    float y[4];
+    float2 y[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = Words<T>::value(w, 4 * k + i) * recip[(4 * k + i) * step];
-    if (bad) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = scaled(Words<T>::value(w, 4 * k + i), recip[(4 * k + i) * step]);
+    for (int h = 0; h < 2; ++h) {
+      const float a = Words<T>::value(w, 4 * k + 2 * h), b = Words<T>::value(w, 4 * k + 2 * h + 1);
+      const Pair r = recip[(2 * k + h) * step];
+      y[h] = both(pair(a, b) * r);
+      if (bad) y[h] = make_float2(scaled(a, both(r).x), scaled(b, both(r).y));
     }
-    out[k] = pack4(y[0], y[1], y[2], y[3]);
+    out[k] = pack4(y[0].x, y[0].y, y[1].x, y[1].y);
   }
   if (left >= kPiece) {
     if constexpr (kPiece == 8) *reinterpret_cast<uint2*>(q) = make_uint2(out[0], out[1]); else *reinterpret_cast<uint32_t*>(q) = out[0];
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 #pragma unroll
       for (int d = 1; d < kLanes; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
       const uint32_t c = scale_code(top);
-      const float recip = scale_recip(c);
+      const Pair recip = pair(scale_recip(c), scale_recip(c));
       const int left = cols - c0 - q * 32 * kPiece;
       if (left > 0 && r0 + i < rows) store_piece<T>(Q + (int64_t)(r0 + i) * ldq + c0 + q * 32 * kPiece, left, w, &recip, 0, bad);
       if constexpr (kLanes == 16) word |= (c | __shfl_down_sync(0xFFFFFFFFu, c, 16) << 8) << (16 * q); else word |= c << (8 * q);
@@ -129,13 +130,13 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 }
 
 template <class T, bool kVec, bool kRows, bool kCols, bool kTiles>
-__global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
                                                             uint8_t* Qc, int64_t ldc, uint8_t* Sc) {
   using W = Words<T>;
   constexpr int kPiece = W::kPiece, kPieces = W::kPieces, kWords = W::kWords, kRowWords = kPieces * kWords;   // words per thread and row
   constexpr int kTileWords = kRowWords * 8;
   __shared__ uint32_t part[8][kCols ? kTileWords : 1];
-  __shared__ float column_recip[kCols ? kBlock : 1];
+  __shared__ __align__(16) float column_recip[kCols ? kBlock : 1];
   __shared__ uint32_t tile_top[8], row_code[kRows ? kBlock : 1];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % 8;
   const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
@@ -186,23 +187,32 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t 
     const uint32_t t = __reduce_max_sync(0xFFFFFFFFu, max(max(row_top[0], row_top[1]), max(row_top[2], row_top[3])));
     if (lane == 0) tile_top[warp] = t;
   }
+  // the four rows' pieces, by reciprocals that belong to the row or to the columns
+  auto store = [&](uint8_t* Q, int64_t ld, auto recip_of, int step) {
+    uint8_t* at = Q + (int64_t)r0 * ld + c0;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const int col = q * 8 * kPiece;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Pair* recip = recip_of(q, i);
+        if (r0 + 32 * i < rows && c0 + col < cols)
+          store_piece<T>(at + (int64_t)(32 * i) * ld + col, cols - c0 - col, &x[i][q * kWords], recip, step, bad);
+      }
+    }
+  };
   if constexpr (kRows) {
+    Pair recip[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t top = row_top[i];
 #pragma unroll
       for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-      const int r = r0 + 32 * i;
-      if (r >= rows) continue;
       const uint32_t code = scale_code(top);
-      const float recip = scale_recip(code);
-#pragma unroll
-      for (int q = 0; q < kPieces; ++q) {
-        const int col = c0 + q * 8 * kPiece;
-        if (col < cols) store_piece<T>(Qr + (int64_t)r * ldr + col, cols - col, &x[i][q * kWords], &recip, 0, bad);
-      }
+      recip[i] = pair(scale_recip(code), scale_recip(code));
       if (c == 0) row_code[threadIdx.x / 8 + 32 * i] = code;
     }
+    store(Qr, ldr, [&](int, int i) { return &recip[i]; }, 0);
   }
   __syncthreads();
   if constexpr (kRows) {   // a warp's 32 scale bytes in one request
@@ -244,19 +254,19 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* X, int64_t 
       }
       __syncthreads();
     }
+    Pair recip[kTiles ? 1 : kPieces * kPiece / 2];
+    if constexpr (kTiles) {
+      recip[0] = pair(tile_recip, tile_recip);
+    } else {
 #pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-      const int col = c0 + q * 8 * kPiece;
-      float recip[kPiece];
+      for (int q = 0; q < kPieces; ++q)
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) recip[k] = kTiles ? tile_recip : column_recip[col - tc * kBlock + k];
-      if (col >= cols) continue;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = r0 + 32 * i;
-        if (r < rows) store_piece<T>(Qc + (int64_t)r * ldc + col, cols - col, &x[i][q * kWords], recip, 1, bad);
-      }
+        for (int k = 0; k < kPiece / 2; ++k) {
+          const float2 f = *reinterpret_cast<const float2*>(&column_recip[(q * 8 + c) * kPiece + 2 * k]);
+          recip[q * kPiece / 2 + k] = pair(f.x, f.y);
+        }
     }
+    store(Qc, ldc, [&](int q, int) { return &recip[kTiles ? 0 : q * kPiece / 2]; }, kTiles ? 0 : 1);
   }
 }
 
