@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
 }
 
 template <class T, bool kVec, bool kRows, bool kCols, bool kTiles>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
                                                             uint8_t* Qc, int64_t ldc, uint8_t* Sc) {
   using W = Words<T>;
   constexpr int kPiece = W::kPiece, kPieces = W::kPieces, kWords = W::kWords, kRowWords = kPieces * kWords;   // words per thread and row
