@@ -139,10 +139,8 @@ class Fp8Matrix:
         if self._words is None:
             return self.scales
         k, lines = (self.cols, self.rows) if self.kind == ROWS else (self.rows, self.cols)
-        s = self._words.reshape(-1, lines)
-        if k % 512:
-            s = s[:-(-k // 128)]
-        return s.T if self.kind == ROWS else s
+        blocks, s = -(-k // 128), self._words.contiguous()   # [groups][four blocks][lines]
+        return s.as_strided((lines, blocks), (1, lines)) if self.kind == ROWS else s.as_strided((blocks, lines), (lines, 1))
 
     def dequantize(self) -> torch.Tensor:
         """Codes times scales in float32."""
@@ -166,7 +164,7 @@ def _input(x: torch.Tensor) -> tuple[int, int, int, int]:
         raise ValueError(f"x has two dimensions, not {x.dim()}")
     rows, cols = x.shape
     ld, step = x.stride()
-    if cols > 1 and step != 1:
+    if cols > 1 and step != 1 and rows:
         raise ValueError("the rows of x are contiguous")
     return rows, cols, kind, ld if rows > 1 else max(cols, 1)
 
@@ -233,10 +231,15 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
     return out
 
 
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    flat = x.reshape(-1, x.shape[-1])
+    return flat if flat.stride(1) == 1 and flat.stride(0) >= flat.shape[1] else flat.contiguous()   # an expanded gradient has strides of 0
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, w8):
-        flat = x.reshape(-1, x.shape[-1])
+        flat = _rows(x)
         by_rows, by_cols = quantize_lines(flat, True, ctx.needs_input_grad[1])
         ctx.x8, ctx.w8, ctx.shape, ctx.types = by_cols, w8, x.shape, (x.dtype, w.dtype)
         return matmul(by_rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
@@ -244,7 +247,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         need_x, need_w = ctx.needs_input_grad[:2]
-        by_rows, by_cols = quantize_lines(dy.reshape(-1, dy.shape[-1]).contiguous(), need_x, need_w)
+        by_rows, by_cols = quantize_lines(_rows(dy), need_x, need_w)
         dx = matmul(by_rows, ctx.w8, over_rows=True, dtype=ctx.types[0]).reshape(ctx.shape) if need_x else None
         dw = matmul(by_cols, ctx.x8, dtype=torch.float32).to(ctx.types[1]) if need_w else None
         return dx, dw, None
@@ -252,8 +255,9 @@ class _Linear(torch.autograd.Function):
 
 def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> torch.Tensor:
     """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms).
-    x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps."""
-    return _Linear.apply(x, w, quantize_tiles(w.detach()) if w8 is None else w8)
+    x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
+    the backward pass, which reads it)."""
+    return _Linear.apply(x, w, quantize_tiles(_rows(w.detach())) if w8 is None else w8)
 
 
 class AdamWTable:

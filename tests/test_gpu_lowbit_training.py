@@ -67,6 +67,23 @@ def test_batched_input_partial_gradients_and_16_bits():
     assert x.grad.shape == x.shape and x.grad.dtype == torch.bfloat16
 
 
+def test_strided_and_empty_arguments():
+    x, w = integers((130, 20), 4, 7).T, integers((130, 40), 4, 8).T      # neither has contiguous rows
+    x, w = x.requires_grad_(), w.requires_grad_()
+    y = lowbit.linear(x, w)
+    y.backward(torch.ones(40, device="cuda").expand(20, 40))
+    assert torch.equal(y, (x.double() @ w.double().T).float())
+    assert torch.equal(x.grad, w.double().sum(0).float().expand(20, -1)) and torch.equal(w.grad, x.double().sum(0).float().expand(40, -1))
+    y = lowbit.linear(x, w)
+    x.grad = w.grad = None
+    y.sum().backward()                                                     # a gradient expanded from one number
+    assert torch.equal(x.grad, w.double().sum(0).float().expand(20, -1))
+    x, w = torch.zeros(0, 64, device="cuda", requires_grad=True), torch.randn(32, 64, device="cuda", requires_grad=True)
+    y = lowbit.linear(x, w)
+    y.sum().backward()
+    assert y.shape == (0, 32) and x.grad.shape == (0, 64) and (w.grad == 0).all()
+
+
 def test_the_example_learns():
     """The 8-bit run follows the 32-bit one: both lose 80 % of the loss, and the 8-bit one ends within a factor of two."""
     import os
