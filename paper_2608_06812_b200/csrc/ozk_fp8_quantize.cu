@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
   using W = Words<T>;
   constexpr int kPiece = W::kPiece, kPieces = W::kPieces, kWords = W::kWords, kRowWords = kPieces * kWords;   // words per thread and row
   constexpr int kTileWords = kRowWords * 8;
-  __shared__ uint32_t part[8][kCols ? kTileWords : 1];
+  __shared__ __align__(16) uint32_t part[8][kCols ? kTileWords : 1];
   __shared__ __align__(16) float column_recip[kCols ? kBlock : 1];
   __shared__ uint32_t tile_top[8], row_code[kRows ? kBlock : 1];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % 8;
