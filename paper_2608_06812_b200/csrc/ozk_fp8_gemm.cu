@@ -791,27 +791,35 @@ EncodeTiledFn encode_fn() {
   }
   return f;
 }
+// cuTensorMapEncodeTiled, which wants a current context: a host thread whose first CUDA call this is has none until the runtime makes the
+// device's primary context current.
+bool encode(CUtensorMap* map, CUtensorMapDataType type, uint32_t rank, void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+            CUtensorMapL2promotion promotion) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint32_t estr[3] = {1, 1, 1};
+  auto call = [&] { return fn(map, type, rank, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE); };
+  CUresult r = call();
+  if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+    r = call();
+  }
+  return r == CUDA_SUCCESS;
+}
 // Tiles of an operand: `lines` x 128 values of k, rows of 128 bytes along k (or along the lines).  What lies outside reads as zero.
 bool operand_map(CUtensorMap* map, const Operand& o, int64_t K, int lines) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)(o.contract_rows ? o.lines : K), (cuuint64_t)(o.contract_rows ? K : o.lines)};
-  cuuint64_t strides[1] = {(cuuint64_t)o.ld};
-  cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)(o.contract_rows ? kBlock : lines)};
-  cuuint32_t estr[2] = {1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(o.codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[2] = {(cuuint64_t)(o.contract_rows ? o.lines : K), (cuuint64_t)(o.contract_rows ? K : o.lines)};
+  const cuuint64_t strides[1] = {(cuuint64_t)o.ld};
+  const cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)(o.contract_rows ? kBlock : lines)};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(o.codes), dims, strides, box, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 bool output_map(CUtensorMap* map, const Output& o, bool bf16, int splits) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
   const cuuint64_t size = bf16 ? 2 : 4;
-  cuuint64_t dims[3] = {(cuuint64_t)o.N, (cuuint64_t)o.M, (cuuint64_t)splits};
-  cuuint64_t strides[2] = {(cuuint64_t)o.ld * size, (cuuint64_t)o.ld * size * (cuuint64_t)o.M};
-  cuuint32_t box[3] = {(cuuint32_t)(128 / size), 32, 1};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, o.ptr, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[3] = {(cuuint64_t)o.N, (cuuint64_t)o.M, (cuuint64_t)splits};
+  const cuuint64_t strides[2] = {(cuuint64_t)o.ld * size, (cuuint64_t)o.ld * size * (cuuint64_t)o.M};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / size), 32, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, o.ptr, dims, strides, box, CU_TENSOR_MAP_L2_PROMOTION_NONE);
 }
 
 constexpr int kMaxDevices = 64;
