@@ -356,13 +356,33 @@ typedef struct {
  *   because the tensor cores truncate when they accumulate.  Results do not depend on timing.
  *   M, N, K = 0 are allowed (K = 0: C = 0, or unchanged with accumulate).  M, N, K < 2^31.
  * workspace: device memory of ozk_fp8_gemm_workspace_bytes() (one size for all shapes), 256-byte aligned, whose first
- * kibibyte has been cleared once (cudaMemset); NULL takes the registered one.  Calls that share it must be ordered by
- * the caller.  A bounded device wait that expired is recorded at its start, see ozk_get_workspace_status().
+ * kibibyte has been cleared once (cudaMemset); NULL takes the registered one.  A call may be several launches that pass sums
+ * through it: calls that share one must be made one after the other on one stream (by one host thread at a time), and a graph that
+ * captured calls must not run beside others with the same workspace.  A bounded device wait that expired is recorded at its start, see
+ * ozk_get_workspace_status().
  * The call only enqueues kernels and, after one eager call, may be captured into a CUDA graph. */
 size_t ozk_fp8_gemm_workspace_bytes(void);
 ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B,
                         void* C, int c_type, int64_t ldc, int accumulate,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same with the two parts of the workspace apart.  status: a kibibyte, cleared once, 256-byte aligned; calls on any stream may
+ * share it.  scratch: memory for the sums of this call alone, 256-byte aligned, until it has run; most products need none (NULL, 0).
+ * One that needs more than scratch_bytes returns OZK_ERR_WORKSPACE and enqueues nothing; ozk_fp8_gemm_plan() says how much. */
+ozk_status ozk_fp8_gemm_scratch(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B,
+                                void* C, int c_type, int64_t ldc, int accumulate,
+                                void* status, void* scratch, size_t scratch_bytes, void* stream);
+
+/* How a product runs on a GPU with `sms` multiprocessors (0: the current device): pairs = 1 if pairs of CTAs form the tiles, 0 for
+ * clusters along K; the tiles' extents and number; the ranges of K that a tile is split into; the scratch that is needed.
+ * Needs no GPU if sms is given. */
+typedef struct {
+  int pairs, tile_rows, tile_cols, splits;
+  int64_t tiles;
+  size_t scratch_bytes;
+} ozk_fp8_plan;
+ozk_status ozk_fp8_gemm_plan(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, int c_type, int sms,
+                             ozk_fp8_plan* plan);
 
 /* ozk_get_async_status() for a workspace that was passed to a call rather than registered. */
 ozk_status ozk_get_workspace_status(void* workspace, void* stream);

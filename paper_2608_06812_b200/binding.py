@@ -33,6 +33,10 @@ class ozk_fp8_operand(ctypes.Structure):
     _fields_ = [("codes", c_void_p), ("ld", c_int64), ("scales", c_void_p), ("scale_kind", c_int), ("contract_rows", c_int)]
 
 
+class ozk_fp8_plan(ctypes.Structure):
+    _fields_ = [("pairs", c_int), ("tile_rows", c_int), ("tile_cols", c_int), ("splits", c_int), ("tiles", c_int64), ("scratch_bytes", c_size_t)]
+
+
 class ozk_adamw_tensor(ctypes.Structure):
     _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
                 ("copy", c_void_p), ("n", c_int64)]
@@ -81,6 +85,8 @@ SIGNATURES = {
     "ozk_fp8_quantize_tiles": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
     "ozk_fp8_gemm_workspace_bytes": (c_size_t, []),
     "ozk_fp8_gemm": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
+    "ozk_fp8_gemm_scratch": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ozk_fp8_gemm_plan": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int, c_void_p]),
     "ozk_adamw_step": (c_int, [c_void_p, c_int64, c_void_p, c_void_p]),
     "ozk_stage_mma_probe": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
 }
@@ -265,6 +271,18 @@ def ozk_fp8_gemm_workspace_bytes() -> int:
 def ozk_fp8_gemm(M, N, K, A, B, C, c_type, ldc, accumulate=0, workspace=None, workspace_bytes=0, stream=0) -> int:
     """A, B: ozk_fp8_operand structures."""
     return lib().ozk_fp8_gemm(M, N, K, ctypes.byref(A), ctypes.byref(B), C, c_type, ldc, accumulate, workspace, workspace_bytes, stream)
+
+
+def ozk_fp8_gemm_scratch(M, N, K, A, B, C, c_type, ldc, accumulate, status, scratch=None, scratch_bytes=0, stream=0) -> int:
+    """A, B: ozk_fp8_operand structures."""
+    return lib().ozk_fp8_gemm_scratch(M, N, K, ctypes.byref(A), ctypes.byref(B), C, c_type, ldc, accumulate, status, scratch, scratch_bytes, stream)
+
+
+def ozk_fp8_gemm_plan(M, N, K, A, B, c_type, sms=0) -> ozk_fp8_plan:
+    """A, B: ozk_fp8_operand structures."""
+    plan = ozk_fp8_plan()
+    check(lib().ozk_fp8_gemm_plan(M, N, K, ctypes.byref(A), ctypes.byref(B), c_type, sms, ctypes.byref(plan)), "ozk_fp8_gemm_plan")
+    return plan
 
 
 def ozk_adamw_step(tensors, count, options, stream=0) -> int:

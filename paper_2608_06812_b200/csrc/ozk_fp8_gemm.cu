@@ -921,27 +921,52 @@ ozk_status run_rows(ProductParams p, const RowsPlan& r, int64_t K, bool floats, 
   return ok ? OZK_OK : OZK_ERR_CUDA;
 }
 
-ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t* workspace, cudaStream_t st) {
-  const int64_t tm = ceil_div(p.out.M, kTileM), tn = ceil_div(p.out.N, kTileN);
+// Which kernel, and how it divides the work.
+struct Plan {
+  bool rows;
+  RowsPlan r;
+  int64_t tiles_m, tiles_n;   // of the pairs
+  int splits;
+  size_t scratch;             // partial sums of the splits in device memory
+};
+Plan product_plan(const ProductParams& p, bool floats, bool bf16, int sms) {
+  Plan q = {};
+  q.r = rows_plan(p, floats, !bf16, sms);
+  q.tiles_m = ceil_div(p.out.M, kTileM), q.tiles_n = ceil_div(p.out.N, kTileN);
+  const int64_t pair_tiles = q.tiles_m * q.tiles_n, row_ctas = (int64_t)q.r.tiles_m * q.r.tiles_n * q.r.cluster;
+  // product_rows_kernel where it keeps more of the GPU busy than pairs of CTAs with 256 x 256 tiles would:
+  //   UE8M0: up to 128 rows, or while the pairs have tiles for half of them at most (and would split K and join).  Rows against pairs, us:
+  //     256 x 4096 x 4096 13.7 : 19.2, 512 x 4096 x 4096 17.9 : 24.9, 1024 x 2048 x 2048 13.7 : 21.4, but 384 x 8192 x 4096 (64 tiles) 26.4 : 18.3.
+  //   FP32 scales: one tile of rows, or CTAs that all run at once with at most 8 blocks each, which take longer to scale than to form:
+  //     128 x 4096 x 4096 13.6 : 16.9, 512 x 1024 x 4096 12.9 : 15.6, but 512 x 2048 x 8192 (32 blocks) 33 : 23.
+  const bool few = floats ? q.r.tiles_m == 1 || (row_ctas <= 2 * sms && 4 * ceil_div(p.groups, q.r.cluster) <= 8)
+                          : p.out.M <= kRowsMost || 2 * pair_tiles <= sms / 2;
+  const bool ranges_fit = bf16 || (int64_t)q.r.cluster * kRowsRangeGroups >= p.groups;
+  q.rows = few && ranges_fit;
+  q.splits = 1;
+  if (q.rows) return q;
+  // fewer tiles than half the pairs: split K so that each pair has one range of at least 1024
+  const int pairs = sms / 2;
+  if (pair_tiles * 2 <= pairs) {
+    q.splits = (int)(pairs / pair_tiles);
+    if (q.splits > p.groups / 2) q.splits = p.groups / 2;
+    if (q.splits < 1) q.splits = 1;
+  }
+  if (q.splits > 1) q.scratch = (size_t)q.splits * p.out.M * (size_t)round_up(p.out.N, 4) * 4;
+  return q;
+}
+
+ozk_status run_pair(ProductParams p, const Plan& plan, int64_t K, bool floats, bool bf16, void* scratch, cudaStream_t st) {
+  const int64_t tm = plan.tiles_m, tn = plan.tiles_n;
   if (tm * tn > INT32_MAX) return OZK_ERR_UNSUPPORTED;
   const int pairs = device_sm_count() / 2;
-  if (pairs < 1) return OZK_ERR_CUDA;
+  const int splits = plan.splits;
   p.tiles_m = (int)tm, p.tiles_n = (int)tn;
   const Output c = p.out;
-  // fewer tiles than half the pairs: split K so that each pair has one range of at least 1024
-  int splits = 1;
-  if (tm * tn * 2 <= pairs) {
-    splits = (int)(pairs / (tm * tn));
-    if (splits > p.groups / 2) splits = p.groups / 2;
-    if (splits < 1) splits = 1;
-  }
   p.splits = splits;
   const bool out_bf16 = bf16 && splits == 1;
   p.chunk_groups = out_bf16 || floats ? p.groups : kRangeGroups;
-  if (splits > 1) {
-    p.out = Output{workspace + kGemmStatusBytes, round_up(c.N, 4), c.M, c.N, 0, 1};
-    if ((size_t)splits * c.M * p.out.ld * 4 + kGemmStatusBytes > kGemmWorkspace) return OZK_ERR_UNSUPPORTED;
-  }
+  if (splits > 1) p.out = Output{scratch, round_up(c.N, 4), c.M, c.N, 0, 1};
   CUtensorMap map_a, map_b, map_c;
   if (!operand_map(&map_a, p.a, K, 128) || !operand_map(&map_b, p.b, K, kTileN / 2)) return OZK_ERR_CUDA;
   if (p.out.tma) {
@@ -973,26 +998,63 @@ ozk_status run_pair(ProductParams p, int64_t K, bool floats, bool bf16, uint8_t*
 
 using namespace ozk;
 
+namespace {
+
+// Arguments that do not depend on where the results go.
+ozk_status check_product(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, int c_type, ProductParams* p, bool* floats) {
+  if (M < 0 || N < 0 || K < 0 || !A || !B || (c_type != OZK_F32 && c_type != OZK_BF16)) return OZK_ERR_INVALID_ARG;
+  if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+  Operand a = {}, b = {};
+  if (K > 0 && M > 0 && N > 0 && (!check_operand(A, M, K, &a) || !check_operand(B, N, K, &b))) return OZK_ERR_INVALID_ARG;
+  *floats = a.kind >= OZK_SCALE_LINES_F32 || b.kind >= OZK_SCALE_LINES_F32;
+  if (*floats && (a.kind != OZK_SCALE_LINES_F32 || b.kind != OZK_SCALE_TILES_F32 || a.contract_rows || b.contract_rows))
+    return OZK_ERR_UNSUPPORTED;
+  *p = ProductParams{};
+  p->a = a, p->b = b;
+  p->out.M = (int)M, p->out.N = (int)N;
+  p->splits = 1;
+  p->groups = (int)ceil_div(K, kGroupK);
+  return OZK_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 size_t ozk_fp8_gemm_workspace_bytes(void) { return kGemmWorkspace; }
 
-ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, void* C, int c_type,
-                        int64_t ldc, int accumulate, void* workspace, size_t workspace_size, void* stream) {
-  if (M < 0 || N < 0 || K < 0 || !A || !B || ldc < N || (c_type != OZK_F32 && c_type != OZK_BF16) || (accumulate != 0 && accumulate != 1))
-    return OZK_ERR_INVALID_ARG;
-  if (M > INT32_MAX || N > INT32_MAX || K > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+ozk_status ozk_fp8_gemm_plan(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, int c_type, int sms, ozk_fp8_plan* plan) {
+  ProductParams p;
+  bool floats;
+  const ozk_status rc = check_product(M, N, K, A, B, c_type, &p, &floats);
+  if (rc != OZK_OK) return rc;
+  if (!plan || sms < 0) return OZK_ERR_INVALID_ARG;
+  *plan = ozk_fp8_plan{};
+  if (M == 0 || N == 0 || K == 0) return OZK_OK;
+  if (sms == 0) sms = device_sm_count();
+  if (sms < 2) return OZK_ERR_CUDA;
+  const Plan q = product_plan(p, floats, c_type == OZK_BF16, sms);
+  plan->pairs = q.rows ? 0 : 1;
+  plan->tile_rows = q.rows ? q.r.NT : kTileM;
+  plan->tile_cols = q.rows ? 128 : kTileN;
+  plan->tiles = q.rows ? (int64_t)q.r.tiles_m * q.r.tiles_n : q.tiles_m * q.tiles_n;
+  plan->splits = q.rows ? q.r.cluster : q.splits;
+  plan->scratch_bytes = q.scratch;
+  return OZK_OK;
+}
+
+ozk_status ozk_fp8_gemm_scratch(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, void* C, int c_type,
+                                int64_t ldc, int accumulate, void* status, void* scratch, size_t scratch_bytes, void* stream) {
+  ProductParams p;
+  bool floats;
+  const ozk_status rc = check_product(M, N, K, A, B, c_type, &p, &floats);
+  if (rc != OZK_OK) return rc;
+  if (ldc < N || (accumulate != 0 && accumulate != 1)) return OZK_ERR_INVALID_ARG;
   if (accumulate && c_type != OZK_F32) return OZK_ERR_UNSUPPORTED;
-  Operand a = {}, b = {};
-  if (K > 0 && M > 0 && N > 0 && (!check_operand(A, M, K, &a) || !check_operand(B, N, K, &b))) return OZK_ERR_INVALID_ARG;
-  const bool floats = a.kind >= OZK_SCALE_LINES_F32 || b.kind >= OZK_SCALE_LINES_F32;
-  if (floats && (a.kind != OZK_SCALE_LINES_F32 || b.kind != OZK_SCALE_TILES_F32 || a.contract_rows || b.contract_rows))
-    return OZK_ERR_UNSUPPORTED;
   if (M == 0 || N == 0) return OZK_OK;
   if (!C || (reinterpret_cast<uintptr_t>(C) & (c_type == OZK_F32 ? 3 : 1))) return OZK_ERR_INVALID_ARG;
-  if (!workspace) workspace = workspace_ptr(), workspace_size = workspace_bytes();
-  if (!workspace || workspace_size < kGemmWorkspace) return OZK_ERR_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(workspace) & 255) return OZK_ERR_INVALID_ARG;
+  if (!status) return OZK_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(status) & 255) || (reinterpret_cast<uintptr_t>(scratch) & 255)) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = c_type == OZK_BF16;
@@ -1001,26 +1063,21 @@ ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* 
     if (!accumulate && cudaMemset2DAsync(C, (size_t)ldc * size, 0, (size_t)N * size, (size_t)M, st) != cudaSuccess) return OZK_ERR_CUDA;
     return OZK_OK;
   }
-  ProductParams p = {};
-  p.a = a, p.b = b;
   p.out = Output{C, ldc, (int)M, (int)N, accumulate, aligned16(C) && ((size_t)ldc * size) % 16 == 0 ? 1 : 0};
-  p.splits = 1;
-  p.groups = (int)ceil_div(K, kGroupK);
-  p.status = static_cast<StatusBlock*>(workspace);
+  p.status = static_cast<StatusBlock*>(status);
   const int sms = device_sm_count();
   if (sms < 2) return OZK_ERR_CUDA;
-  const RowsPlan rows = rows_plan(p, floats, !bf16, sms);
-  // product_rows_kernel where it keeps more of the GPU busy than pairs of CTAs with 256 x 256 tiles would:
-  //   UE8M0: up to 128 rows, or while the pairs have tiles for half of them at most (and would split K and join).  Rows against pairs, us:
-  //     256 x 4096 x 4096 13.7 : 19.2, 512 x 4096 x 4096 17.9 : 24.9, 1024 x 2048 x 2048 13.7 : 21.4, but 384 x 8192 x 4096 (64 tiles) 26.4 : 18.3.
-  //   FP32 scales: one tile of rows, or CTAs that all run at once with at most 8 blocks each, which take longer to scale than to form:
-  //     128 x 4096 x 4096 13.6 : 16.9, 512 x 1024 x 4096 12.9 : 15.6, but 512 x 2048 x 8192 (32 blocks) 33 : 23.
-  const int64_t pair_tiles = ceil_div(M, kTileM) * ceil_div(N, kTileN), row_ctas = (int64_t)rows.tiles_m * rows.tiles_n * rows.cluster;
-  const bool few = floats ? rows.tiles_m == 1 || (row_ctas <= 2 * sms && 4 * ceil_div(p.groups, rows.cluster) <= 8)
-                          : M <= kRowsMost || 2 * pair_tiles <= sms / 2;
-  const bool ranges_fit = bf16 || (int64_t)rows.cluster * kRowsRangeGroups >= p.groups;
-  if (few && ranges_fit) return run_rows(p, rows, K, floats, bf16, st);
-  return run_pair(p, K, floats, bf16, static_cast<uint8_t*>(workspace), st);
+  const Plan plan = product_plan(p, floats, bf16, sms);
+  if (plan.rows) return run_rows(p, plan.r, K, floats, bf16, st);
+  if (plan.scratch > 0 && (!scratch || scratch_bytes < plan.scratch)) return OZK_ERR_WORKSPACE;   // before anything is enqueued
+  return run_pair(p, plan, K, floats, bf16, scratch, st);
+}
+
+ozk_status ozk_fp8_gemm(int64_t M, int64_t N, int64_t K, const ozk_fp8_operand* A, const ozk_fp8_operand* B, void* C, int c_type,
+                        int64_t ldc, int accumulate, void* workspace, size_t workspace_size, void* stream) {
+  if (!workspace) workspace = workspace_ptr(), workspace_size = workspace_bytes();
+  uint8_t* ws = workspace_size < kGemmWorkspace ? nullptr : static_cast<uint8_t*>(workspace);
+  return ozk_fp8_gemm_scratch(M, N, K, A, B, C, c_type, ldc, accumulate, ws, ws ? ws + kGemmStatusBytes : nullptr, ws ? kGemmWorkspace - kGemmStatusBytes : 0, stream);
 }
 
 }  // extern "C"

@@ -32,14 +32,18 @@ def _stream(index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _call(index: int, name: str, *args) -> None:
-    """Calls the library with the device current, and raises its errors."""
+def _code(index: int, name: str, *args) -> int:
+    """Calls the library with the device current."""
     fn = getattr(ozk.lib(), name)
     if torch._C._cuda_getDevice() == index:
-        status = fn(*args)
-    else:
-        with torch.cuda.device(index):
-            status = fn(*args)
+        return fn(*args)
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
+def _call(index: int, name: str, *args) -> None:
+    """The same, and raises the library's errors."""
+    status = _code(index, name, *args)
     if status != ozk.OZK_OK:
         raise ozk.OzkError(status, name)
 
@@ -56,28 +60,27 @@ def _need_cuda(t: torch.Tensor, what: str) -> None:
         raise ValueError(f"{what} is not on a GPU")
 
 
-# The product's scratch, one for each device and stream (calls on one stream are ordered, calls on two may overlap).
-_workspaces: dict[tuple[int, int], tuple[int, int, torch.Tensor]] = {}
+# The status word of the products' bounded waits, one for each device: (address, tensor).
+_statuses: dict[int, tuple[int, torch.Tensor]] = {}
 
 
-def _workspace(index: int, stream: int) -> tuple[int, int, torch.Tensor]:
-    """(address, bytes, tensor)"""
-    ws = _workspaces.get((index, stream))
-    if ws is None:
+def _status(index: int) -> int:
+    found = _statuses.get(index)
+    if found is None:
         if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("the first product on a stream cannot be captured: make one before, for its workspace")
-        size = ozk.ozk_fp8_gemm_workspace_bytes()
-        t = torch.zeros(size, dtype=torch.uint8, device=torch.device("cuda", index))
-        ws = _workspaces[index, stream] = (t.data_ptr(), size, t)
-    return ws
+            raise RuntimeError("the first product on a GPU cannot be captured: make one before, for its status word")
+        t = torch.zeros(1024, dtype=torch.uint8, device=torch.device("cuda", index))
+        torch.cuda.current_stream(index).synchronize()   # other streams may use it next
+        found = _statuses.setdefault(index, (t.data_ptr(), t))   # the first of two threads
+    return found[0]
 
 
-def check_async(device: torch.device | int | None = None) -> None:
-    """Waits for the current stream and raises OzkError if a wait inside a product kernel on it had run out."""
-    index = torch.cuda.current_device() if device is None else torch.device("cuda", device).index if isinstance(device, int) else device.index
-    stream = _stream(index)
-    if (index, stream) in _workspaces:
-        _call(index, "ozk_get_workspace_status", _workspaces[index, stream][0], stream)
+def check_async(device: torch.device | str | int | None = None) -> None:
+    """Waits for the current stream and raises OzkError if a wait inside a product kernel on that GPU had run out."""
+    index = device if isinstance(device, int) else None if device is None else torch.device(device).index
+    index = torch.cuda.current_device() if index is None else index
+    if index in _statuses:
+        _call(index, "ozk_get_workspace_status", _statuses[index][0], _stream(index))
 
 
 class Fp8Matrix:
@@ -224,10 +227,19 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
         out = torch.empty(m, _up(n, 8), dtype=dtype, device=a.codes.device)[:, :n]   # rows at 16-byte boundaries
     elif out.shape != (m, n) or out.get_device() != index or (n > 1 and out.stride(1) != 1):
         raise ValueError(f"out is [{m}, {n}] on GPU {index} with contiguous rows")
-    stream = _stream(index)
-    ws, size, _ = _workspace(index, stream)
-    _call(index, "ozk_fp8_gemm", m, n, k, a._at[a_over], b._at[b_over], out.data_ptr(), _type(out, "out"), out.stride(0) if m > 1 else max(n, 1),
-          1 if accumulate else 0, ws, size, stream)
+    stream, kind = _stream(index), _type(out, "out")
+    call = (index, "ozk_fp8_gemm_scratch", m, n, k, a._at[a_over], b._at[b_over], out.data_ptr(), kind, out.stride(0) if m > 1 else max(n, 1),
+            1 if accumulate else 0, _status(index))
+    status = _code(*call, None, 0, stream)
+    if status == ozk.OZK_ERR_WORKSPACE:
+        # K is split and nothing has been enqueued.  The sums' memory is this call's until both launches are, then the allocator's to
+        # order on the stream: no two threads or streams hold the same, and what a graph captures is the graph's own.
+        plan = ozk.ozk_fp8_plan()
+        _call(index, "ozk_fp8_gemm_plan", m, n, k, a._at[a_over], b._at[b_over], kind, 0, ctypes.byref(plan))
+        scratch = torch.empty(plan.scratch_bytes, dtype=torch.uint8, device=a.codes.device)
+        status = _code(*call, scratch.data_ptr(), plan.scratch_bytes, stream)
+    if status != ozk.OZK_OK:
+        raise ozk.OzkError(status, "ozk_fp8_gemm")
     return out
 
 
