@@ -16,6 +16,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as ozk
 
@@ -257,6 +258,7 @@ class _Linear(torch.autograd.Function):
         return matmul(by_rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
 
     @staticmethod
+    @once_differentiable   # the products below are not seen by autograd: a second derivative raises
     def backward(ctx, dy):
         need_x, need_w = ctx.needs_input_grad[:2]
         by_rows, by_cols = quantize_lines(_rows(dy), need_x, need_w)
@@ -266,7 +268,8 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> torch.Tensor:
-    """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms).
+    """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms; gradients of these
+    gradients raise RuntimeError).
     x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
     the backward pass, which reads it)."""
     return _Linear.apply(x, w, quantize_tiles(_rows(w.detach())) if w8 is None else w8)

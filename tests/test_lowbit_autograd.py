@@ -1,0 +1,51 @@
+"""What `lowbit.linear` tells autograd, on the CPU: exact stand-ins take the places of the kernels."""
+import pytest
+import torch
+
+from paper_2608_06812_b200 import lowbit
+
+
+class Matrix:
+    def __init__(self, x, kind):
+        self.codes, self.scales, self.kind, (self.rows, self.cols), self.index = x, torch.zeros(1), kind, x.shape, 0
+
+
+@pytest.fixture(autouse=True)
+def asked(monkeypatch):
+    """Replaces the kernels; the list of forms that quantize_lines was asked for."""
+    forms = []
+
+    def quantize_lines(x, rows=True, cols=False):
+        forms.append((bool(rows), bool(cols)))
+        return Matrix(x.detach().clone(), "rows") if rows else None, Matrix(x.detach().clone(), "cols") if cols else None
+
+    def matmul(a, b, out=None, over_rows=False, dtype=torch.bfloat16, accumulate=False):
+        A = a.codes.T if a.kind == "cols" else a.codes
+        B = b.codes.T if b.kind == "cols" or over_rows else b.codes
+        return (A @ B.T).to(dtype)
+
+    monkeypatch.setattr(lowbit, "quantize_lines", quantize_lines)
+    monkeypatch.setattr(lowbit, "quantize_tiles", lambda x, out=None: Matrix(x.detach().clone(), "tiles"))
+    monkeypatch.setattr(lowbit, "matmul", matmul)
+    return forms
+
+
+def arguments():
+    g = torch.Generator().manual_seed(0)
+    return torch.randn(5, 6, generator=g, requires_grad=True), torch.randn(4, 6, generator=g, requires_grad=True)
+
+
+def test_first_derivatives():
+    x, w = arguments()
+    dx, dw = torch.autograd.grad(lowbit.linear(x, w).square().sum(), (x, w))
+    y = torch.nn.functional.linear(x, w)
+    ex, ew = torch.autograd.grad(y.square().sum(), (x, w))
+    assert torch.allclose(dx, ex) and torch.allclose(dw, ew)
+
+
+def test_second_derivatives_are_refused():
+    """The gradients are formed in 8 bits outside autograd: a penalty on them would be left out without a word."""
+    x, w = arguments()
+    dx, = torch.autograd.grad(lowbit.linear(x, w).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dx.square().sum().backward()
