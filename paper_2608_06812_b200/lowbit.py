@@ -251,9 +251,9 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, w8):
+    def forward(ctx, x, w, w8, for_dw):
         flat = _rows(x)
-        by_rows, by_cols = quantize_lines(flat, True, ctx.needs_input_grad[1])
+        by_rows, by_cols = quantize_lines(flat, True, for_dw)
         ctx.x8, ctx.w8, ctx.shape, ctx.types = by_cols, w8, x.shape, (x.dtype, w.dtype)
         return matmul(by_rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
 
@@ -264,7 +264,7 @@ class _Linear(torch.autograd.Function):
         by_rows, by_cols = quantize_lines(_rows(dy), need_x, need_w)
         dx = matmul(by_rows, ctx.w8, over_rows=True, dtype=ctx.types[0]).reshape(ctx.shape) if need_x else None
         dw = matmul(by_cols, ctx.x8, dtype=torch.float32).to(ctx.types[1]) if need_w else None
-        return dx, dw, None
+        return dx, dw, None, None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> torch.Tensor:
@@ -272,7 +272,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> tor
     gradients raise RuntimeError).
     x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
     the backward pass, which reads it)."""
-    return _Linear.apply(x, w, quantize_tiles(_rows(w.detach())) if w8 is None else w8)
+    for_dw = w.requires_grad and torch.is_grad_enabled()   # a Function's needs_input_grad is set under no_grad too
+    return _Linear.apply(x, w, quantize_tiles(_rows(w.detach())) if w8 is None else w8, for_dw)
 
 
 class AdamWTable:

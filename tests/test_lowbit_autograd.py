@@ -49,3 +49,17 @@ def test_second_derivatives_are_refused():
     dx, = torch.autograd.grad(lowbit.linear(x, w).square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         dx.square().sum().backward()
+
+
+def test_columns_are_quantised_only_for_a_weight_gradient(asked):
+    """The form of x by columns serves the weight gradient alone."""
+    x, w = arguments()
+    lowbit.linear(x, w)
+    assert asked.pop() == (True, True)
+    for call in (lambda: lowbit.linear(x, w.detach()), lambda: lowbit.linear(x.detach(), w.detach())):
+        call()
+        assert asked.pop() == (True, False)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            lowbit.linear(x, w)
+            assert asked.pop() == (True, False), mode
