@@ -272,8 +272,12 @@ def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> tor
     gradients raise RuntimeError).
     x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
     the backward pass, which reads it)."""
-    for_dw = w.requires_grad and torch.is_grad_enabled()   # a Function's needs_input_grad is set under no_grad too
-    return _Linear.apply(x, w, quantize_tiles(_rows(w.detach())) if w8 is None else w8, for_dw)
+    grads = torch.is_grad_enabled()   # a Function's needs_input_grad is set under no_grad too
+    if w8 is None:
+        w8 = quantize_tiles(_rows(w.detach()))
+    elif (w8.rows, w8.cols) != tuple(w.shape) or w8.scales.dtype != torch.uint8 or not (w8.kind == TILES or (w8.kind == ROWS and not (grads and x.requires_grad))):
+        raise ValueError(f"w8 is a {tuple(w.shape)} Fp8Matrix by {TILES} with UE8M0 scales (or by {ROWS}, where x needs no gradient), not {w8.rows} x {w8.cols} by {w8.kind}")
+    return _Linear.apply(x, w, w8, grads and w.requires_grad)
 
 
 class AdamWTable:

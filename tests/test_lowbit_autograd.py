@@ -63,3 +63,28 @@ def test_columns_are_quantised_only_for_a_weight_gradient(asked):
         with mode():
             lowbit.linear(x, w)
             assert asked.pop() == (True, False), mode
+
+
+def test_kept_weights_that_do_not_fit_are_refused():
+    """Weights by rows serve the forward product only: summed over their rows, dx would be dy w^T of a square weight."""
+    x, w = arguments()
+    square = torch.randn(6, 6, generator=torch.Generator().manual_seed(1), requires_grad=True)
+    tiles, rows, cols = (Matrix(square.detach(), k) for k in ("tiles", "rows", "cols"))
+    floats = Matrix(square.detach(), "tiles")
+    floats.scales = torch.ones(1, 1)
+    for m in (tiles, rows, cols):
+        m.scales = torch.zeros(1, 1, dtype=torch.uint8)
+    for bad in (rows, cols, floats):
+        with pytest.raises(ValueError):
+            lowbit.linear(x, square, bad)
+    for bad in (cols, floats):
+        with torch.no_grad(), pytest.raises(ValueError):
+            lowbit.linear(x, square, bad)
+    with pytest.raises(ValueError):
+        lowbit.linear(x, w, tiles)                     # another weight's
+    want = torch.nn.functional.linear(x, square)
+    assert torch.allclose(lowbit.linear(x, square, tiles), want)
+    with torch.no_grad():
+        assert torch.allclose(lowbit.linear(x, square, rows), want)
+    y = lowbit.linear(x.detach(), square, rows)        # no gradient of x: the weights are summed over their columns only
+    assert torch.allclose(torch.autograd.grad(y.sum(), square)[0], torch.autograd.grad(want.sum(), square)[0])
