@@ -211,6 +211,8 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
       matmul(dy by ROWS, w by TILES, over_rows=True)  dy w
       matmul(dy by COLS, x by COLS)                   dy^T x
     Returns a [lines of a, lines of b] tensor, `out` if given (float32 or bfloat16; float32 with accumulate, which adds)."""
+    if over_rows and b.kind == ROWS:
+        raise ValueError("a matrix by rows cannot be summed over its rows")
     a_over = a.kind == COLS or (a.kind == TILES and b.kind == COLS)
     b_over = b.kind == COLS or (b.kind == TILES and over_rows)
     m, k = (a.cols, a.rows) if a_over else (a.rows, a.cols)
