@@ -37,8 +37,7 @@ def train(steps: int, bits: int, product) -> tuple[list[float], list[torch.Tenso
     """Losses and weights of `steps` steps with `product` for the layers and states of `bits` bits."""
     params = [w.requires_grad_() for w in weights(1)]
     grads = [torch.zeros_like(p) for p in params]
-    flat = [p.detach() for p in params]
-    table = lowbit.AdamWTable.zeros([p.view(-1) for p in flat], [g.view(-1) for g in grads], bits=bits)
+    table = lowbit.AdamWTable.zeros(params, grads, bits=bits)
     losses = []
     for step, (x, want) in enumerate(batches(steps, 2), 1):
         loss = (product(torch.relu(product(x, params[0])), params[1]) - want).square().mean()
@@ -48,7 +47,7 @@ def train(steps: int, bits: int, product) -> tuple[list[float], list[torch.Tenso
         clip = torch.clamp(1.0 / (norm + 1e-6), max=1.0)
         table.step(lr=2e-3, step=step, betas=(0.9, 0.95), weight_decay=0.01, seed=step if bits == 8 else None, grad_scale=clip)
         losses.append(loss.detach())
-    return torch.stack(losses).tolist(), flat
+    return torch.stack(losses).tolist(), [p.detach() for p in params]
 
 
 def answer(tokens: torch.Tensor, layers: list[lowbit.Fp8Matrix]) -> torch.Tensor:

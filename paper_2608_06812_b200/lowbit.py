@@ -28,15 +28,15 @@ def _up(n: int, m: int) -> int:
     return -(-n // m) * m
 
 
-def _stream(index: int) -> int:
-    """The raw handle of the current stream of a device."""
-    return torch._C._cuda_getCurrentRawStream(index)
+# The raw handle of the current stream of a device, and the current device (a torch without CUDA has neither).
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _code(index: int, name: str, *args) -> int:
     """Calls the library with the device current."""
     fn = getattr(ozk.lib(), name)
-    if torch._C._cuda_getDevice() == index:
+    if _device() == index:
         return fn(*args)
     with torch.cuda.device(index):
         return fn(*args)
@@ -59,6 +59,15 @@ def _type(t: torch.Tensor, what: str) -> int:
 def _need_cuda(t: torch.Tensor, what: str) -> None:
     if not t.is_cuda:
         raise ValueError(f"{what} is not on a GPU")
+
+
+# Tells autograd that the library has written to tensors of the caller (a list): a backward pass that saved one of them raises.
+_written = torch._C._increment_version
+
+
+def _versioned(tensors) -> list[torch.Tensor]:
+    """Those that have versions: tensors made in inference mode have none."""
+    return [t for t in tensors if not t.is_inference()]
 
 
 # The status word of the products' bounded waits, one for each device: (address, tensor).
@@ -116,6 +125,7 @@ class Fp8Matrix:
         # views that are asked for at every step
         self._values8 = codes.view(torch.float8_e4m3fn)[:, :cols]
         self._words = None if floats or kind == TILES else scales.transpose(1, 2)
+        self._seen = _versioned((codes, scales))
         # what the quantisers are given, and what a matrix to be written is compared with
         self._target = (codes.data_ptr(), ld, scales.data_ptr())
         self._form = (rows, cols, kind, floats, self.index)
@@ -191,6 +201,10 @@ def quantize_lines(x: torch.Tensor, rows: "bool | Fp8Matrix | None" = True, cols
     to_rows = _NONE if by_rows is None else _output(by_rows, r, c, ROWS, index)
     to_cols = _NONE if by_cols is None else _output(by_cols, r, c, COLS, index)
     _call(index, "ozk_fp8_quantize_lines", r, c, x.data_ptr(), kind, ld, *to_rows, *to_cols, _stream(index))
+    if by_rows is rows and rows:
+        _written(rows._seen)
+    if by_cols is cols and cols:
+        _written(cols._seen)
     return by_rows, by_cols
 
 
@@ -200,6 +214,8 @@ def quantize_tiles(x: torch.Tensor, out: Fp8Matrix | None = None) -> Fp8Matrix:
     index = x.get_device()
     q = Fp8Matrix.empty(r, c, TILES, x.device) if out is None else out
     _call(index, "ozk_fp8_quantize_tiles", r, c, x.data_ptr(), kind, ld, *_output(q, r, c, TILES, index), _stream(index))
+    if out is not None:
+        _written(out._seen)
     return q
 
 
@@ -222,6 +238,7 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
     index = a.index
     if b.index != index:
         raise ValueError("the operands are on two devices")
+    given = out
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -243,6 +260,8 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
         status = _code(*call, scratch.data_ptr(), plan.scratch_bytes, stream)
     if status != ozk.OZK_OK:
         raise ozk.OzkError(status, "ozk_fp8_gemm")
+    if given is not None and not given.is_inference():
+        _written((given,))
     return out
 
 
@@ -287,7 +306,9 @@ class AdamWTable:
 
     params float32 or bfloat16, grads float32 or bfloat16; m, v float32, or uint8 E4M3 codes with m_scale, v_scale (uint8,
     one for each 128 elements; v then holds the ROOT of the second moment); copies: optional bfloat16 copies of float32
-    params, written at every step.  The table holds the tensors' addresses (and keeps the tensors alive): build it once."""
+    params, written at every step.  The table holds the tensors' addresses (and keeps the tensors alive): build it once.
+    Autograd is told of writes to the copies and to params that require gradients; a program that hands in their detached aliases sees to
+    it by itself that no step comes between a forward pass and its backward pass."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
         lists = dict(params=list(params), grads=list(grads), m=list(m), v=list(v))
@@ -316,6 +337,8 @@ class AdamWTable:
             if copies is not None and (first["params"] != torch.float32 or first["copies"] != torch.bfloat16):
                 raise ValueError("copies are bfloat16, of float32 params")
         self.tensors, self.count = lists, count
+        # what autograd may have saved when a step writes to it; 0.05 us a tensor and step
+        self._seen = _versioned([p for p in lists["params"] if p.requires_grad] + (lists["copies"] or []))
         self._table = (ozk.ozk_adamw_tensor * max(count, 1))()
         self._options = ozk.ozk_adamw_options()
         self._table_at, self._options_at = ctypes.addressof(self._table), ctypes.addressof(self._options)
@@ -353,3 +376,5 @@ class AdamWTable:
         o.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
         o.skip = None if skip is None else skip.data_ptr()
         _call(self.device.index, "ozk_adamw_step", self._table_at, self.count, self._options_at, _stream(self.device.index))
+        if self._seen:
+            _written(self._seen)
