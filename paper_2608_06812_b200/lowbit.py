@@ -276,12 +276,15 @@ class _Linear(torch.autograd.Function):
         flat = _rows(x)
         by_rows, by_cols = quantize_lines(flat, True, for_dw)
         ctx.x8, ctx.w8, ctx.shape, ctx.types = by_cols, w8, x.shape, (x.dtype, w.dtype)
+        ctx.versions = [(t, t._version) for t in _versioned((w8.codes, w8.scales))]
         return matmul(by_rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
 
     @staticmethod
     @once_differentiable   # the products below are not seen by autograd: a second derivative raises
     def backward(ctx, dy):
         need_x, need_w = ctx.needs_input_grad[:2]
+        if need_x and any(t._version != v for t, v in ctx.versions):
+            raise RuntimeError("the 8-bit weights needed for the gradient of x have been modified by an inplace operation")
         by_rows, by_cols = quantize_lines(_rows(dy), need_x, need_w)
         dx = matmul(by_rows, ctx.w8, over_rows=True, dtype=ctx.types[0]).reshape(ctx.shape) if need_x else None
         dw = matmul(by_cols, ctx.x8, dtype=torch.float32).to(ctx.types[1]) if need_w else None
@@ -292,7 +295,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> tor
     """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms; gradients of these
     gradients raise RuntimeError).
     x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
-    the backward pass, which reads it)."""
+    the backward pass, which reads it for the gradient of x and raises RuntimeError if it has been written again)."""
     grads = torch.is_grad_enabled()   # a Function's needs_input_grad is set under no_grad too
     if w8 is None:
         w8 = quantize_tiles(_rows(w.detach()))

@@ -88,3 +88,32 @@ def test_kept_weights_that_do_not_fit_are_refused():
         assert torch.allclose(lowbit.linear(x, square, rows), want)
     y = lowbit.linear(x.detach(), square, rows)        # no gradient of x: the weights are summed over their columns only
     assert torch.allclose(torch.autograd.grad(y.sum(), square)[0], torch.autograd.grad(want.sum(), square)[0])
+
+
+def test_kept_weights_written_again_before_the_backward_pass_are_noticed():
+    x, w = arguments()
+    w8 = Matrix(w.detach().clone(), "tiles")
+    w8.scales = torch.zeros(1, 1, dtype=torch.uint8)
+    for part in (w8.codes, w8.scales):
+        y = lowbit.linear(x, w, w8)
+        part.zero_()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    y = lowbit.linear(x.detach(), w, w8)     # the weight gradient does not read them
+    w8.codes.zero_()
+    y.sum().backward()
+    with torch.inference_mode():             # tensors of inference mode have no versions, and serve as before
+        w8 = Matrix(w.detach().clone(), "tiles")
+        w8.scales = torch.zeros(1, 1, dtype=torch.uint8)
+    x.grad = None
+    lowbit.linear(x, w, w8).sum().backward()
+    assert torch.allclose(x.grad, w.detach().sum(0).expand(5, -1))
+
+
+def test_a_graph_may_be_walked_again():
+    x, w = arguments()
+    loss = lowbit.linear(x, w).sum()
+    loss.backward()
+    first = x.grad.clone()
+    loss.backward()
+    assert torch.equal(x.grad, 2 * first)
