@@ -310,6 +310,7 @@ class AdamWTable:
     params float32 or bfloat16, grads float32 or bfloat16; m, v float32, or uint8 E4M3 codes with m_scale, v_scale (uint8,
     one for each 128 elements; v then holds the ROOT of the second moment); copies: optional bfloat16 copies of float32
     params, written at every step.  The table holds the tensors' addresses (and keeps the tensors alive): build it once.
+    Where a gradient is a param's own `.grad`, a step raises RuntimeError once that has been replaced: zero_grad(set_to_none=False) keeps it.
     Autograd is told of writes to the copies and to params that require gradients; a program that hands in their detached aliases sees to
     it by itself that no step comes between a forward pass and its backward pass."""
 
@@ -342,6 +343,8 @@ class AdamWTable:
         self.tensors, self.count = lists, count
         # what autograd may have saved when a step writes to it; 0.05 us a tensor and step
         self._seen = _versioned([p for p in lists["params"] if p.requires_grad] + (lists["copies"] or []))
+        # gradients that autograd owns: it may put others in their place
+        self._owned = [(p, g, g.data_ptr()) for p, g in zip(lists["params"], lists["grads"]) if p.is_leaf and p.grad is not None and p.grad.data_ptr() == g.data_ptr()]
         self._table = (ozk.ozk_adamw_tensor * max(count, 1))()
         self._options = ozk.ozk_adamw_options()
         self._table_at, self._options_at = ctypes.addressof(self._table), ctypes.addressof(self._options)
@@ -373,6 +376,10 @@ class AdamWTable:
         for t, dtype, name in ((grad_scale, torch.float32, "grad_scale"), (skip, torch.int32, "skip")):
             if t is not None and (t.dtype != dtype or t.numel() != 1 or t.device != self.device):
                 raise ValueError(f"{name} is one {dtype} on {self.device}")
+        for p, g, at in self._owned:
+            now = p.grad
+            if now is not g and (now is None or now.data_ptr() != at):
+                raise RuntimeError("the gradient of a param is no longer the tensor that the table was built with: zero gradients in place (set_to_none=False), or build the table again")
         o = self._options
         o.stochastic, o.seed = (0, 0) if seed is None else (1, seed & 0xFFFFFFFF)
         o.lr, (o.beta1, o.beta2), o.eps, o.weight_decay, o.step = lr, betas, eps, weight_decay, step
