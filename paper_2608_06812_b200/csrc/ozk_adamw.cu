@@ -279,7 +279,7 @@ __device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEig
       top_v = max(max(finite_bits(v[0]), finite_bits(v[1])), max(finite_bits(v[2]), finite_bits(v[3])));
       top_m = __reduce_max_sync(0xFFFFFFFFu, top_m), top_v = __reduce_max_sync(0xFFFFFFFFu, top_v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m[i] += m[i] - m[i], r[i] += r[i] - r[i];
+      for (int i = 0; i < 4; ++i) m[i] -= m[i] - m[i], r[i] -= r[i] - r[i];   // subtracted: a negative zero keeps its sign
     }
     const uint32_t code_m = scale_code(top_m), code_r = root_scale_code(top_v);
     const float im = scale_recip(code_m), ir = scale_recip(code_r);

@@ -41,8 +41,8 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t amax_bits) {
 // 2^(c - 127) and its reciprocal; c = 0 is the subnormal 2^-127.
 __device__ __forceinline__ float scale_value(uint32_t c) { return __uint_as_float(max(c << 23, 1u << 22)); }
 __device__ __forceinline__ float scale_recip(uint32_t c) { return __uint_as_float((254u - c) << 23); }   // c <= 247 from scale_code
-// x / scale where x is finite, else NaN: x - x is 0 or NaN.
-__device__ __forceinline__ float scaled(float x, float recip) { return fmaf(x, recip, x - x); }
+// x / scale where x is finite, else NaN: x - x is 0 or NaN.  Subtracted, so that a negative zero keeps its sign.
+__device__ __forceinline__ float scaled(float x, float recip) { return fmaf(x, recip, -(x - x)); }
 
 // Pairs of floats, multiplied in one instruction; each operation rounds both by itself, as the scalar one does.
 struct Pair {
