@@ -413,7 +413,7 @@ typedef struct {
   const int* skip;             /* optional device flag: nonzero leaves everything unchanged (overflow in the gradients) */
 } ozk_adamw_options;
 
-/* One AdamW step over `count` tensors (host array) in one launch per 192 of them, all FP32 arithmetic:
+/* One AdamW step over `count` tensors (host array) in one launch per 448 of them, all FP32 arithmetic:
  *   g' = g grad_scale;  m' = beta1 m + (1 - beta1) g';  v' = beta2 v + (1 - beta2) g'^2;  r = sqrt(v')
  *   p' = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m' / (r / sqrt(1 - beta2^step) + eps)
  * 8-bit states are then rounded to their block's scale as by the quantiser: m' to nearest, r to nearest or, with

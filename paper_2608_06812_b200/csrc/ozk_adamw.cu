@@ -21,9 +21,11 @@ using namespace fp8;
 // is formed (with 8-bit states and FP32 parameters 6 to 8 KiB a warp), which is what keeps enough bytes in flight.
 constexpr int kPieceBlocks = 4;
 constexpr int kPiece = kPieceBlocks * kBlock;
-// Tensors per launch: the table travels in the parameters, which the host copies at every launch.  150 small tensors, time per step
-// of a loop: 8.4 us with room for 192, 10.5 us with 448, 12.6 us with 128 (two launches).
-constexpr int kTableTensors = 192;
+// Tensors per launch: the table travels in the parameters, which the host copies at every launch, and a launch more costs more than that.
+// Up to 192 tensors take the small table, more of them launches of 448 (the most that parameters hold) and a small one for a rest.  A step
+// of n tensors of 5000 in a loop, us, small : large tables only: n = 20 5.5 : 6.7, 150 6.3 : 7.3, 200 11.4 : 7.6, 300 12.6 : 10.2, 448 19.5 : 11.5,
+// 1000 47 : 33.
+constexpr int kFewTensors = 192, kMostTensors = 448;
 
 struct Entry {
   void* param;
@@ -35,7 +37,7 @@ struct Entry {
   __nv_bfloat16* copy;
   int64_t n;        // negative: not all arrays are aligned for vector access, -n elements
 };
-struct Table {
+struct Step {
   int count;
   uint32_t first_tensor;              // index in the caller's array of entry 0: part of the hash
   uint32_t pieces;
@@ -43,10 +45,13 @@ struct Table {
   const int* skip;
   float beta1, one_minus_beta1, beta2, one_minus_beta2, decay, step_size, root_bias, eps;
   uint32_t seed_key;                  // mix(seed)
-  uint32_t first_piece[kTableTensors + 1];
-  Entry entry[kTableTensors];
 };
-static_assert(sizeof(Table) <= 32764, "kernel parameters");
+template <int kTensors>
+struct Table : Step {
+  uint32_t first_piece[kTensors + 1];
+  Entry entry[kTensors];
+};
+static_assert(sizeof(Table<kMostTensors>) <= 32764, "kernel parameters");
 
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x ^= x >> 16;
@@ -232,7 +237,7 @@ struct Block {
 
 // One block; returns the codes of its new scales (m in the low half, v in the high half).
 template <class P, class G, bool kEight, bool kStochastic>
-__device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEight>& l, const Block<P, G, kEight>& x, int b, bool vec, int64_t left, float clip, uint32_t key) {
+__device__ __forceinline__ uint32_t update(const Step& t, const Lane<P, G, kEight>& l, const Block<P, G, kEight>& x, int b, bool vec, int64_t left, float clip, uint32_t key) {
   const Pair clip2 = pair(clip, clip), b1 = pair(t.beta1, t.beta1), c1 = pair(t.one_minus_beta1, t.one_minus_beta1), b2 = pair(t.beta2, t.beta2),
              c2 = pair(t.one_minus_beta2, t.one_minus_beta2);
   float p[4], m[4], v[4], r[4];
@@ -295,8 +300,8 @@ __device__ __forceinline__ uint32_t update(const Table& t, const Lane<P, G, kEig
   }
 }
 
-template <class P, class G, bool kEight, bool kStochastic>
-__global__ void __launch_bounds__(256, !kEight ? 2 : sizeof(P) == 4 ? 3 : 4) adamw_kernel(const __grid_constant__ Table t) {
+template <class P, class G, bool kEight, bool kStochastic, int kTensors>
+__global__ void __launch_bounds__(256, !kEight ? 2 : sizeof(P) == 4 ? 3 : 4) adamw_kernel(const __grid_constant__ Table<kTensors> t) {
   if (t.skip && *t.skip) return;
   const float clip = t.grad_scale ? *t.grad_scale : 1.f;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -340,8 +345,8 @@ __global__ void __launch_bounds__(256, !kEight ? 2 : sizeof(P) == 4 ? 3 : 4) ada
   }
 }
 
-template <class P, class G>
-cudaError_t launch(const Table& t, bool eight, bool stochastic, unsigned blocks, cudaStream_t st) {
+template <class P, class G, int kTensors>
+cudaError_t launch(const Table<kTensors>& t, bool eight, bool stochastic, unsigned blocks, cudaStream_t st) {
   if (eight)
     stochastic ? adamw_kernel<P, G, true, true><<<blocks, 256, 0, st>>>(t) : adamw_kernel<P, G, true, false><<<blocks, 256, 0, st>>>(t);
   else
@@ -350,6 +355,34 @@ cudaError_t launch(const Table& t, bool eight, bool stochastic, unsigned blocks,
 }
 
 bool aligned_to(const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
+
+// One launch over `count` <= kTensors of the caller's tensors, from `first` on.
+template <int kTensors>
+cudaError_t run(const Step& step, const ozk_adamw_tensor* tensors, int64_t first, int count, const ozk_adamw_options* o, cudaStream_t st) {
+  const int ps = o->param_type == OZK_F32 ? 4 : 2, gs = o->grad_type == OZK_F32 ? 4 : 2, ss = o->state_bits == 8 ? 1 : 4;
+  Table<kTensors> t;
+  static_cast<Step&>(t) = step;
+  t.count = count;
+  t.first_tensor = (uint32_t)first;
+  uint32_t pieces = 0;
+  for (int i = 0; i < count; ++i) {
+    const ozk_adamw_tensor& x = tensors[first + i];
+    const bool vec = aligned_to(x.param, 4 * ps) && aligned_to(x.grad, 4 * gs) && aligned_to(x.m, 4 * ss) && aligned_to(x.v, 4 * ss) && aligned_to(x.copy, 8);
+    t.entry[i] = Entry{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, static_cast<__nv_bfloat16*>(x.copy), vec ? x.n : -x.n};
+    t.first_piece[i] = pieces;
+    pieces += (uint32_t)ceil_div(x.n, kPiece);
+  }
+  t.first_piece[count] = pieces;
+  t.pieces = pieces;
+  if (pieces == 0) return cudaSuccess;
+  // a warp for every piece; from 32 thread blocks per multiprocessor on (eight to sixteen times what runs at a time) each takes several
+  const int64_t most = (int64_t)device_sm_count() * 32, wanted = ceil_div(pieces, 8);
+  const unsigned blocks = (unsigned)(wanted < most ? wanted : most);
+  const bool eight = o->state_bits == 8, stochastic = o->stochastic && (eight || o->param_type == OZK_BF16);
+  if (o->param_type == OZK_F32)
+    return o->grad_type == OZK_F32 ? launch<float, float>(t, eight, stochastic, blocks, st) : launch<float, __nv_bfloat16>(t, eight, stochastic, blocks, st);
+  return o->grad_type == OZK_F32 ? launch<__nv_bfloat16, float>(t, eight, stochastic, blocks, st) : launch<__nv_bfloat16, __nv_bfloat16>(t, eight, stochastic, blocks, st);
+}
 
 }  // namespace
 }  // namespace ozk
@@ -373,11 +406,11 @@ extern "C" ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t co
       return OZK_ERR_INVALID_ARG;
     if (o->state_bits == 8 && (!x.m_scale || !x.v_scale)) return OZK_ERR_INVALID_ARG;
     if (x.copy && (o->param_type != OZK_F32 || !aligned_to(x.copy, 2))) return OZK_ERR_INVALID_ARG;
-    if (ceil_div(x.n, kPiece) > INT32_MAX / kTableTensors) return OZK_ERR_UNSUPPORTED;   // the pieces of a launch are counted in 31 bits
+    if (ceil_div(x.n, kPiece) > INT32_MAX) return OZK_ERR_UNSUPPORTED;   // the pieces of a launch are counted in 31 bits
   }
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  Table t;
+  Step t;
   t.grad_scale = o->grad_scale;
   t.skip = o->skip;
   t.beta1 = (float)o->beta1, t.one_minus_beta1 = (float)(1.0 - o->beta1);
@@ -387,31 +420,15 @@ extern "C" ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t co
   t.root_bias = (float)(1.0 / sqrt(1.0 - pow(o->beta2, (double)o->step)));
   t.eps = (float)o->eps;
   t.seed_key = mix(o->seed);
-  for (int64_t first = 0; first < count; first += kTableTensors) {
-    t.count = (int)(count - first < kTableTensors ? count - first : kTableTensors);
-    t.first_tensor = (uint32_t)first;
-    uint32_t pieces = 0;
-    for (int i = 0; i < t.count; ++i) {
-      const ozk_adamw_tensor& x = tensors[first + i];
-      const bool vec = aligned_to(x.param, 4 * ps) && aligned_to(x.grad, 4 * gs) && aligned_to(x.m, 4 * ss) && aligned_to(x.v, 4 * ss) && aligned_to(x.copy, 8);
-      t.entry[i] = Entry{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, static_cast<__nv_bfloat16*>(x.copy), vec ? x.n : -x.n};
-      t.first_piece[i] = pieces;
-      pieces += (uint32_t)ceil_div(x.n, kPiece);
+  for (int64_t first = 0; first < count;) {
+    int here = 0;
+    for (int64_t pieces = 0; here < kMostTensors && first + here < count; ++here) {
+      pieces += ceil_div(tensors[first + here].n, kPiece);
+      if (pieces > INT32_MAX) break;
     }
-    t.first_piece[t.count] = pieces;
-    t.pieces = pieces;
-    if (pieces == 0) continue;
-    // a warp for every piece; from 32 thread blocks per multiprocessor on (eight times what runs at a time) each takes several
-    const int64_t most = (int64_t)device_sm_count() * 32, wanted = ceil_div(pieces, 8);
-    const unsigned blocks = (unsigned)(wanted < most ? wanted : most);
-    const bool eight = o->state_bits == 8, stochastic = o->stochastic && (eight || o->param_type == OZK_BF16);
-    cudaError_t e;
-    if (o->param_type == OZK_F32)
-      e = o->grad_type == OZK_F32 ? launch<float, float>(t, eight, stochastic, blocks, st) : launch<float, __nv_bfloat16>(t, eight, stochastic, blocks, st);
-    else
-      e = o->grad_type == OZK_F32 ? launch<__nv_bfloat16, float>(t, eight, stochastic, blocks, st)
-                                  : launch<__nv_bfloat16, __nv_bfloat16>(t, eight, stochastic, blocks, st);
+    const cudaError_t e = here <= kFewTensors ? run<kFewTensors>(t, tensors, first, here, o, st) : run<kMostTensors>(t, tensors, first, here, o, st);
     if (e != cudaSuccess) return OZK_ERR_CUDA;
+    first += here;
   }
   return OZK_OK;
 }
