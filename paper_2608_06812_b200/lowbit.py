@@ -266,7 +266,7 @@ def matmul(a: Fp8Matrix, b: Fp8Matrix, out: torch.Tensor | None = None, over_row
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
-    flat = x.reshape(-1, x.shape[-1])
+    flat = x.reshape(x.shape[:-1].numel(), x.shape[-1])
     return flat if flat.stride(1) == 1 and flat.stride(0) >= flat.shape[1] else flat.contiguous()   # an expanded gradient has strides of 0
 
 
