@@ -349,7 +349,9 @@ typedef struct {
 /* C[m,n] = sum_k A(m,k) B(n,k) on the scaled values, FP32 accumulation, C row-major M x N (OZK_F32 or OZK_BF16,
  * ldc >= N), rounded once; accumulate = 1 (OZK_F32 only) adds the product to C instead.
  *   UE8M0 scales (LINES or TILES on either operand): the tensor cores apply them.  Float scales: A is
- *   LINES_F32 and B TILES_F32, both contract_rows = 0.  Other combinations return OZK_ERR_UNSUPPORTED.
+ *   LINES_F32 and B TILES_F32, both contract_rows = 0.  Other combinations return OZK_ERR_UNSUPPORTED.  A float scale of A times
+ *   one of B is formed in FP32 before it meets a block's sum: the two should stay within 2^-126 .. 2^127 together.  (The quantiser writes
+ *   UE8M0 scales; float scales are for operands that come with them.)
  *   A forward product y = x w^T has A = x (LINES), B = w (TILES); its input gradient dy w has A = dy (LINES), B = w
  *   with contract_rows = 1; its weight gradient dy^T x has A = dy, B = x, both LINES with contract_rows = 1.
  *   FP32 results: sums over more than 8192 are formed in ranges of at most 8192 that are added in FP32 in order,
@@ -420,7 +422,7 @@ typedef struct {
  * `stochastic`, up or down (a root that changes by less than half a unit per step would never change otherwise);
  * a root that is not zero is stored as at least 2^-9 of its scale, so that m / (r + eps) stays bounded.  The hash is
  * mix(i mod 2^32 ^ mix(index of the tensor + 1) ^ mix(seed)), mix(x): x ^= x>>16, x *= 0x7feb352d, x ^= x>>15, x *= 0x846ca68b,
- * x ^= x>>16; the root uses its upper 16 bits, a BF16 parameter the lower 16.
+ * x ^= x>>16 (Chris Wellons' lowbias32, 2018); the root uses its upper 16 bits, a BF16 parameter the lower 16.
  * Second moments below 2^-126 have the root zero.  Non-finite gradients give non-finite (8-bit: NaN) values in their own
  * element only.  No tensor may overlap another. */
 ozk_status ozk_adamw_step(const ozk_adamw_tensor* tensors, int64_t count, const ozk_adamw_options* options, void* stream);

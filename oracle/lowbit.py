@@ -63,7 +63,7 @@ def spread(s: np.ndarray, shape: tuple[int, int], kind: str) -> np.ndarray:
 
 
 def mix(x: np.ndarray) -> np.ndarray:
-    """The hash of the stochastic rounding, on uint32."""
+    """The hash of the stochastic rounding, on uint32: Chris Wellons' lowbias32 ("Prospecting for Hash Functions", 2018)."""
     x = np.asarray(x, np.uint64) & 0xFFFFFFFF
     x ^= x >> np.uint64(16)
     x = (x * np.uint64(0x7FEB352D)) & np.uint64(0xFFFFFFFF)

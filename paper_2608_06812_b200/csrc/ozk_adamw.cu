@@ -18,7 +18,7 @@ namespace {
 using namespace fp8;
 
 // A piece is what one warp works on at a time: four blocks of 128 elements.  All its loads are issued before the first result
-// is formed (with 8-bit states and FP32 parameters 6 to 8 KiB a warp), which is what keeps enough bytes in flight.
+// is formed (with 8-bit states and FP32 parameters 4 to 5 KiB a warp), which is what keeps enough bytes in flight.
 constexpr int kPieceBlocks = 4;
 constexpr int kPiece = kPieceBlocks * kBlock;
 // Tensors per launch: the table travels in the parameters, which the host copies at every launch, and a launch more costs more than that.
@@ -53,6 +53,7 @@ struct Table : Step {
 };
 static_assert(sizeof(Table<kMostTensors>) <= 32764, "kernel parameters");
 
+// A published hash of 32 bits (Chris Wellons, "Prospecting for Hash Functions", 2018: lowbias32).
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x ^= x >> 16;
   x *= 0x7feb352du;

@@ -383,7 +383,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if constexpr (kFloat) set_registers_more<S::kEpilogueRegs>();
     // ------------------------------ epilogue (both CTAs) ----------------------------------
     const uint32_t quad = (uint32_t)(warp & 3);
-    const int part = (warp - S::kFirstEpilogue) >> 2;   // which kWarpCols of the columns
+    const int part = (warp - S::kFirstEpilogue) >> 2;   // which 128 of the columns
     uint8_t* box = staging + (warp - S::kFirstEpilogue) * 4096;
     const uint32_t lanes = tmem + ((quad * 32u) << 16);
     const uint32_t empty0 = map_to_cta(smem_u32(&sh->acc_empty[0]), 0), overlap = map_to_cta(smem_u32(&sh->overlap), 0);
@@ -982,7 +982,8 @@ ozk_status run_pair(ProductParams p, const Plan& plan, int64_t K, bool floats, b
   if (!ok) return OZK_ERR_CUDA;
   if (splits > 1) {
     const int64_t blocks = ceil_div((int64_t)c.M * c.N, 256);
-    const unsigned g = (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16);
+    const int64_t most = (int64_t)device_sm_count() * 16;
+    const unsigned g = (unsigned)(blocks < most ? blocks : most);
     const float* part = static_cast<const float*>(p.out.ptr);
     if (bf16)
       join_kernel<true><<<g, 256, 0, st>>>(part, splits, c.M, c.N, p.out.ld, c.ptr, c.ld, 0);
