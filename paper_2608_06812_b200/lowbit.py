@@ -344,7 +344,7 @@ class AdamWTable:
         # what autograd may have saved when a step writes to it; 0.05 us a tensor and step
         self._seen = _versioned([p for p in lists["params"] if p.requires_grad] + (lists["copies"] or []))
         # gradients that autograd owns: it may put others in their place
-        self._owned = [(p, g, g.data_ptr()) for p, g in zip(lists["params"], lists["grads"]) if p.is_leaf and p.grad is not None and p.grad.data_ptr() == g.data_ptr()]
+        self._owned = [(p, g, g.data_ptr()) for p, g in zip(lists["params"], lists["grads"]) if p.numel() and p.is_leaf and p.grad is not None and p.grad.data_ptr() == g.data_ptr()]
         self._table = (ozk.ozk_adamw_tensor * max(count, 1))()
         self._options = ozk.ozk_adamw_options()
         self._table_at, self._options_at = ctypes.addressof(self._table), ctypes.addressof(self._options)

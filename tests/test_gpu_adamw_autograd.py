@@ -70,3 +70,12 @@ def test_gradients_of_the_callers_own_are_not_watched():
     view[0].grad = None
     with pytest.raises(RuntimeError, match="gradient"):
         table.step(lr=1e-2, step=2)
+
+
+def test_params_without_elements_are_not_watched():
+    p, q = torch.nn.Parameter(torch.zeros(0, device="cuda")), torch.nn.Parameter(torch.zeros(5, device="cuda"))
+    p.grad = torch.zeros(0, device="cuda")
+    table = lowbit.AdamWTable.zeros([p, q], [torch.zeros(0, device="cuda"), torch.ones(5, device="cuda")])
+    p.grad = None
+    table.step(lr=1e-2, step=1)
+    assert (q != 0).all()
