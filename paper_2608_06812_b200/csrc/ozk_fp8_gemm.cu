@@ -89,7 +89,7 @@ struct Output {
   int64_t ld;
   int M, N;
   int add;   // add to what is there (FP32)
-  int tma;   // 16-byte aligned rows: whole boxes by TMA
+  int tma;   // 16-byte aligned rows: boxes by TMA
 };
 
 struct ProductParams {
@@ -163,14 +163,17 @@ template <bool kBf16>
 __device__ __forceinline__ void store_box(const Output& o, const CUtensorMap* map, uint8_t* staging, int lane, const uint32_t (&w)[32], int m, int n, int z,
                                           bool add) {
   if (m >= o.M || n >= o.N) return;   // the same for all lanes
-  if (o.tma) {
+  // A tiled store writes whole 16-byte pieces, also past the map's last column: a box across an edge within such a piece is stored singly.
+  constexpr int kWidth = kBf16 ? 64 : 32, kPiece = kBf16 ? 8 : 4;
+  const bool tma = o.tma && (n + kWidth <= o.N || o.N % kPiece == 0);
+  if (o.tma) {   // an earlier box may still be read from the staging
     if (lane == 0) bulk_wait_read();
     __syncwarp();
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     *reinterpret_cast<uint4*>(staging + lane * 128 + ((j ^ (lane & 7)) * 16)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-  if (o.tma) {
+  if (tma) {
     fence_proxy_async();
     __syncwarp();
     if (lane == 0) {
@@ -966,7 +969,10 @@ ozk_status run_pair(ProductParams p, const Plan& plan, int64_t K, bool floats, b
   p.splits = splits;
   const bool out_bf16 = bf16 && splits == 1;
   p.chunk_groups = out_bf16 || floats ? p.groups : kRangeGroups;
-  if (splits > 1) p.out = Output{scratch, round_up(c.N, 4), c.M, c.N, 0, 1};
+  if (splits > 1) {   // rows of whole 16-byte pieces, the last one's zeros included
+    const int ld = (int)round_up(c.N, 4);
+    p.out = Output{scratch, ld, c.M, ld, 0, 1};
+  }
   CUtensorMap map_a, map_b, map_c;
   if (!operand_map(&map_a, p.a, K, 128) || !operand_map(&map_b, p.b, K, kTileN / 2)) return OZK_ERR_CUDA;
   if (p.out.tma) {
