@@ -356,7 +356,7 @@ typedef struct {
  *   with contract_rows = 1; its weight gradient dy^T x has A = dy, B = x, both LINES with contract_rows = 1.
  *   FP32 results: sums over more than 8192 are formed in ranges of at most 8192 that are added in FP32 in order,
  *   because the tensor cores truncate when they accumulate.  Results do not depend on timing.
- *   M, N, K = 0 are allowed (K = 0: C = 0, or unchanged with accumulate).  M, N, K < 2^31.
+ *   M, N, K = 0 are allowed (K = 0: C = 0, or unchanged with accumulate).  M, N, K < 2^31.  What lies between the rows of C is not touched.
  * workspace: device memory of ozk_fp8_gemm_workspace_bytes() (one size for all shapes), 256-byte aligned, whose first
  * kibibyte has been cleared once (cudaMemset); NULL takes the registered one.  A call may be several launches that pass sums
  * through it: calls that share one must be made one after the other on one stream (by one host thread at a time), and a graph that
