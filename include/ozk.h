@@ -389,6 +389,72 @@ ozk_status ozk_fp8_gemm_plan(int64_t M, int64_t N, int64_t K, const ozk_fp8_oper
 /* ozk_get_async_status() for a workspace that was passed to a call rather than registered. */
 ozk_status ozk_get_workspace_status(void* workspace, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Around the 8-bit products: the norm that writes their operands, and products grouped by expert.
+ * ------------------------------------------------------------------------------------- */
+
+/* RMS norm of X (rows x cols, x_type) with the residual stream R (r_type: x_type or OZK_F32) added first:
+ *   h = x + r, rounded to r_type and written to H (the updated stream);  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
+ * R NULL: h = x, and H is not used.  H may be R (same ld), or X where the types agree: the stream is updated in place.
+ * The norm is of h as it is stored.  weight: cols numbers of w_type.  FP32 arithmetic, sums in an order that depends on cols alone.
+ *   root       optional, rows floats: s, which the backward pass reads (wanted where col_codes are)
+ *   Y          optional, rows x cols of x_type: y without quantisation
+ *   row_codes, row_scales / col_codes, col_scales   optional: y by 1 x 128 / 128 x 1 blocks, as by ozk_fp8_quantize_lines
+ * Mean squares beyond FP32 count as infinite (s = 0).  A NaN or an infinity in a row makes NaN of the row's y (0 of what is finite beside an infinity).
+ * cols <= 32768.  rows, cols = 0 are allowed. */
+ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, const void* R, int r_type, int64_t ldr,
+                        void* H, int64_t ldh, const void* weight, int w_type, double eps, float* root, void* Y, int64_t ldy,
+                        uint8_t* row_codes, int64_t row_ld, uint8_t* row_scales, uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales,
+                        void* stream);
+
+/* Its gradients.  dY (dy_type): gradient of y; H (h_type), root: what the forward pass normed and its s; dH: optional gradient of h from
+ * elsewhere (h_type).
+ *   g = dy w;  dX = dh + s (g - h s mean(g h s)), in h_type, the gradient of x and of r alike;  dweight = sum over the rows of dy h s (FP32, optional)
+ * dX may be dH.  scratch: ozk_rms_norm_backward_scratch_bytes(), 16-byte aligned, for this call alone; not needed without dweight. */
+size_t ozk_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols);
+ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int dy_type, int64_t lddy, const void* H, int h_type, int64_t ldh,
+                                 const float* root, const void* weight, int w_type, const void* dH, int64_t lddh, void* dX, int64_t lddx,
+                                 float* dweight, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Segments: rows lie in the order of the experts they belong to; expert e has rows offsets[e] .. offsets[e+1] - 1 (offsets: experts + 1 numbers in
+ * device memory, ascending from offsets[0] >= 0 to offsets[experts] <= rows).  Segments may be empty; rows before the first and behind the last
+ * belong to nobody.  Offsets that fall or leave the rows are read as the nearest that do not.  experts <= 1024 in products. */
+
+/* The operand of a product that sums over the rows of each expert: blocks of 128 rows that begin with each segment.  Block b of the segments has
+ * rows 128 b .. 128 b + 127 of col_codes, with zeros behind the end of a segment, and scales as LINES (lines = cols, k = 128 x
+ * ozk_fp8_segment_blocks()); blocks that no segment takes are left as they were.  row_codes, row_scales: optional, the rows of the segments
+ * as by ozk_fp8_quantize_lines; other rows are left as they were. */
+int64_t ozk_fp8_segment_blocks(int64_t rows, int64_t experts);   /* floor((rows + 127 min(experts, rows)) / 128): enough for any offsets */
+ozk_status ozk_fp8_quantize_segments(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, const int32_t* offsets, int64_t segments,
+                                     uint8_t* row_codes, int64_t row_ld, uint8_t* row_scales,
+                                     uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales, void* stream);
+
+/* ozk_fp8_quantize_tiles of `experts` matrices x_step elements apart; their codes lie `step` bytes apart (a multiple of 16), their
+ * scales one after another. */
+ozk_status ozk_fp8_quantize_experts(int64_t experts, int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, int64_t x_step,
+                                    uint8_t* codes, int64_t ld, int64_t step, uint8_t* scales, void* stream);
+
+/* The experts' weights, as ozk_fp8_quantize_experts writes them.  contract_rows as in ozk_fp8_operand. */
+typedef struct {
+  const uint8_t* codes;
+  int64_t ld, stride;     /* from row to row, from expert to expert */
+  const uint8_t* scales;
+  int contract_rows;
+} ozk_fp8_experts;
+
+/* C[t,n] = sum_k X(t,k) W_e(n,k) for the rows t of each expert e (X: rows x K, LINES, contract_rows = 0; C: rows x N), as ozk_fp8_gemm with that
+ * expert's weights; input gradients have W's contract_rows = 1.  Rows of C outside the segments are left as they were, or cleared with
+ * clear_rest = 1.  status: as for ozk_fp8_gemm_scratch.  No other memory is used. */
+ozk_status ozk_fp8_grouped_gemm(int64_t rows, int64_t N, int64_t K, const ozk_fp8_operand* X, const ozk_fp8_experts* W, int64_t experts,
+                                const int32_t* offsets, void* C, int c_type, int64_t ldc, int clear_rest, void* status, void* stream);
+
+/* C_e[m,n] = sum over the rows t of expert e of A(t,m) B(t,n), for every expert (weight gradients): C is [experts][M][N], `stride` elements
+ * from expert to expert.  A, B: by ozk_fp8_quantize_segments with the same offsets (contract_rows = 1, LINES).  An expert without rows gets
+ * zeros, or with accumulate (OZK_F32 only, adds to C) keeps what it has. */
+ozk_status ozk_fp8_segment_gemm(int64_t experts, int64_t M, int64_t N, int64_t rows, const ozk_fp8_operand* A, const ozk_fp8_operand* B,
+                                const int32_t* offsets, void* C, int c_type, int64_t ldc, int64_t stride, int accumulate, void* status,
+                                void* stream);
+
 /* One tensor of an AdamW step: n elements, contiguous.  Element i of the optimiser's block b has i / 128 = b.
  *   32-bit states: m, v are floats.  8-bit states: m holds E4M3 codes of the first moment and v E4M3 codes of the
  *   ROOT r = sqrt(v) of the second (its 17.8 binades below a block's largest entry are 35 of v), m_scale and v_scale one

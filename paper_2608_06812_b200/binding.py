@@ -37,6 +37,10 @@ class ozk_fp8_plan(ctypes.Structure):
     _fields_ = [("pairs", c_int), ("tile_rows", c_int), ("tile_cols", c_int), ("splits", c_int), ("tiles", c_int64), ("scratch_bytes", c_size_t)]
 
 
+class ozk_fp8_experts(ctypes.Structure):
+    _fields_ = [("codes", c_void_p), ("ld", c_int64), ("stride", c_int64), ("scales", c_void_p), ("contract_rows", c_int)]
+
+
 class ozk_adamw_tensor(ctypes.Structure):
     _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
                 ("copy", c_void_p), ("n", c_int64)]
@@ -87,6 +91,16 @@ SIGNATURES = {
     "ozk_fp8_gemm": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
     "ozk_fp8_gemm_scratch": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ozk_fp8_gemm_plan": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int, c_void_p]),
+    "ozk_rms_norm": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int, c_double, c_void_p, c_void_p, c_int64,
+                             c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "ozk_rms_norm_backward_scratch_bytes": (c_size_t, [c_int64, c_int64]),
+    "ozk_rms_norm_backward": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_void_p, c_void_p, c_int, c_void_p, c_int64, c_void_p, c_int64,
+                                      c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ozk_fp8_segment_blocks": (c_int64, [c_int64, c_int64]),
+    "ozk_fp8_quantize_segments": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "ozk_fp8_quantize_experts": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_int, c_int64, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_void_p]),
+    "ozk_fp8_grouped_gemm": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p]),
+    "ozk_fp8_segment_gemm": (c_int, [c_int64, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_int, c_void_p, c_void_p]),
     "ozk_adamw_step": (c_int, [c_void_p, c_int64, c_void_p, c_void_p]),
     "ozk_stage_mma_probe": (c_int, [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p]),
 }
@@ -283,6 +297,42 @@ def ozk_fp8_gemm_plan(M, N, K, A, B, c_type, sms=0) -> ozk_fp8_plan:
     plan = ozk_fp8_plan()
     check(lib().ozk_fp8_gemm_plan(M, N, K, ctypes.byref(A), ctypes.byref(B), c_type, sms, ctypes.byref(plan)), "ozk_fp8_gemm_plan")
     return plan
+
+
+def ozk_rms_norm(rows, cols, X, x_type, ldx, R, r_type, ldr, H, ldh, weight, w_type, eps, root=None, Y=None, ldy=0,
+                 row_codes=None, row_ld=0, row_scales=None, col_codes=None, col_ld=0, col_scales=None, stream=0) -> int:
+    return lib().ozk_rms_norm(rows, cols, X, x_type, ldx, R, r_type, ldr, H, ldh, weight, w_type, eps, root, Y, ldy,
+                              row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream)
+
+
+def ozk_rms_norm_backward_scratch_bytes(rows: int, cols: int) -> int:
+    return lib().ozk_rms_norm_backward_scratch_bytes(rows, cols)
+
+
+def ozk_rms_norm_backward(rows, cols, dY, dy_type, lddy, H, h_type, ldh, root, weight, w_type, dH, lddh, dX, lddx, dweight=None, scratch=None, scratch_bytes=0, stream=0) -> int:
+    return lib().ozk_rms_norm_backward(rows, cols, dY, dy_type, lddy, H, h_type, ldh, root, weight, w_type, dH, lddh, dX, lddx, dweight, scratch, scratch_bytes, stream)
+
+
+def ozk_fp8_segment_blocks(rows: int, experts: int) -> int:
+    return lib().ozk_fp8_segment_blocks(rows, experts)
+
+
+def ozk_fp8_quantize_segments(rows, cols, X, x_type, ldx, offsets, segments, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream=0) -> int:
+    return lib().ozk_fp8_quantize_segments(rows, cols, X, x_type, ldx, offsets, segments, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream)
+
+
+def ozk_fp8_quantize_experts(experts, rows, cols, X, x_type, ldx, x_step, codes, ld, step, scales, stream=0) -> int:
+    return lib().ozk_fp8_quantize_experts(experts, rows, cols, X, x_type, ldx, x_step, codes, ld, step, scales, stream)
+
+
+def ozk_fp8_grouped_gemm(rows, N, K, X, W, experts, offsets, C, c_type, ldc, clear_rest, status, stream=0) -> int:
+    """X: an ozk_fp8_operand; W: an ozk_fp8_experts."""
+    return lib().ozk_fp8_grouped_gemm(rows, N, K, ctypes.byref(X), ctypes.byref(W), experts, offsets, C, c_type, ldc, clear_rest, status, stream)
+
+
+def ozk_fp8_segment_gemm(experts, M, N, rows, A, B, offsets, C, c_type, ldc, stride, accumulate, status, stream=0) -> int:
+    """A, B: ozk_fp8_operand structures."""
+    return lib().ozk_fp8_segment_gemm(experts, M, N, rows, ctypes.byref(A), ctypes.byref(B), offsets, C, c_type, ldc, stride, accumulate, status, stream)
 
 
 def ozk_adamw_step(tensors, count, options, stream=0) -> int:

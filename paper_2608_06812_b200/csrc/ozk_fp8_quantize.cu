@@ -129,9 +129,47 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* X, int64_t 
   }
 }
 
-template <class T, bool kVec, bool kRows, bool kCols, bool kTiles>
+// Ranges of rows whose blocks of 128 begin with each of them: tile row tr is a block of the segments, and the codes by columns lie
+// block after block, with zeros behind the rows of a segment's last one.
+struct Segments {
+  const int* offsets;
+  int count;
+};
+// First row of block `index`, and how many rows of its segment are left from there (0: there is no such block).  Offsets are held within the rows and
+// never fall.  By one warp.
+__device__ __forceinline__ int2 segment_block(const Segments& s, int rows, int index, int lane) {
+  int carry = 0, top = min(max(__ldg(s.offsets), 0), rows);
+  for (int e0 = 0; e0 < s.count; e0 += 32) {
+    int f = e0 + lane < s.count ? min(max(__ldg(s.offsets + e0 + lane + 1), top), rows) : top;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, f, d);
+      if (lane >= d) f = max(f, v);
+    }
+    int b = __shfl_up_sync(0xFFFFFFFFu, f, 1);
+    if (lane == 0) b = top;
+    const int blocks = (f - b + kBlock - 1) / kBlock;
+    int sum = blocks;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      if (lane >= d) sum += v;
+    }
+    const uint32_t beyond = __ballot_sync(0xFFFFFFFFu, index < carry + sum);
+    if (beyond) {
+      const int first = b + (index - carry - sum + blocks) * kBlock, l = __ffs(beyond) - 1;
+      return make_int2(__shfl_sync(0xFFFFFFFFu, first, l), __shfl_sync(0xFFFFFFFFu, f - first, l));
+    }
+    carry += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    top = __shfl_sync(0xFFFFFFFFu, f, 31);
+  }
+  return make_int2(0, 0);
+}
+
+// kTiles: blockIdx.y is one of several matrices, x_step and q_step apart.
+template <class T, bool kVec, bool kRows, bool kCols, bool kTiles, bool kSegments = false>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_kernel(const T* X, int64_t ldx, int rows, int cols, uint8_t* Qr, int64_t ldr, uint8_t* Sr,
-                                                            uint8_t* Qc, int64_t ldc, uint8_t* Sc) {
+                                                            uint8_t* Qc, int64_t ldc, uint8_t* Sc, Segments segments = {}, int64_t x_step = 0, int64_t q_step = 0) {
   using W = Words<T>;
   constexpr int kPiece = W::kPiece, kPieces = W::kPieces, kWords = W::kWords, kRowWords = kPieces * kWords;   // words per thread and row
   constexpr int kTileWords = kRowWords * 8;
@@ -141,14 +179,26 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c = lane % 8;
   const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
   const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
-  const int r0 = tr * kBlock + threadIdx.x / 8, c0 = tc * kBlock + c * kPiece;
+  int first = tr * kBlock, live = rows - first;   // the tile's first row of X, and the rows from there on
+  if constexpr (kSegments) {
+    __shared__ int2 block;
+    if (warp == 0) {
+      const int2 found = segment_block(segments, rows, tr, lane);
+      if (lane == 0) block = found;
+    }
+    __syncthreads();
+    first = block.x, live = block.y;
+    if (live == 0) return;
+  }
+  if constexpr (kTiles) X += blockIdx.y * x_step, Qc += blockIdx.y * q_step, Sc += blockIdx.y * (int64_t)tiles_r * tiles_c;
+  const int r_in = threadIdx.x / 8, r0 = first + r_in, c0 = tc * kBlock + c * kPiece;
   uint32_t x[4][kRowWords];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       const int col = c0 + q * 8 * kPiece;
-      load_piece<T, kVec>(X + (int64_t)(r0 + 32 * i) * ldx + col, r0 + 32 * i < rows ? cols - col : 0, &x[i][q * kWords]);
+      load_piece<T, kVec>(X + (int64_t)(r0 + 32 * i) * ldx + col, r_in + 32 * i < live ? cols - col : 0, &x[i][q * kWords]);
     }
   // largest magnitudes of this thread's rows and columns
   uint32_t row_top[4], col_top[kRowWords];
@@ -188,15 +238,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
     if (lane == 0) tile_top[warp] = t;
   }
   // the four rows' pieces, by reciprocals that belong to the row or to the columns
-  auto store = [&](uint8_t* Q, int64_t ld, auto recip_of, int step) {
-    uint8_t* at = Q + (int64_t)r0 * ld + c0;
+  auto store = [&](uint8_t* Q, int64_t ld, int row, int most, auto recip_of, int step) {   // the first `most` rows of the tile from `row` on
+    uint8_t* at = Q + (int64_t)(row + r_in) * ld + c0;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
       const int col = q * 8 * kPiece;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const Pair* recip = recip_of(q, i);
-        if (r0 + 32 * i < rows && c0 + col < cols)
+        if (r_in + 32 * i < most && c0 + col < cols)
           store_piece<T>(at + (int64_t)(32 * i) * ld + col, cols - c0 - col, &x[i][q * kWords], recip, step, bad);
       }
     }
@@ -212,12 +262,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
       recip[i] = pair(scale_recip(code), scale_recip(code));
       if (c == 0) row_code[threadIdx.x / 8 + 32 * i] = code;
     }
-    store(Qr, ldr, [&](int, int i) { return &recip[i]; }, 0);
+    store(Qr, ldr, first, live, [&](int, int i) { return &recip[i]; }, 0);
   }
   __syncthreads();
   if constexpr (kRows) {   // a warp's 32 scale bytes in one request
-    const int i = (int)threadIdx.x - kBlock, r = tr * kBlock + i;
-    if (i >= 0 && r < rows) {
+    const int i = (int)threadIdx.x - kBlock, r = first + i;
+    if (i >= 0 && i < live) {
       uint8_t* s = Sr + ((int64_t)(tc / 4) * rows + r) * 4;
       s[tc % 4] = (uint8_t)row_code[i];
       if (tc + 1 == tiles_c)
@@ -247,7 +297,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
           if (tc * kBlock + col < cols) {
             uint8_t* s = Sc + ((int64_t)(tr / 4) * cols + tc * kBlock + col) * 4;
             s[tr % 4] = (uint8_t)code;
-            if (tr + 1 == tiles_r)
+            if (!kSegments && tr + 1 == tiles_r)
               for (int b = tr % 4 + 1; b < 4; ++b) s[b] = 127;
           }
         }
@@ -266,7 +316,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) quantize_tile_ker
           recip[q * kPiece / 2 + k] = pair(f.x, f.y);
         }
     }
-    store(Qc, ldc, [&](int q, int) { return &recip[kTiles ? 0 : q * kPiece / 2]; }, kTiles ? 0 : 1);
+    store(Qc, ldc, kSegments ? tr * kBlock : first, kSegments ? kBlock : live, [&](int q, int) { return &recip[kTiles ? 0 : q * kPiece / 2]; }, kTiles ? 0 : 1);
   }
 }
 
@@ -308,9 +358,17 @@ cudaError_t launch_lines(int rows, int cols, const T* X, int64_t ldx, uint8_t* Q
   return cudaGetLastError();
 }
 template <class T, bool kVec>
-cudaError_t launch_tiles(int rows, int cols, const T* X, int64_t ldx, uint8_t* Q, int64_t ld, uint8_t* S, cudaStream_t st) {
-  const int64_t tiles = ceil_div(rows, kBlock) * ceil_div(cols, kBlock);
-  quantize_tile_kernel<T, kVec, false, false, true><<<(unsigned)tiles, 256, 0, st>>>(X, ldx, rows, cols, nullptr, 0, nullptr, Q, ld, S);
+cudaError_t launch_tiles(int count, int rows, int cols, const T* X, int64_t ldx, int64_t x_step, uint8_t* Q, int64_t ld, int64_t q_step, uint8_t* S, cudaStream_t st) {
+  const dim3 grid((unsigned)(ceil_div(rows, kBlock) * ceil_div(cols, kBlock)), (unsigned)count);
+  quantize_tile_kernel<T, kVec, false, false, true><<<grid, 256, 0, st>>>(X, ldx, rows, cols, nullptr, 0, nullptr, Q, ld, S, Segments{}, x_step, q_step);
+  return cudaGetLastError();
+}
+template <class T, bool kVec>
+cudaError_t launch_segments(int64_t blocks, const Segments& s, int rows, int cols, const T* X, int64_t ldx, uint8_t* Qr, int64_t ldr, uint8_t* Sr, uint8_t* Qc, int64_t ldc,
+                            uint8_t* Sc, cudaStream_t st) {
+  const unsigned tiles = (unsigned)(blocks * ceil_div(cols, kBlock));
+  if (Qr) quantize_tile_kernel<T, kVec, true, true, false, true><<<tiles, 256, 0, st>>>(X, ldx, rows, cols, Qr, ldr, Sr, Qc, ldc, Sc, s);
+  else quantize_tile_kernel<T, kVec, false, true, false, true><<<tiles, 256, 0, st>>>(X, ldx, rows, cols, nullptr, 0, nullptr, Qc, ldc, Sc, s);
   return cudaGetLastError();
 }
 
@@ -352,24 +410,62 @@ ozk_status ozk_fp8_quantize_lines(int64_t rows, int64_t cols, const void* X, int
   return e == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
 }
 
-ozk_status ozk_fp8_quantize_tiles(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
-                                  void* stream) {
+ozk_status ozk_fp8_quantize_segments(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, const int32_t* offsets, int64_t segments,
+                                     uint8_t* row_codes, int64_t row_ld, uint8_t* row_scales, uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales, void* stream) {
   bool vec;
   const ozk_status rc = check_input(rows, cols, X, x_type, ldx, &vec);
   if (rc != OZK_OK) return rc;
-  if (rows == 0 || cols == 0) return OZK_OK;
-  if (!good_codes(codes, ld, cols, scales, 1)) return OZK_ERR_INVALID_ARG;
+  if (segments < 0) return OZK_ERR_INVALID_ARG;
+  if (segments > INT32_MAX - 1024) return OZK_ERR_UNSUPPORTED;
+  if (rows == 0 || cols == 0 || segments == 0) return OZK_OK;
+  if (!offsets || (reinterpret_cast<uintptr_t>(offsets) & 3)) return OZK_ERR_INVALID_ARG;
+  const int64_t blocks = ozk_fp8_segment_blocks(rows, segments);
+  if (blocks * ceil_div(cols, kBlock) > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+  if ((row_codes || row_scales) && !good_codes(row_codes, row_ld, cols, row_scales, 4)) return OZK_ERR_INVALID_ARG;
+  if (!good_codes(col_codes, col_ld, cols, col_scales, 4)) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const Segments s{offsets, (int)segments};
   const int r = (int)rows, c = (int)cols;
   cudaError_t e;
   if (x_type == OZK_F32) {
     const float* x = static_cast<const float*>(X);
-    e = vec ? launch_tiles<float, true>(r, c, x, ldx, codes, ld, scales, st) : launch_tiles<float, false>(r, c, x, ldx, codes, ld, scales, st);
+    e = vec ? launch_segments<float, true>(blocks, s, r, c, x, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, st)
+            : launch_segments<float, false>(blocks, s, r, c, x, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, st);
   } else {
     const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(X);
-    e = vec ? launch_tiles<__nv_bfloat16, true>(r, c, x, ldx, codes, ld, scales, st)
-            : launch_tiles<__nv_bfloat16, false>(r, c, x, ldx, codes, ld, scales, st);
+    e = vec ? launch_segments<__nv_bfloat16, true>(blocks, s, r, c, x, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, st)
+            : launch_segments<__nv_bfloat16, false>(blocks, s, r, c, x, ldx, row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, st);
+  }
+  return e == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
+}
+
+ozk_status ozk_fp8_quantize_tiles(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, uint8_t* codes, int64_t ld, uint8_t* scales,
+                                  void* stream) {
+  return ozk_fp8_quantize_experts(1, rows, cols, X, x_type, ldx, 0, codes, ld, 0, scales, stream);
+}
+
+ozk_status ozk_fp8_quantize_experts(int64_t experts, int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, int64_t x_step, uint8_t* codes, int64_t ld,
+                                    int64_t step, uint8_t* scales, void* stream) {
+  bool vec;
+  const ozk_status rc = check_input(rows, cols, X, x_type, ldx, &vec);
+  if (rc != OZK_OK) return rc;
+  if (experts < 0 || step % 16 || (experts > 1 && (x_step < 0 || step < (rows - 1) * ld + cols))) return OZK_ERR_INVALID_ARG;
+  if (experts > 65535) return OZK_ERR_UNSUPPORTED;
+  if (experts == 0 || rows == 0 || cols == 0) return OZK_OK;
+  if (!good_codes(codes, ld, cols, scales, 1)) return OZK_ERR_INVALID_ARG;
+  if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
+  vec = vec && (x_step * (x_type == OZK_F32 ? 4 : 2)) % 16 == 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int n = (int)experts, r = (int)rows, c = (int)cols;
+  cudaError_t e;
+  if (x_type == OZK_F32) {
+    const float* x = static_cast<const float*>(X);
+    e = vec ? launch_tiles<float, true>(n, r, c, x, ldx, x_step, codes, ld, step, scales, st) : launch_tiles<float, false>(n, r, c, x, ldx, x_step, codes, ld, step, scales, st);
+  } else {
+    const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(X);
+    e = vec ? launch_tiles<__nv_bfloat16, true>(n, r, c, x, ldx, x_step, codes, ld, step, scales, st)
+            : launch_tiles<__nv_bfloat16, false>(n, r, c, x, ldx, x_step, codes, ld, step, scales, st);
   }
   return e == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
 }

@@ -1,4 +1,4 @@
-"""The 8-bit operators on torch tensors: quantisation by blocks of 128, the block-scaled product, AdamW.
+"""The 8-bit operators on torch tensors: quantisation by blocks of 128, the block-scaled product, the norm before it, products by expert, AdamW.
 
 A linear layer in 8 bits:
 
@@ -8,12 +8,25 @@ A linear layer in 8 bits:
     dx = matmul(quantize_lines(dy)[0], w8, over_rows=True)                       # dx = dy w
     dw = matmul(quantize_lines(dy, rows=False, cols=True)[1], xt8, over_rows=True, dtype=torch.float32)   # dw = dy^T x
 
-`linear` is the same as a differentiable function.  Everything runs on the current stream of the tensors' device
+`linear` is the same as a differentiable function.  `rms_norm` adds the residual stream, norms it and writes x8 and xt8 in its place; `norm_linear` is the
+differentiable whole.
+
+A layer of experts, whose rows lie in the order of the experts (`offsets[e]` .. `offsets[e + 1]` are those of expert e):
+
+    x8, xt8 = quantize_segments(x, offsets)             # xt8: blocks of 128 tokens that begin with each expert
+    w8 = quantize_experts(w)                            # [experts, outputs, inputs]
+    y = grouped_matmul(x8, w8, offsets)
+    dy8, dyt8 = quantize_segments(dy, offsets)
+    dx = grouped_matmul(dy8, w8, offsets, over_rows=True)
+    dw = grouped_matmul(dyt8, xt8, offsets, dtype=torch.float32)
+
+`expert_linear` is the same as a differentiable function.  Everything runs on the current stream of the tensors' device
 through libozk.so; arguments are checked here (ValueError) and in the library (OzkError), nothing falls back.
 """
 from __future__ import annotations
 
 import ctypes
+from typing import NamedTuple
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -313,6 +326,382 @@ def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> tor
     elif w.shape != (w8.rows, w8.cols) or w8.scales.dtype != torch.uint8 or not (w8.kind == TILES or (w8.kind == ROWS and not for_dx)):
         raise ValueError(f"w8 is a {tuple(w.shape)} Fp8Matrix by {TILES} with UE8M0 scales (or by {ROWS}, where x needs no gradient), not {w8.rows} x {w8.cols} by {w8.kind}")
     return _Linear.apply(x, w, w8, for_dx, for_dw)
+
+
+class Normed(NamedTuple):
+    """What rms_norm was asked for: the 8-bit forms, the answer without quantisation, the updated stream, its inverse roots."""
+    rows: "Fp8Matrix | None"
+    cols: "Fp8Matrix | None"
+    y: "torch.Tensor | None"
+    total: torch.Tensor
+    root: "torch.Tensor | None"
+
+
+def _beside(t: torch.Tensor, what: str, x: torch.Tensor, dtypes) -> int:
+    """Checks a matrix of the shape of x, and returns its leading dimension."""
+    if t.dtype not in dtypes or t.shape != x.shape or t.get_device() != x.get_device() or (t.shape[1] > 1 and t.stride(1) != 1 and t.shape[0]):
+        raise ValueError(f"{what} is {' or '.join(map(str, dtypes))} {tuple(x.shape)} on {x.device} with contiguous rows, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vector(t: torch.Tensor, what: str, n: int, index: int) -> int:
+    kind = _type(t, what)
+    if t.shape != (n,) or t.get_device() != index or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what} is a contiguous [{n}] on GPU {index}")
+    return kind
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6, rows: "bool | Fp8Matrix | None" = True,
+             cols: "bool | Fp8Matrix | None" = False, y: "bool | torch.Tensor | None" = False, total: torch.Tensor | None = None,
+             root: "bool | torch.Tensor | None" = False) -> Normed:
+    """The RMS norm of x + residual, times `weight` [cols], as operands of the products: h = x + residual, s = 1 / sqrt(mean(h^2) + eps), h s weight.
+    x [rows, cols] float32 or bfloat16; residual of the same type or float32, and h is rounded to it before it is normed.
+    `rows`, `cols`: as for quantize_lines; `y`: whether (or where) the answer is wanted in the type of x too; `total`: where h is written (a new tensor if
+    None; may be `residual`, or x if of one type); `root`: whether (or where) s is wanted, float32 [rows], for rms_norm_backward."""
+    r, c, kind, ld = _input(x)
+    index, device = x.get_device(), x.device
+    w_kind = _vector(weight, "weight", c, index)
+    written = []
+    if residual is None:
+        if total is not None:
+            raise ValueError("total is written where there is a residual")
+        total, to_residual = x, (None, 0, 0, None, 0)
+    else:
+        ldr = _beside(residual, "residual", x, (x.dtype,) if x.dtype is torch.float32 else (x.dtype, torch.float32))
+        if total is None:
+            total = torch.empty(r, c, dtype=residual.dtype, device=device)
+        else:
+            written.append(total)
+        ldt = _beside(total, "total", x, (residual.dtype,))
+        to_residual = (residual.data_ptr(), _TYPES[residual.dtype], ldr, total.data_ptr(), ldt)
+    by_rows = Fp8Matrix.empty(r, c, ROWS, device) if rows is True else rows or None
+    by_cols = Fp8Matrix.empty(r, c, COLS, device) if cols is True else cols or None
+    to_rows = _NONE if by_rows is None else _output(by_rows, r, c, ROWS, index)
+    to_cols = _NONE if by_cols is None else _output(by_cols, r, c, COLS, index)
+    if y is True:
+        y, ldy = torch.empty(r, c, dtype=x.dtype, device=device), max(c, 1)
+    elif y is None or y is False:
+        y, ldy = None, 0
+    else:
+        ldy = _beside(y, "y", x, (x.dtype,))
+        written.append(y)
+    if root is True or ((root is None or root is False) and by_cols is not None):
+        root = torch.empty(r, dtype=torch.float32, device=device)
+    elif root is None or root is False:
+        root = None
+    elif _vector(root, "root", r, index) != ozk.OZK_F32:
+        raise ValueError("root is float32")
+    else:
+        written.append(root)
+    _call(index, "ozk_rms_norm", r, c, x.data_ptr(), kind, ld, *to_residual, weight.data_ptr(), w_kind, eps, None if root is None else root.data_ptr(),
+          None if y is None else y.data_ptr(), ldy, *to_rows, *to_cols, _stream(index))
+    if by_rows is rows and rows:
+        _rewritten(rows)
+    if by_cols is cols and cols:
+        _rewritten(cols)
+    if written:
+        _written(_versioned(written))
+    return Normed(by_rows, by_cols, y, total, root)
+
+
+def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, root: torch.Tensor, weight: torch.Tensor, dtotal: torch.Tensor | None = None,
+                      need_weight: bool = True) -> tuple[torch.Tensor, torch.Tensor | None]:
+    """Gradients of rms_norm: (that of x and of the residual, in the type of `total`; that of the weight, float32, if wanted).
+    dy: the gradient of the answer; total, root: from rms_norm (total is x where there was no residual); dtotal: the gradient that reaches `total` from elsewhere, in its type."""
+    r, c, kind, ld = _input(total)
+    index = total.get_device()
+    _type(dy, "dy")
+    ldd = _beside(dy, "dy", total, (dy.dtype,))
+    if _vector(root, "root", r, index) != ozk.OZK_F32:
+        raise ValueError("root is float32")
+    w_kind = _vector(weight, "weight", c, index)
+    to_dtotal = (None, 0) if dtotal is None else (dtotal.data_ptr(), _beside(dtotal, "dtotal", total, (total.dtype,)))
+    dx = torch.empty(r, c, dtype=total.dtype, device=total.device)
+    if need_weight:
+        dw = torch.empty(c, dtype=torch.float32, device=total.device)
+        size = _code(index, "ozk_rms_norm_backward_scratch_bytes", r, c)
+        scratch = torch.empty(size, dtype=torch.uint8, device=total.device)
+        to_dw = (dw.data_ptr(), scratch.data_ptr(), size)
+    else:
+        dw, to_dw = None, (None, None, 0)
+    _call(index, "ozk_rms_norm_backward", r, c, dy.data_ptr(), _TYPES[dy.dtype], ldd, total.data_ptr(), kind, ld, root.data_ptr(), weight.data_ptr(), w_kind, *to_dtotal,
+          dx.data_ptr(), max(c, 1), *to_dw, _stream(index))
+    return dx, dw
+
+
+class _NormLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, norm_weight, w, residual, eps, w8, need_n, need_w):
+        flat = _rows(x)
+        n = rms_norm(flat, norm_weight, None if residual is None else _rows(residual), eps, True, need_w, root=need_n)
+        ctx.set_materialize_grads(False)
+        ctx.n8, ctx.w8, ctx.shape, ctx.types = n.cols, w8, x.shape, (x.dtype, norm_weight.dtype, w.dtype, None if residual is None else residual.dtype)
+        ctx.versions = [(t, t._version) for t in _versioned((w8.codes, w8.scales))] if need_n else []
+        out = matmul(n.rows, w8, dtype=x.dtype).reshape(*x.shape[:-1], w8.rows)
+        if residual is None:
+            ctx.save_for_backward(x, n.root, norm_weight)
+            return out
+        total = n.total.reshape(x.shape)
+        ctx.save_for_backward(total, n.root, norm_weight)
+        return out, total
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dtotal=None):
+        total, root, norm_weight = ctx.saved_tensors
+        need_x, need_nw, need_w, need_r = ctx.needs_input_grad[:4]
+        need_n = need_x or need_nw or need_r
+        if need_n and any(t._version != v for t, v in ctx.versions):
+            raise RuntimeError("the 8-bit weights needed for the gradient of x have been modified by an inplace operation")
+        dx = dnw = dw = None
+        if dy is None:   # only the stream was used
+            dx = dtotal
+        else:
+            by_rows, by_cols = quantize_lines(_rows(dy), need_n, need_w)
+            if need_n:
+                dn = matmul(by_rows, ctx.w8, over_rows=True, dtype=ctx.types[0])
+                dx, dnw = rms_norm_backward(dn, _rows(total), root, norm_weight, None if dtotal is None else _rows(dtotal), need_nw)
+                dx = dx.reshape(ctx.shape)
+                dnw = dnw.to(ctx.types[1]) if need_nw else None
+            if need_w:
+                dw = matmul(by_cols, ctx.n8, dtype=torch.float32).to(ctx.types[2])
+        return dx.to(ctx.types[0]) if need_x and dx is not None else None, dnw, dw, dx if need_r else None, None, None, None, None
+
+
+def norm_linear(x: torch.Tensor, norm_weight: torch.Tensor, w: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
+                w8: Fp8Matrix | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(norm(x + residual) w^T, x + residual): rms_norm and linear in 8 bits, with gradients of x, residual, norm_weight and w (gradients of these gradients
+    raise RuntimeError).  x, residual: [..., inputs]; norm_weight: [inputs]; w: [outputs, inputs], all the layer's projections side by side; w8: as for `linear`.
+    Without a residual the second answer is x."""
+    grads = torch.is_grad_enabled()
+    need_n = grads and (x.requires_grad or norm_weight.requires_grad or (residual is not None and residual.requires_grad))
+    need_w = grads and w.requires_grad
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"residual is {tuple(x.shape)}, not {tuple(residual.shape)}")
+    if w8 is None:
+        w8 = quantize_tiles(_rows(w.detach()))
+    elif w.shape != (w8.rows, w8.cols) or w8.scales.dtype != torch.uint8 or not (w8.kind == TILES or (w8.kind == ROWS and not need_n)):
+        raise ValueError(f"w8 is a {tuple(w.shape)} Fp8Matrix by {TILES} with UE8M0 scales (or by {ROWS}, where nothing before it needs a gradient), not {w8.rows} x {w8.cols} by {w8.kind}")
+    out = _NormLinear.apply(x, norm_weight, w, residual, eps, w8, need_n, need_w)
+    return (out, x) if residual is None else out
+
+
+class Fp8Experts:
+    """The weights of several experts, [experts, rows, cols]: E4M3 codes (uint8 [experts, rows, ld], ld and the step between experts multiples of 16) with a UE8M0 scale for
+    each 128 x 128 tile of each expert (uint8 [experts, ceil(rows/128), ceil(cols/128)]).  Products sum over the columns, or over the rows."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
+        _need_cuda(codes, "codes")
+        if codes.dtype == torch.float8_e4m3fn:
+            codes = codes.view(torch.uint8)
+        if codes.dtype != torch.uint8 or codes.dim() != 3 or codes.shape[1] != rows or codes.shape[2] < cols:
+            raise ValueError(f"codes are uint8 or float8_e4m3fn [experts, {rows}, at least {cols}], not {codes.dtype} {tuple(codes.shape)}")
+        n = codes.shape[0]
+        ld = codes.stride(1) if rows > 1 else _up(max(codes.shape[2], 1), 16)
+        step = codes.stride(0) if n > 1 else 0
+        if n and rows and cols and (codes.stride(2) != 1 or ld % 16 or ld < cols or codes.data_ptr() % 16 or step % 16 or (n > 1 and step < (rows - 1) * ld + cols)):
+            raise ValueError("codes lie in rows of a multiple of 16 bytes, at a multiple of 16 bytes, experts apart from each other")
+        want = (n, -(-rows // 128), -(-cols // 128))
+        if scales.dtype != torch.uint8 or scales.device != codes.device or not scales.is_contiguous() or tuple(scales.shape) != want:
+            raise ValueError(f"scales of {n} x {rows} x {cols}: {scales.dtype} {tuple(scales.shape)}, wanted torch.uint8 {want} on {codes.device}")
+        self.codes, self.scales, self.experts, self.rows, self.cols = codes, scales, n, rows, cols
+        self.index = codes.device.index
+        self._seen = None
+        self._operand = [ozk.ozk_fp8_experts(codes.data_ptr(), ld, step, scales.data_ptr(), over) for over in (0, 1)]
+        self._at = [ctypes.addressof(o) for o in self._operand]
+        self._target = (codes.data_ptr(), ld, step, scales.data_ptr())
+
+    @classmethod
+    def empty(cls, experts: int, rows: int, cols: int, device: torch.device | str = "cuda") -> "Fp8Experts":
+        codes = torch.empty(experts, rows, max(_up(cols, 16), 16), dtype=torch.uint8, device=device)
+        return cls(codes, torch.empty(experts, -(-rows // 128), -(-cols // 128), dtype=torch.uint8, device=device), rows, cols)
+
+    def values8(self) -> torch.Tensor:
+        """The codes as torch's 8-bit type, [experts, rows, cols], without the scales."""
+        return self.codes.view(torch.float8_e4m3fn)[:, :, :self.cols]
+
+    def dequantize(self) -> torch.Tensor:
+        """Codes times scales in float32."""
+        s = torch.where(self.scales > 0, self.scales.int() << 23, 1 << 22).view(torch.float32)
+        return self.values8().float() * s.repeat_interleave(128, 1)[:, :self.rows].repeat_interleave(128, 2)[:, :, :self.cols]
+
+
+class Fp8Segments:
+    """A rows x cols matrix whose rows belong to experts, as products that sum over the rows of each of them want it: E4M3 codes (uint8 [blocks * 128, ld]) in blocks of
+    128 rows that begin with each expert's rows, zeros behind them, and UE8M0 scales per 128 x 1 block (uint8 [ceil(blocks/4), cols, 4]).  blocks:
+    segment_blocks(rows, experts), which is enough for any offsets; those that no expert takes hold nothing."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int, experts: int):
+        _need_cuda(codes, "codes")
+        if codes.dtype == torch.float8_e4m3fn:
+            codes = codes.view(torch.uint8)
+        blocks = segment_blocks(rows, experts)
+        if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[0] != blocks * 128 or codes.shape[1] < cols:
+            raise ValueError(f"codes are uint8 or float8_e4m3fn [{blocks * 128}, at least {cols}], not {codes.dtype} {tuple(codes.shape)}")
+        ld = codes.stride(0)
+        if blocks and cols and (codes.stride(1) != 1 or ld % 16 or ld < cols or codes.data_ptr() % 16):
+            raise ValueError("codes lie in rows of a multiple of 16 bytes, at a multiple of 16 bytes")
+        want = (-(-blocks // 4), cols, 4)
+        if scales.dtype != torch.uint8 or scales.device != codes.device or not scales.is_contiguous() or tuple(scales.shape) != want:
+            raise ValueError(f"scales of {blocks} blocks and {cols} columns: {scales.dtype} {tuple(scales.shape)}, wanted torch.uint8 {want} on {codes.device}")
+        self.codes, self.scales, self.rows, self.cols, self.experts = codes, scales, rows, cols, experts
+        self.index = codes.device.index
+        self._seen = None
+        self._values8 = codes.view(torch.float8_e4m3fn)[:, :cols]
+        self._target = (codes.data_ptr(), ld, scales.data_ptr())
+        self._operand = ozk.ozk_fp8_operand(codes.data_ptr(), ld, scales.data_ptr(), ozk.OZK_SCALE_LINES, 1)
+        self._at = ctypes.addressof(self._operand)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, experts: int, device: torch.device | str = "cuda") -> "Fp8Segments":
+        blocks = segment_blocks(rows, experts)
+        codes = torch.empty(blocks * 128, max(_up(cols, 16), 16), dtype=torch.uint8, device=device)
+        return cls(codes, torch.empty(-(-blocks // 4), cols, 4, dtype=torch.uint8, device=device), rows, cols, experts)
+
+    def values8(self) -> torch.Tensor:
+        """The codes as torch's 8-bit type, [blocks * 128, cols], without the scales."""
+        return self._values8
+
+
+def segment_blocks(rows: int, experts: int) -> int:
+    """Blocks of 128 rows that the segments of any offsets fit into, where each begins a block of its own."""
+    return (rows + 127 * min(experts, rows)) // 128
+
+
+def _offsets(offsets: torch.Tensor, experts: int, index: int) -> int:
+    if offsets.dtype is not torch.int32 or offsets.shape != (experts + 1,) or offsets.get_device() != index or not offsets.is_contiguous():
+        raise ValueError(f"offsets are contiguous int32 [{experts + 1}] on GPU {index}, not {offsets.dtype} {tuple(offsets.shape)} on {offsets.device}")
+    return offsets.data_ptr()
+
+
+def quantize_experts(w: torch.Tensor, out: Fp8Experts | None = None) -> Fp8Experts:
+    """w [experts, rows, cols] (float32 or bfloat16), every expert by 128 x 128 tiles of its own."""
+    kind = _type(w, "w")
+    _need_cuda(w, "w")
+    if w.dim() != 3 or (w.numel() and w.shape[2] > 1 and w.stride(2) != 1):
+        raise ValueError("w has three dimensions and contiguous rows")
+    n, r, c = w.shape
+    q = Fp8Experts.empty(n, r, c, w.device) if out is None else out
+    if (q.experts, q.rows, q.cols, q.index) != (n, r, c, w.get_device()):
+        raise ValueError(f"out is an Fp8Experts of {n} x {r} x {c} on GPU {w.get_device()}")
+    codes, ld, step, scales = q._target
+    _call(q.index, "ozk_fp8_quantize_experts", n, r, c, w.data_ptr(), kind, w.stride(1) if r > 1 else max(c, 1), w.stride(0) if n > 1 else 0, codes, ld, step, scales, _stream(q.index))
+    if out is not None:
+        _rewritten(out)
+    return q
+
+
+def quantize_segments(x: torch.Tensor, offsets: torch.Tensor, rows: "bool | Fp8Matrix | None" = True, cols: "Fp8Segments | None" = None):
+    """x [rows, cols] (float32 or bfloat16), whose rows offsets[e] .. offsets[e + 1] - 1 belong to expert e (offsets: int32, ascending, on the GPU): the pair of
+    its form by 1 x 128 blocks (None where `rows` is False; an Fp8Matrix to write to) and its Fp8Segments (`cols`, or a new one), in one pass over x.
+    Rows that belong to no expert are not read; what stands for them in `rows` is left as it was."""
+    r, c, kind, ld = _input(x)
+    index = x.get_device()
+    experts = offsets.shape[0] - 1 if offsets.dim() == 1 else -1
+    if experts < 0:
+        raise ValueError("offsets have one dimension, a number more than there are experts")
+    at = _offsets(offsets, experts, index)
+    by_rows = Fp8Matrix.empty(r, c, ROWS, x.device) if rows is True else rows or None
+    to_rows = _NONE if by_rows is None else _output(by_rows, r, c, ROWS, index)
+    by_cols = Fp8Segments.empty(r, c, experts, x.device) if cols is None else cols
+    if (by_cols.rows, by_cols.cols, by_cols.experts, by_cols.index) != (r, c, experts, index):
+        raise ValueError(f"cols is an Fp8Segments of {r} x {c} and {experts} experts on GPU {index}")
+    _call(index, "ozk_fp8_quantize_segments", r, c, x.data_ptr(), kind, ld, at, experts, *to_rows, *by_cols._target, _stream(index))
+    if by_rows is rows and rows:
+        _rewritten(rows)
+    if cols is not None:
+        _rewritten(cols)
+    return by_rows, by_cols
+
+
+def grouped_matmul(a: "Fp8Matrix | Fp8Segments", b: "Fp8Experts | Fp8Segments", offsets: torch.Tensor, out: torch.Tensor | None = None, over_rows: bool = False,
+                   dtype: torch.dtype = torch.bfloat16, accumulate: bool = False) -> torch.Tensor:
+    """Products grouped by expert; rows offsets[e] .. offsets[e + 1] - 1 are those of expert e (int32, ascending, on the GPU).
+      grouped_matmul(x by ROWS, w, offsets)                    x w_e^T, [rows, rows of w]
+      grouped_matmul(dy by ROWS, w, offsets, over_rows=True)   dy w_e, [rows, columns of w]
+      grouped_matmul(dy segments, x segments, offsets)         dy_e^T x_e, [experts, columns of dy, columns of x]
+    Returns `out` if given (float32 or bfloat16; float32 with accumulate, which adds, for the third).  Rows that belong to no expert are left as they
+    were in `out`, and are zero in a new result; an expert without rows has a product of zeros."""
+    if isinstance(b, Fp8Segments):
+        if not isinstance(a, Fp8Segments) or over_rows:
+            raise ValueError("segments are multiplied with segments, over their rows")
+        if (a.rows, a.experts) != (b.rows, b.experts):
+            raise ValueError(f"the operands have {a.rows} rows of {a.experts} experts and {b.rows} of {b.experts}")
+        shape, experts = (a.experts, a.cols, b.cols), a.experts
+    else:
+        if not isinstance(b, Fp8Experts) or not isinstance(a, Fp8Matrix) or a.kind != ROWS or a.scales.dtype != torch.uint8:
+            raise ValueError("an Fp8Matrix by rows with UE8M0 scales is multiplied with Fp8Experts")
+        if accumulate:
+            raise ValueError("only products of segments are added")
+        k, n = (b.rows, b.cols) if over_rows else (b.cols, b.rows)
+        if a.cols != k:
+            raise ValueError(f"the operands are summed over {a.cols} and {k} elements")
+        shape, experts = (a.rows, n), b.experts
+    index = a.index
+    if b.index != index:
+        raise ValueError("the operands are on two devices")
+    at = _offsets(offsets, experts, index)
+    given = out
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        if dtype not in _TYPES:
+            raise ValueError(f"the result is float32 or bfloat16, not {dtype}")
+        out = torch.empty(*shape[:-1], _up(shape[-1], 8), dtype=dtype, device=a.codes.device)[..., :shape[-1]]   # rows at 16-byte boundaries
+    elif tuple(out.shape) != shape or out.get_device() != index or (shape[-1] > 1 and out.stride(-1) != 1):
+        raise ValueError(f"out is {list(shape)} on GPU {index} with contiguous rows")
+    kind, status, stream = _type(out, "out"), _status(index), _stream(index)
+    ldc = out.stride(-2) if shape[-2] > 1 else max(shape[-1], 1)
+    if len(shape) == 3:
+        _call(index, "ozk_fp8_segment_gemm", experts, shape[1], shape[2], a.rows, a._at, b._at, at, out.data_ptr(), kind, ldc, out.stride(0) if experts > 1 else 0,
+              1 if accumulate else 0, status, stream)
+    else:
+        _call(index, "ozk_fp8_grouped_gemm", shape[0], shape[1], a.cols, a._at[0], b._at[1 if over_rows else 0], experts, at, out.data_ptr(), kind, ldc,
+              1 if given is None else 0, status, stream)
+    if given is not None and not given.is_inference():
+        _written((given,))
+    return out
+
+
+class _ExpertLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, offsets, w8, for_dx, for_dw):
+        flat = _rows(x)
+        by_rows, by_cols = quantize_segments(flat, offsets) if for_dw else (quantize_lines(flat)[0], None)
+        ctx.x8, ctx.w8, ctx.types = by_cols, w8, (x.dtype, w.dtype)
+        ctx.versions = [(t, t._version) for t in _versioned((w8.codes, w8.scales))] if for_dx else []
+        ctx.save_for_backward(offsets)
+        return grouped_matmul(by_rows, w8, offsets, dtype=x.dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        offsets, = ctx.saved_tensors
+        need_x, need_w = ctx.needs_input_grad[:2]
+        if need_x and any(t._version != v for t, v in ctx.versions):
+            raise RuntimeError("the 8-bit weights needed for the gradient of x have been modified by an inplace operation")
+        flat = _rows(dy)
+        by_rows, by_cols = quantize_segments(flat, offsets, need_x) if need_w else (quantize_lines(flat)[0] if need_x else None, None)
+        dx = grouped_matmul(by_rows, ctx.w8, offsets, over_rows=True, dtype=ctx.types[0]) if need_x else None
+        dw = grouped_matmul(by_cols, ctx.x8, offsets, dtype=torch.float32).to(ctx.types[1]) if need_w else None
+        return dx, dw, None, None, None, None
+
+
+def expert_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, w8: Fp8Experts | None = None) -> torch.Tensor:
+    """x w_e^T in 8 bits, e the expert of each row, with gradients of x and w as `linear` has them.  x: [rows, inputs], rows in the order of the experts; w: [experts, outputs, inputs];
+    offsets: int32 [experts + 1], ascending, on the GPU: expert e has rows offsets[e] .. offsets[e + 1] - 1.  Rows that belong to nobody answer zeros and get gradients of zero.
+    w8: quantize_experts(w), where a program keeps it between steps."""
+    if x.dim() != 2 or w.dim() != 3 or x.shape[1] != w.shape[2]:
+        raise ValueError(f"x is [rows, inputs] and w [experts, outputs, inputs], not {tuple(x.shape)} and {tuple(w.shape)}")
+    _offsets(offsets, w.shape[0], x.get_device())
+    grads = torch.is_grad_enabled()
+    for_dx, for_dw = grads and x.requires_grad, grads and w.requires_grad
+    if w8 is None:
+        d = w.detach()
+        w8 = quantize_experts(d if d.is_contiguous() else d.contiguous())
+    elif tuple(w.shape) != (w8.experts, w8.rows, w8.cols):
+        raise ValueError(f"w8 is an Fp8Experts of {tuple(w.shape)}, not of {(w8.experts, w8.rows, w8.cols)}")
+    return _ExpertLinear.apply(x, w, offsets, w8, for_dx, for_dw)
 
 
 class AdamWTable:
