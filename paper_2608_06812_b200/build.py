@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libozk.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared",   # no fast-math: the FP32 residue arithmetic relies on IEEE fused multiply-adds
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0",   # sources side by side; no fast-math: the FP32 residue arithmetic relies on IEEE fused multiply-adds
 ]
 
 

@@ -5,101 +5,259 @@
 // The norm is of h as it is stored, so that the backward pass, which reads h and s, differentiates what was computed.  Sums and all
 // arithmetic in FP32, in an order that depends on the sizes alone; y is rounded once, to its codes.
 //
-// Rows: a row lies in the registers of 1 to 16 warps, 512 columns a warp and step; in each step lane l holds columns 128 b + 4 l .. + 3 (or, where
-// the rows do not allow 4 elements at a time, 128 b + 32 i + l) of four blocks b, so that a block's maximum is one warp-wide integer maximum
-// and the four scales of a word are known to the whole warp.
+// Rows: a row lies over 1 to 16 warps, 512 columns (one word of scales) a warp and step.  A lane holds eight consecutive columns of each 256, or four of
+// each 128, so that 16 or 32 lanes hold a block.  Thread blocks stay and take row after row, the next ones already on their way to shared memory.
 // Columns: blocks run along the rows, so a second kernel reads h again, tile by tile, with s known.
 #include <type_traits>
 
-#include "ozk_fp8.cuh"
+#include "ozk_fp8_product.cuh"
 
 namespace ozk {
 namespace {
 
 using namespace fp8;
 
-// ---- four elements of a lane ------------------------------------------------------------
-template <class T>
-struct Quad {
-  uint32_t w[sizeof(T)];   // BF16: two words, FP32: four
+// ---- consecutive elements of a lane ---------------------------------------------------------
+constexpr int kGroup = 512;   // columns a warp holds at a time
+template <class T, int kL>
+struct Piece {
+  uint32_t w[kL * sizeof(T) / 4];
 };
-__device__ __forceinline__ float quad_value(const Quad<__nv_bfloat16>& q, int i) { return i % 2 ? bf16_hi(q.w[i / 2]) : bf16_lo(q.w[i / 2]); }
-__device__ __forceinline__ float quad_value(const Quad<float>& q, int i) { return __uint_as_float(q.w[i]); }
-// Column of element i of a lane in the block that starts at `c0`, and how far those of a lane are apart.
-template <bool kVec>
-__device__ __forceinline__ int quad_col(int c0, int lane, int i) { return kVec ? c0 + 4 * lane + i : c0 + 32 * i + lane; }
+template <int kL>
+__device__ __forceinline__ float value(const Piece<__nv_bfloat16, kL>& q, int i) { return i % 2 ? bf16_hi(q.w[i / 2]) : bf16_lo(q.w[i / 2]); }
+template <int kL>
+__device__ __forceinline__ float value(const Piece<float, kL>& q, int i) { return __uint_as_float(q.w[i]); }
+// Two elements, rounded to the type.
+template <int kL>
+__device__ __forceinline__ void set2(Piece<__nv_bfloat16, kL>& q, int i, float a, float b) { q.w[i / 2] = pack_bf16(a, b); }
+template <int kL>
+__device__ __forceinline__ void set2(Piece<float, kL>& q, int i, float a, float b) { q.w[i] = __float_as_uint(a), q.w[i + 1] = __float_as_uint(b); }
 
-// Read once, so it need not stay in L1; not through the read-only path, because h may be written over x or r.
-__device__ __forceinline__ void load_stream(const __nv_bfloat16* p, Quad<__nv_bfloat16>& q) {
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(q.w[0]), "=r"(q.w[1]) : "l"(p) : "memory");
+// What is read once need not stay in L1; not through the read-only path, because h may be written over x or r.
+template <int kBytes>
+__device__ __forceinline__ void load_bytes(const void* p, uint32_t* w) {
+  if constexpr (kBytes == 16) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+  else if constexpr (kBytes == 8) asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  else if constexpr (kBytes == 4) asm volatile("ld.global.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
 }
-__device__ __forceinline__ void load_stream(const float* p, Quad<float>& q) {
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3]) : "l"(p) : "memory");
+template <int kBytes>
+__device__ __forceinline__ void store_bytes(void* p, const uint32_t* w) {
+  if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
 }
-// The lane's elements of the block at column c0 of a row; zeros beyond `cols`.
-template <bool kVec, class T>
-__device__ __forceinline__ void load_quad(const T* row, int c0, int lane, int cols, Quad<T>& q) {
-  if (kVec && c0 + 4 * lane + 4 <= cols) {
-    load_stream(row + c0 + 4 * lane, q);
+__device__ __forceinline__ uint32_t load_16(const void* p) {
+  uint16_t v;
+  asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
+  return v;
+}
+// Bytes of one access: kE elements, as far as places and strides allow, and 16 bytes at most.
+template <class T, int kE>
+__host__ __device__ constexpr int access() { return kE * (int)sizeof(T) > 16 ? 16 : kE * (int)sizeof(T); }
+// BF16 rows at odd places: a lane's elements are cut from the 4-byte words that hold them.  The words at a row's ends hold a neighbour's element too, which
+// in the matrix's first and last rows (`edge`) may not be there: these two are read element by element.
+template <class T, int kE>
+__host__ __device__ constexpr bool odd_places() { return sizeof(T) == 2 && kE == 1; }
+__device__ __forceinline__ int at_odd(const void* p) { return (int)(reinterpret_cast<uintptr_t>(p) & 2); }
+template <int kWords>
+__device__ __forceinline__ void cut(const uint32_t* in, int odd, uint32_t* out) {
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) out[i] = __funnelshift_r(in[i], in[i + 1], 8 * odd);
+}
+// The lane's elements from `p` on.  kFull: all belong to the row; otherwise `left` of them do, and the others are zero.
+template <bool kFull, int kE, class T, int kL>
+__device__ __forceinline__ void load_piece(const T* p, int left, bool edge, Piece<T, kL>& q) {
+  constexpr int kBytes = access<T, kE>(), kStep = kBytes / (int)sizeof(T);
+  if constexpr (odd_places<T, kE>()) {
+    if ((kFull || left >= kL) && !edge) {
+      const int odd = at_odd(p);
+      const char* from = reinterpret_cast<const char*>(p) - odd;
+      uint32_t w[kL / 2 + 1];
+#pragma unroll
+      for (int i = 0; i < kL / 2; ++i) load_bytes<4>(from + 4 * i, w + i);
+      w[kL / 2] = 0;
+      if (odd) load_bytes<4>(from + 2 * kL, w + kL / 2);
+      cut<kL / 2>(w, odd, q.w);
+      return;
+    }
+  } else if (kFull || left >= kL) {
+#pragma unroll
+    for (int i = 0; i < kL; i += kStep) load_bytes<kBytes>(p + i, q.w + i * (int)sizeof(T) / 4);
     return;
   }
 #pragma unroll
-  for (int k = 0; k < (int)sizeof(T); ++k) q.w[k] = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = quad_col<kVec>(c0, lane, i);
-    if (c >= cols) continue;
-    if constexpr (sizeof(T) == 2) q.w[i / 2] |= (uint32_t) * reinterpret_cast<const volatile uint16_t*>(row + c) << (16 * (i % 2));
-    else q.w[i] = *reinterpret_cast<const volatile uint32_t*>(row + c);
-  }
-}
-template <bool kVec, class T>
-__device__ __forceinline__ void store_quad(T* row, int c0, int lane, int cols, const float (&v)[4]) {
-  if (kVec && c0 + 4 * lane + 4 <= cols) {
+  for (int i = 0; i < kL; ++i) {
     if constexpr (sizeof(T) == 2) {
-      const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-      *reinterpret_cast<uint2*>(row + c0 + 4 * lane) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      const uint32_t v = i < left ? load_16(p + i) : 0u;
+      q.w[i / 2] = i % 2 ? q.w[i / 2] | v << 16 : v;
     } else {
-      *reinterpret_cast<float4*>(row + c0 + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
+      q.w[i] = 0u;
+      if (i < left) load_bytes<4>(p + i, q.w + i);
+    }
+  }
+}
+template <bool kFull, int kE, class T, int kL>
+__device__ __forceinline__ void store_piece(T* p, int left, const Piece<T, kL>& q) {
+  constexpr int kBytes = access<T, kE>(), kStep = kBytes / (int)sizeof(T);
+  if (kFull || left >= kL) {
+    if constexpr (!odd_places<T, kE>()) {
+#pragma unroll
+      for (int i = 0; i < kL; i += kStep) store_bytes<kBytes>(p + i, q.w + i * (int)sizeof(T) / 4);
+    } else if (at_odd(p)) {
+      reinterpret_cast<uint16_t*>(p)[0] = (uint16_t)q.w[0];
+#pragma unroll
+      for (int i = 1; i < kL - 1; i += 2) *reinterpret_cast<uint32_t*>(p + i) = __funnelshift_r(q.w[i / 2], q.w[i / 2 + 1], 16);
+      reinterpret_cast<uint16_t*>(p)[kL - 1] = (uint16_t)(q.w[kL / 2 - 1] >> 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kL; i += 2) store_bytes<4>(p + i, q.w + i / 2);
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = quad_col<kVec>(c0, lane, i);
-    if (c < cols) store_element(row + c, v[i]);
+  for (int i = 0; i < kL; ++i) {
+    if (i >= left) continue;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p + i) = (uint16_t)(q.w[i / 2] >> (16 * (i % 2)));
+    else store_bytes<4>(p + i, q.w + i);
   }
 }
-// E4M3 codes, which lie at multiples of 16 bytes: four at a time in either layout of x where the lane's columns are neighbours.
-template <bool kVec>
-__device__ __forceinline__ void store_codes(uint8_t* row, int c0, int lane, int cols, uint32_t codes) {
-  if (kVec && c0 + 4 * lane + 4 <= cols) {
-    *reinterpret_cast<uint32_t*>(row + c0 + 4 * lane) = codes;
-    return;
-  }
+// Weights: cols numbers of either type; a lane's are read together where the array is aligned for it.
+enum { kWeightBf16 = 1, kWeightLoose = 2 };
+template <bool kFull, int kL>
+__device__ __forceinline__ void load_weights(const void* w, int kind, int c, int left, float (&v)[kL]) {
+  if ((kFull || left >= kL) && !(kind & kWeightLoose)) {
+    if (kind & kWeightBf16) {
+      Piece<__nv_bfloat16, kL> q;
+      if constexpr (kL == 8) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + c));
+        q.w[0] = u.x, q.w[1] = u.y, q.w[2] = u.z, q.w[3] = u.w;
+      } else {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + c));
+        q.w[0] = u.x, q.w[1] = u.y;
+      }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = quad_col<kVec>(c0, lane, i);
-    if (c < cols) row[c] = (uint8_t)(codes >> (8 * i));
-  }
-}
-// Weights are read again for every row: they stay in L1, and the registers they would take hold the rows in flight.
-template <bool kVec>
-__device__ __forceinline__ void load_weight(const void* w, int bf16, int c0, int lane, int cols, float (&v)[4]) {
-  if (kVec && c0 + 4 * lane + 4 <= cols) {
-    if (bf16) {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + c0 + 4 * lane));
-      v[0] = bf16_lo(u.x), v[1] = bf16_hi(u.x), v[2] = bf16_lo(u.y), v[3] = bf16_hi(u.y);
+      for (int i = 0; i < kL; ++i) v[i] = value(q, i);
     } else {
-      const float4 f = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c0 + 4 * lane));
-      v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+#pragma unroll
+      for (int i = 0; i < kL; i += 4) {
+        const float4 f = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + i));
+        v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+      }
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = quad_col<kVec>(c0, lane, i);
-    v[i] = c >= cols ? 0.f : bf16 ? __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(w) + c)) : __ldg(static_cast<const float*>(w) + c);
+  for (int i = 0; i < kL; ++i)
+    v[i] = i >= left ? 0.f : kind & kWeightBf16 ? __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(w) + c + i)) : __ldg(static_cast<const float*>(w) + c + i);
+}
+
+// ---- rows on their way ----------------------------------------------------------------------
+// A thread copies its own elements of the rows it will see next to shared memory and reads back nobody else's, so that no barrier is needed, no
+// register holds what is in flight, and a row's reduction does not hold up the next one's loads.  A lane's elements that the row ends among are read directly.
+constexpr int kRingBytes = 200 << 10;   // of a multiprocessor's shared memory
+template <int kBytes>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+template <int kBytes>
+__device__ __forceinline__ void load_shared(uint32_t at, uint32_t* w) {
+  if constexpr (kBytes == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+  else if constexpr (kBytes == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+}
+template <class T, int kL, int kE, int V, bool kWhole, bool kOn>
+struct Stream {
+  static constexpr bool kOdd = odd_places<T, kE>();
+  static constexpr int kBytes = kOdd ? 4 : access<T, kE>(), kStep = kBytes / (int)sizeof(T), kCopies = kL / kStep + (kOdd ? 1 : 0), kPieces = 16 / kL;
+  static constexpr int kThread = kOn ? V * kPieces * kCopies * kBytes : 0;   // bytes of a thread's share of a row
+  // Copy i of piece k of group v: the threads' copies lie side by side.
+  __device__ static __forceinline__ uint32_t place(uint32_t base, int v, int k, int i) { return base + (uint32_t)((((v * kPieces + k) * kCopies + i) * (int)blockDim.x) + (int)threadIdx.x) * kBytes; }
+  // row: the lane's first column in the row; group_left: columns of the row from the warp's group on.
+  __device__ static __forceinline__ void fetch(const T* row, uint32_t base, int step, int lane, int group_left, bool edge) {
+    if constexpr (kOn) {
+      const int odd = kOdd ? at_odd(row) : 0;
+      if (kOdd && edge) return;
+      const char* from = reinterpret_cast<const char*>(row) - odd;
+      auto copy = [&](int v, int k) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i)
+          if (!kOdd || i + 1 < kCopies || odd) copy_async<kBytes>(place(base, v, k, i), from + (int64_t)(v * step + k * 32 * kL) * (int)sizeof(T) + i * kBytes);
+      };
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int left = group_left - v * step;   // the same for all lanes
+        if (kWhole ? left > 0 : left >= kGroup) {
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) copy(v, k);
+        } else if (!kWhole && left > 0) {
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k)
+            if (left - k * 32 * kL - lane * kL >= kL) copy(v, k);
+        }
+      }
+    }
+  }
+  template <bool kFull>
+  __device__ static __forceinline__ void take(const T* row, uint32_t base, int at, int left, bool edge, int v, int k, Piece<T, kL>& out) {
+    if constexpr (kOn) {
+      if ((kFull || left >= kL) && !(kOdd && edge)) {
+        uint32_t w[kCopies * kBytes / 4];
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) load_shared<kBytes>(place(base, v, k, i), w + i * kBytes / 4);
+        if constexpr (kOdd) {
+          cut<kL / 2>(w, at_odd(row), out.w);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kL * (int)sizeof(T) / 4; ++i) out.w[i] = w[i];
+        }
+        return;
+      }
+    }
+    load_piece<kFull, kE>(row + at, left, edge, out);
+  }
+};
+// Rows that are on their way for each thread block of `threads` that shares a multiprocessor with `blocks - 1` others.
+constexpr int ring_stages(int thread_bytes, int threads, int blocks) {
+  const int room = thread_bytes ? kRingBytes / blocks / (thread_bytes * threads) : 0;
+  return room > 2 ? 2 : room;
+}
+
+// ---- scales -----------------------------------------------------------------------------
+// Largest magnitude; NaN where one is not a number, whose bits are above all others'.
+__device__ __forceinline__ float largest(float m, float x, float y) {
+  asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(x)), "f"(fabsf(y)));
+  return m;
+}
+// Maxima are compared as the upper 16 bits of magnitudes, rounded up, two at a time.  That loses nothing: 448 times a power of two has no lower bits, and
+// neither a carry into the exponent nor one across 1.75 changes the scale.  What is not finite, or rounds up to infinity, shows as 0x7F80 and more.
+constexpr uint32_t kNotFinite = 0x7F80u;
+__device__ __forceinline__ uint32_t upper(float m) { return (__float_as_uint(m) + 0xFFFFu) >> 16; }
+__device__ __forceinline__ bool not_finite2(uint32_t m) { return (m & 0xFFFFu) >= kNotFinite || m >= kNotFinite << 16; }
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Codes of kL numbers by reciprocals of their scales.  NaN gives NaN; infinities would give 448 and are replaced before.
+template <int kL>
+__device__ __forceinline__ void codes_of(const float (&y)[kL], const float* recip, int step, uint32_t (&c)[kL / 4]) {
+#pragma unroll
+  for (int k = 0; k < kL / 4; ++k)
+    c[k] = pack4(y[4 * k] * recip[4 * k * step], y[4 * k + 1] * recip[(4 * k + 1) * step], y[4 * k + 2] * recip[(4 * k + 2) * step], y[4 * k + 3] * recip[(4 * k + 3) * step]);
+}
+__device__ __forceinline__ float finite_or_nan(float y) { return y + (y - y); }
+template <bool kFull, int kL>
+__device__ __forceinline__ void store_codes(uint8_t* p, int left, const uint32_t (&c)[kL / 4]) {
+  if (kFull || left >= kL) {
+    store_bytes<kL>(p, c);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kL; ++i)
+      if (i < left) p[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
   }
 }
 __device__ __forceinline__ float warp_sum(float v) {
@@ -108,7 +266,6 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-constexpr int kGroup = 512;       // columns a warp holds at a time
 constexpr int kMostWarps = 16;
 constexpr int kMostCols = kGroup * kMostWarps * 4;
 
@@ -116,22 +273,27 @@ constexpr int kMostCols = kGroup * kMostWarps * 4;
 struct Layout {
   int warps, rows, v;
 };
-Layout row_layout(int64_t cols, int most_of_one) {
+// A row's own cost (its sum, addresses, barriers) is shared by two groups a warp where there are rows enough to fill the GPU all the same; few rows
+// have as many warps as they can use.  `most`: groups a warp takes in thread blocks of eight warps; wider rows have thread blocks of 16.
+Layout row_layout(int64_t rows, int64_t cols, int most) {
   const int groups = (int)ceil_div(cols, kGroup);
-  int v = groups <= most_of_one ? 1 : groups <= 32 ? 2 : 4, warps = 1;
-  while (warps * v < groups) warps *= 2;
+  int v = most == 4 && groups > 1 && rows * groups >= (int64_t)device_sm_count() * 64 ? 2 : 1;
+  while (v < most && 8 * v < groups) v *= 2;
+  if (8 * v < groups) v = groups <= 32 ? 2 : 4;
+  const int warps = (int)ceil_div(groups, v);
   return {warps, warps < 8 ? 8 / warps : 1, v};
 }
-constexpr int kNormOne = 16, kGradOne = 8;   // groups up to which a warp takes one
+constexpr int kNormMost = 4, kGradMost = 2;
 // Sum over the warps of this thread's row, the same in all of them.  `side` alternates, so that one barrier is enough.
 __device__ __forceinline__ float row_sum(float v, float (*part)[kMostWarps], int side, int warps, int warp) {
   v = warp_sum(v);
   if (warps == 1) return v;
   if (threadIdx.x % 32 == 0) part[side][warp] = v;
   __syncthreads();
-  const int first = warp & ~(warps - 1);
-  v = 0.f;
-  for (int i = 0; i < warps; ++i) v += part[side][first + i];
+  const int i = threadIdx.x % 16;   // both halves of the warp alike
+  v = i < warps ? part[side][warp / warps * warps + i] : 0.f;
+#pragma unroll
+  for (int d = 8; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
 
@@ -139,8 +301,8 @@ struct NormParams {
   const void *x, *r, *w;
   void *h, *y;
   int64_t ldx, ldr, ldh, ldy, ldq;
-  int rows, cols, w_bf16, warps, side_rows;
-  float eps;
+  int rows, cols, w_kind, warps, side_rows;
+  float eps, inv_cols;
   float* root;
   uint8_t* codes;
   uint32_t* scales;
@@ -152,127 +314,294 @@ struct Stored { using type = TR; };
 template <class TX>
 struct Stored<TX, None> { using type = TX; };
 
-template <class TX, class TR, bool kVec, int V>
-__global__ void __launch_bounds__(512, V == 4 ? 1 : 2) norm_rows_kernel(const __grid_constant__ NormParams p) {
-  constexpr bool kAdd = !std::is_same<TR, None>::value;
+// h of a lane's elements.  BF16 to BF16: the packed addition rounds the exact sum once, and so does rounding the FP32 sum, which is exact
+// wherever it lies near the middle of two BF16 numbers.
+template <int kL>
+__device__ __forceinline__ void add_piece(const Piece<__nv_bfloat16, kL>& x, Piece<__nv_bfloat16, kL>& h) {
+#pragma unroll
+  for (int j = 0; j < kL / 2; ++j) {
+    const __nv_bfloat162 v = __hadd2_rn(*reinterpret_cast<const __nv_bfloat162*>(&x.w[j]), *reinterpret_cast<const __nv_bfloat162*>(&h.w[j]));
+    h.w[j] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+template <class TX, int kL>
+__device__ __forceinline__ void add_piece(const Piece<TX, kL>& x, Piece<float, kL>& h) {
+#pragma unroll
+  for (int i = 0; i < kL; ++i) h.w[i] = __float_as_uint(value(x, i) + __uint_as_float(h.w[i]));
+}
+
+// How a kernel of V groups a warp is laid out: thread blocks that share a multiprocessor, rows on their way.
+template <class TX, class TR, int kL, int kE, int V, int kThreads, bool kWhole>
+struct NormShape {
+  static constexpr bool kAdd = !std::is_same<TR, None>::value;
   using TH = typename Stored<TX, TR>::type;
-  __shared__ float part[2][kMostWarps];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, in_row = warp % p.warps, step = p.warps * kGroup;
-  const int c_first = in_row * kGroup;
-  const int64_t row = (int64_t)blockIdx.x * p.side_rows + warp / p.warps;
-  const bool live = row < p.rows;
-  float h[V][4][4], sum = 0.f;
-  if (live) {
-    const TX* px = static_cast<const TX*>(p.x) + row * p.ldx;
-    const TH* pr = static_cast<const TH*>(p.r) + row * p.ldr;
+  static constexpr int kPieces = 16 / kL;
+  static constexpr int kBlocks = kThreads == 512 ? 1 : V == 4 || (V == 2 && sizeof(TH) == 4) ? 2 : 3;
+  template <bool kOn>
+  static constexpr int bytes() { return Stream<TX, kL, kE, V, kWhole, kOn>::kThread + (kAdd ? Stream<TH, kL, kE, V, kWhole, kOn>::kThread : 0); }
+  static constexpr int kStages = ring_stages(bytes<true>(), kThreads, kBlocks);
+  static constexpr bool kOn = kStages > 0;
+  static constexpr int kThreadBytes = bytes<kOn>();
+};
+
+// One row's share of a warp: h of group v and its sum of squares ...
+template <class S, class SX, class SR, bool kFull, class TX, class TH, int kL, int kE>
+__device__ __forceinline__ float norm_read(const TX* x, const TH* r, TH* out, uint32_t base, uint32_t r_at, int at, int left, bool edge, int v, Piece<TH, kL> (&h)[16 / kL], float sum) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c0 = c_first + v * step;
-      Quad<TX> x[4];
-      Quad<TH> r[4];
+  for (int k = 0; k < 16 / kL; ++k) {
+    const int c = at + k * 32 * kL, rest = left - k * 32 * kL;
+    if constexpr (S::kAdd) {
+      Piece<TX, kL> q;
+      SX::template take<kFull>(x, base, c, rest, edge, v, k, q);
+      SR::template take<kFull>(r, base + r_at, c, rest, edge, v, k, h[k]);
+      add_piece(q, h[k]);
+      store_piece<kFull, kE>(out + c, rest, h[k]);
+    } else {
+      SX::template take<kFull>(x, base, c, rest, edge, v, k, h[k]);
+    }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        load_quad<kVec>(px, c0 + q * kBlock, lane, p.cols, x[q]);
-        if constexpr (kAdd) load_quad<kVec>(pr, c0 + q * kBlock, lane, p.cols, r[q]);
-      }
+    for (int i = 0; i < kL; ++i) sum = fmaf(value(h[k], i), value(h[k], i), sum);
+  }
+  return sum;
+}
+// ... and y of it with its codes; the word of scales for all lanes.  y_out, codes: the lane's first column, or NULL.
+template <bool kFull, class TX, class TH, int kL, int kE>
+__device__ __forceinline__ uint32_t norm_write(const Piece<TH, kL> (&h)[16 / kL], float s, const void* weights, int w_kind, int c_lane, int left, TX* y_out, uint8_t* codes) {
+  constexpr int kPieces = 16 / kL;
+  float y[kPieces][kL], top[kPieces];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+  for (int k = 0; k < kPieces; ++k) {
+    const int at = k * 32 * kL;
+    float w[kL];
+    load_weights<kFull, kL>(weights, w_kind, c_lane + at, left - at, w);
+    top[k] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float f = quad_value(x[q], i);
-          if constexpr (kAdd) {
-            f += quad_value(r[q], i);
-            if constexpr (sizeof(TH) == 2) f = __bfloat162float(__float2bfloat16_rn(f));
-          }
-          h[v][q][i] = f;
-          sum = fmaf(f, f, sum);
-        }
-        if constexpr (kAdd) store_quad<kVec>(static_cast<TH*>(p.h) + row * p.ldh, c0 + q * kBlock, lane, p.cols, h[v][q]);
-      }
+    for (int i = 0; i < kL; ++i) y[k][i] = value(h[k], i) * s * w[i];
+#pragma unroll
+    for (int i = 0; i < kL; i += 2) top[k] = largest(top[k], y[k][i], y[k][i + 1]);
+    if (y_out) {
+      Piece<TX, kL> q;
+#pragma unroll
+      for (int i = 0; i < kL; i += 2) set2(q, i, y[k][i], y[k][i + 1]);
+      store_piece<kFull, kE>(y_out + at, left - at, q);
     }
   }
-  sum = row_sum(sum, part, 0, p.warps, warp);
-  if (!live) return;
-  const float s = __frsqrt_rn(__fdiv_rn(sum, (float)p.cols) + p.eps);
-  if (in_row == 0 && lane == 0 && p.root) p.root[row] = s;
-  if (!p.codes && !p.y) return;
+  if (!codes) return 0u;
+  uint32_t tops[kPieces / 2], c[kPieces];
+  bool odd = false;
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int c0 = c_first + v * step;
-    if (c0 >= p.cols) break;
-    uint32_t word = 0;
+  for (int k = 0; k < kPieces / 2; ++k) {
+    tops[k] = upper(top[2 * k]) | upper(top[2 * k + 1]) << 16;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float w[4], (&y)[4] = h[v][q];
-      load_weight<kVec>(p.w, p.w_bf16, c0 + q * kBlock, lane, p.cols, w);
+    for (int d = 1; d < 128 / kL; d *= 2) tops[k] = larger2(tops[k], __shfl_xor_sync(0xFFFFFFFFu, tops[k], d));
+    odd = odd || not_finite2(tops[k]);
+    c[2 * k] = scale_code(tops[k] << 16), c[2 * k + 1] = scale_code(tops[k] & 0xFFFF0000u);
+  }
+  const bool bad = __any_sync(0xFFFFFFFFu, odd);
+  if (bad) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = y[i] * s * w[i];
-      if (p.y) store_quad<kVec>(static_cast<TX*>(p.y) + row * p.ldy, c0 + q * kBlock, lane, p.cols, y);
-      if (!p.codes) continue;
-      const uint32_t top = max(max(finite_bits(y[0]), finite_bits(y[1])), max(finite_bits(y[2]), finite_bits(y[3])));
-      const uint32_t c = scale_code(__reduce_max_sync(0xFFFFFFFFu, top));
-      const float recip = scale_recip(c);
-      store_codes<kVec>(p.codes + row * p.ldq, c0 + q * kBlock, lane, p.cols, pack4(scaled(y[0], recip), scaled(y[1], recip), scaled(y[2], recip), scaled(y[3], recip)));
-      word |= c << (8 * q);
+    for (int k = 0; k < kPieces; ++k) {
+      uint32_t t = 0;
+#pragma unroll
+      for (int i = 0; i < kL; ++i) t = max(t, finite_bits(y[k][i])), y[k][i] = finite_or_nan(y[k][i]);
+#pragma unroll
+      for (int d = 1; d < 128 / kL; d *= 2) t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, d));
+      c[k] = scale_code(t);
     }
-    if (p.codes && lane == 0) p.scales[(int64_t)(c0 / kGroup) * p.rows + row] = word;
+  }
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const int at = k * 32 * kL;
+    const float recip = scale_recip(c[k]);
+    uint32_t q[kL / 4];
+    codes_of<kL>(y[k], &recip, 0, q);
+    if (kFull || left > at) store_codes<kFull, kL>(codes + at, left - at, q);
+  }
+  if constexpr (kL == 4) return c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+  const uint32_t mine = c[0] | c[1] << 16;   // lanes 0 .. 15 have blocks 0 and 2, the others blocks 1 and 3
+  return mine | __shfl_down_sync(0xFFFFFFFFu, mine, 16) << 8;
+}
+
+// kWhole: all groups are full.
+template <class TX, class TR, int kL, int kE, int V, int kThreads, bool kWhole>
+__global__ void __launch_bounds__(kThreads, NormShape<TX, TR, kL, kE, V, kThreads, kWhole>::kBlocks) norm_rows_kernel(const __grid_constant__ NormParams p) {
+  using S = NormShape<TX, TR, kL, kE, V, kThreads, kWhole>;
+  using TH = typename S::TH;
+  using SX = Stream<TX, kL, kE, V, kWhole, S::kOn>;
+  using SR = Stream<TH, kL, kE, V, kWhole, S::kOn>;
+  constexpr int kSlots = S::kOn ? S::kStages : 1;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float part[2][kMostWarps];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, in_row = warp % p.warps, step = p.warps * kGroup;
+  const int c_warp = in_row * kGroup, c_lane = c_warp + lane * kL, group_left = p.cols - c_warp;   // group v is v * step further
+  const uint32_t slot_bytes = S::kThreadBytes * blockDim.x, r_at = SX::kThread * blockDim.x, ring_at = smem_u32(ring);
+  int row = (int)blockIdx.x * p.side_rows + warp / p.warps, ahead = row;   // of the row at hand, and of the next to be fetched
+  const int stride = (int)gridDim.x * p.side_rows;
+  const int64_t x_step = stride * p.ldx, r_step = stride * p.ldr, h_step = stride * p.ldh, q_step = stride * p.ldq, y_step = stride * p.ldy;
+  const TX *x = static_cast<const TX*>(p.x) + row * p.ldx + c_lane, *x_ahead = x;
+  const TH *r = static_cast<const TH*>(p.r) + row * p.ldr + c_lane, *r_ahead = r;
+  TH* out = static_cast<TH*>(p.h) + row * p.ldh + c_lane;
+  TX* y = p.y ? static_cast<TX*>(p.y) + row * p.ldy + c_lane : nullptr;
+  uint8_t* codes = p.codes ? p.codes + row * p.ldq + c_lane : nullptr;
+  auto fetch = [&](int slot) {
+    if constexpr (S::kOn) {
+      if (ahead < p.rows) {
+        const bool edge = ahead == 0 || ahead == p.rows - 1;
+        SX::fetch(x_ahead, ring_at + slot * slot_bytes, step, lane, group_left, edge);
+        if constexpr (S::kAdd) SR::fetch(r_ahead, ring_at + slot * slot_bytes + r_at, step, lane, group_left, edge);
+      }
+      copy_commit();
+      ahead += stride, x_ahead += x_step;
+      if constexpr (S::kAdd) r_ahead += r_step;
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) fetch(k);
+  const int rounds = (p.rows - (int)blockIdx.x * p.side_rows + stride - 1) / stride;   // the same for all threads: they meet at barriers
+  int slot = 0;
+  for (int n = 0; n < rounds; ++n) {
+    const bool live = row < p.rows, edge = row == 0 || row == p.rows - 1;
+    Piece<TH, kL> h[V][16 / kL];
+    float sum = 0.f;
+    const uint32_t base = ring_at + slot * slot_bytes;
+    if constexpr (S::kOn) copy_wait<kSlots - 1>();
+    if (live) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int left = group_left - v * step;   // the same for all lanes
+        if (left <= 0) continue;
+        if (kWhole || left >= kGroup) sum = norm_read<S, SX, SR, true, TX, TH, kL, kE>(x, r, out, base, r_at, v * step, left - lane * kL, edge, v, h[v], sum);
+        else if constexpr (!kWhole) sum = norm_read<S, SX, SR, false, TX, TH, kL, kE>(x, r, out, base, r_at, v * step, left - lane * kL, edge, v, h[v], sum);
+      }
+    }
+    fetch(slot);
+    slot = slot + 1 == kSlots ? 0 : slot + 1;
+    sum = row_sum(sum, part, n & 1, p.warps, warp);
+    if (live) {
+      const float s = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
+      if (in_row == 0 && lane == 0 && p.root) p.root[row] = s;
+      if (codes || y) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int left = group_left - v * step, at = v * step;
+          if (left <= 0) break;
+          TX* y_at = y ? y + at : nullptr;
+          uint8_t* codes_at = codes ? codes + at : nullptr;
+          const uint32_t word = kWhole || left >= kGroup ? norm_write<true, TX, TH, kL, kE>(h[v], s, p.w, p.w_kind, c_lane + at, left - lane * kL, y_at, codes_at)
+                                               : norm_write<false, TX, TH, kL, kE>(h[v], s, p.w, p.w_kind, c_lane + at, left - lane * kL, y_at, codes_at);
+          if (codes && lane == 0) p.scales[(int64_t)((c_warp + at) / kGroup) * p.rows + row] = word;
+        }
+      }
+    }
+    row += stride, x += x_step;
+    if constexpr (S::kAdd) r += r_step, out += h_step;
+    if (y) y += y_step;
+    if (codes) codes += q_step;
   }
 }
 
-// Codes by columns: a 128 x 128 tile of h a thread block, warp w with rows w + 8 i.
-template <class TH, bool kVec>
-__global__ void __launch_bounds__(256, sizeof(TH) == 2 ? 4 : 2) norm_cols_kernel(const TH* H, int64_t ldh, const float* root, const void* W, int w_bf16, int rows, int cols,
-                                                                               uint8_t* Q, int64_t ldq, uint8_t* S) {
-  __shared__ uint32_t part[8][kBlock];
-  __shared__ float recips[kBlock], roots[kBlock];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
-  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c, r0 = tr * kBlock, c0 = tc * kBlock;
-  Quad<TH> h[16];
+// Codes by columns: a 128 x 128 tile of h a thread block.  128 / kL lanes hold a row's columns; a thread's rows are kRows apart.
+template <class TH, int kL, int kE, bool kFull>
+__device__ __forceinline__ void norm_cols_tile(const TH* H, int64_t ldh, const float* root, const void* W, int w_kind, int rows, int cols, uint8_t* Q, int64_t ldq, uint8_t* S,
+                                               uint32_t (*part)[kBlock / 2], float* recips, float* roots, int tr, int tc, int tiles_r) {
+  constexpr int kLanes = kBlock / kL, kRows = 256 / kLanes, kN = kBlock / kRows;   // lanes a row, rows side by side, rows a thread
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, c_in = threadIdx.x % kLanes * kL, r_in = threadIdx.x / kLanes;
+  const int r0 = tr * kBlock, c = tc * kBlock + c_in, left = cols - c;
+  Piece<TH, kL> h[kN];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) load_quad<kVec>(H + (int64_t)(r0 + warp + 8 * i) * ldh, c0, lane, r0 + warp + 8 * i < rows ? cols : 0, h[i]);
-  if (threadIdx.x < kBlock) roots[threadIdx.x] = r0 + (int)threadIdx.x < rows ? root[r0 + threadIdx.x] : 0.f;
-  float w[4];
-  load_weight<kVec>(W, w_bf16, c0, lane, cols, w);
-  __syncthreads();
-  uint32_t top[4] = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float s = roots[warp + 8 * i];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) top[k] = max(top[k], finite_bits(quad_value(h[i], k) * s * w[k]));
+  for (int i = 0; i < kN; ++i) {
+    const TH* at = H + (int64_t)(r0 + r_in + kRows * i) * ldh + c;
+    const int r = r0 + r_in + kRows * i;
+    load_piece<kFull, kE>(at, kFull ? kL : r < rows ? left : 0, r == 0 || r == rows - 1, h[i]);
   }
+  if (threadIdx.x < kBlock) roots[threadIdx.x] = kFull || r0 + (int)threadIdx.x < rows ? root[r0 + threadIdx.x] : 0.f;
+  float w[kL];
+  load_weights<kFull, kL>(W, w_kind, c, left, w);
+  __syncthreads();
+  float top[kL] = {};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[warp][quad_col<kVec>(0, lane, k)] = top[k];
+  for (int i = 0; i < kN; i += 2) {
+    const float s = roots[r_in + kRows * i], t = roots[r_in + kRows * (i + 1)];
+#pragma unroll
+    for (int j = 0; j < kL; ++j) top[j] = largest(top[j], value(h[i], j) * s * w[j], value(h[i + 1], j) * t * w[j]);
+  }
+  uint32_t tops[kL / 2], worst = 0;
+#pragma unroll
+  for (int j = 0; j < kL / 2; ++j) {
+    tops[j] = upper(top[2 * j]) | upper(top[2 * j + 1]) << 16;
+    worst = larger2(worst, tops[j]);
+  }
+  const bool bad = __syncthreads_or(not_finite2(worst));
+  if (bad) {   // again without them; magnitudes that round up to infinity count as the largest below it, which has the same scale
+#pragma unroll
+    for (int j = 0; j < kL / 2; ++j) {
+      uint32_t a = 0, b = 0;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const float s = roots[r_in + kRows * i];
+        a = max(a, finite_bits(value(h[i], 2 * j) * s * w[2 * j])), b = max(b, finite_bits(value(h[i], 2 * j + 1) * s * w[2 * j + 1]));
+      }
+      tops[j] = min(upper(__uint_as_float(a)), kNotFinite - 1) | min(upper(__uint_as_float(b)), kNotFinite - 1) << 16;
+    }
+  }
+  if constexpr (kLanes == 16) {
+#pragma unroll
+    for (int j = 0; j < kL / 2; ++j) tops[j] = larger2(tops[j], __shfl_xor_sync(0xFFFFFFFFu, tops[j], 16));
+  }
+  if (lane < kLanes) store_bytes<2 * kL>(&part[warp][c_in / 2], tops);
   __syncthreads();
   if (threadIdx.x < kBlock) {
-    uint32_t t = part[0][threadIdx.x];
+    uint32_t t = part[0][threadIdx.x / 2];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) t = max(t, part[i][threadIdx.x]);
-    const uint32_t c = scale_code(t);
-    recips[threadIdx.x] = scale_recip(c);
-    const int col = c0 + (int)threadIdx.x;
+    for (int i = 1; i < 8; ++i) t = larger2(t, part[i][threadIdx.x / 2]);
+    const uint32_t code = scale_code(threadIdx.x % 2 ? t & 0xFFFF0000u : t << 16);
+    recips[threadIdx.x] = scale_recip(code);
+    const int col = tc * kBlock + (int)threadIdx.x;
     if (col < cols) {
       uint8_t* s = S + ((int64_t)(tr / 4) * cols + col) * 4;
-      s[tr % 4] = (uint8_t)c;
+      s[tr % 4] = (uint8_t)code;
       if (tr + 1 == tiles_r)
         for (int b = tr % 4 + 1; b < 4; ++b) s[b] = 127;
     }
   }
   __syncthreads();
-  float recip[4];
+  float recip[kL];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) recip[k] = recips[quad_col<kVec>(0, lane, k)];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + warp + 8 * i;
-    if (r >= rows) break;
-    const float s = roots[warp + 8 * i];
-    float y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = scaled(quad_value(h[i], k) * s * w[k], recip[k]);
-    store_codes<kVec>(Q + (int64_t)r * ldq, c0, lane, cols, pack4(y[0], y[1], y[2], y[3]));
+  for (int j = 0; j < kL; j += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(&recips[c_in + j]);
+    recip[j] = f.x, recip[j + 1] = f.y, recip[j + 2] = f.z, recip[j + 3] = f.w;
   }
+  auto write = [&](auto odd) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int r = r0 + r_in + kRows * i;
+      const float s = roots[r_in + kRows * i];
+      float y[kL];
+#pragma unroll
+      for (int j = 0; j < kL; ++j) {
+        y[j] = value(h[i], j) * s * w[j];
+        if constexpr (decltype(odd)::value) y[j] = finite_or_nan(y[j]);
+      }
+      uint32_t q[kL / 4];
+      codes_of<kL>(y, recip, 1, q);
+      if (kFull || (r < rows && left > 0)) store_codes<kFull, kL>(Q + (int64_t)r * ldq + c, left, q);
+    }
+  };
+  if (bad) write(std::true_type{}); else write(std::false_type{});
+}
+template <class TH, int kL, int kE>
+__global__ void __launch_bounds__(256, sizeof(TH) == 2 ? 3 : 2) norm_cols_kernel(const TH* H, int64_t ldh, const float* root, const void* W, int w_kind, int rows, int cols,
+                                                                               uint8_t* Q, int64_t ldq, uint8_t* S) {
+  __shared__ __align__(16) uint32_t part[8][kBlock / 2];
+  __shared__ __align__(16) float recips[kBlock];
+  __shared__ float roots[kBlock];
+  const int tiles_c = (cols + kBlock - 1) / kBlock, tiles_r = (rows + kBlock - 1) / kBlock;
+  const int tile = (int)(gridDim.x - 1 - blockIdx.x);   // from the end, which the rows' kernel has just written: it is still in L2
+  const int tr = tile / tiles_c, tc = tile % tiles_c;
+  if (tr * kBlock + kBlock <= rows && tc * kBlock + kBlock <= cols)
+    norm_cols_tile<TH, kL, kE, true>(H, ldh, root, W, w_kind, rows, cols, Q, ldq, S, part, recips, roots, tr, tc, tiles_r);
+  else
+    norm_cols_tile<TH, kL, kE, false>(H, ldh, root, W, w_kind, rows, cols, Q, ldq, S, part, recips, roots, tr, tc, tiles_r);
 }
 
 // ---- gradients --------------------------------------------------------------------------
@@ -281,95 +610,148 @@ struct GradParams {
   void* dx;
   const float* root;
   int64_t lddy, ldh, lddh, lddx;
-  int rows, cols, w_bf16, warps, side_rows;
+  int rows, cols, w_kind, warps, side_rows;
+  float inv_cols;
   float* parts;   // [grid x side_rows][cols], or NULL
 };
 
-// Rows as in the forward pass.  Each thread adds up its columns' share of dw over the rows it sees; dw_kernel adds the thread blocks' sums.
-template <class TD, class TH, bool kVec, int V>
-__global__ void __launch_bounds__(V == 1 ? 256 : 512, V == 1 ? 3 : 1) norm_backward_kernel(const __grid_constant__ GradParams p) {
+template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
+struct GradShape {
+  static constexpr int kBlocks = kThreads == 512 ? 1 : V == 1 && sizeof(TD) + sizeof(TH) == 4 ? 3 : 2;
+  template <bool kOn>
+  static constexpr int bytes() { return Stream<TD, kL, kE, V, kWhole, kOn>::kThread + 2 * Stream<TH, kL, kE, V, kWhole, kOn>::kThread; }
+  static constexpr int kStages = ring_stages(bytes<true>(), kThreads, kBlocks);
+  static constexpr bool kOn = kStages > 0;
+  static constexpr int kThreadBytes = bytes<kOn>();
+};
+
+// Rows as in the forward pass; what is needed again after the sum is read again from shared memory.  Each thread adds up its
+// columns' share of dw over the rows it sees; norm_dw_kernel adds the thread blocks' sums.
+template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
+__global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThreads, kWhole>::kBlocks) norm_backward_kernel(const __grid_constant__ GradParams p) {
+  using S = GradShape<TD, TH, kL, kE, V, kThreads, kWhole>;
+  using SD = Stream<TD, kL, kE, V, kWhole, S::kOn>;
+  using SH = Stream<TH, kL, kE, V, kWhole, S::kOn>;
+  constexpr int kSlots = S::kOn ? S::kStages : 1, kPieces = 16 / kL;
+  extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float part[2][kMostWarps];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, in_row = warp % p.warps, step = p.warps * kGroup;
-  const int c_first = in_row * kGroup;
-  const int64_t stride = (int64_t)gridDim.x * p.side_rows, first = (int64_t)blockIdx.x * p.side_rows + warp / p.warps;
-  Quad<TD> d[V][4];
-  Quad<TH> h[V][4], e[4];   // e: what is added, fetched early where it has room
-  float dw[V][4][4];
+  const int c_warp = in_row * kGroup, c_lane = c_warp + lane * kL, group_left = p.cols - c_warp;
+  const int first = (int)blockIdx.x * p.side_rows + warp / p.warps, stride = (int)gridDim.x * p.side_rows;
+  const uint32_t slot_bytes = S::kThreadBytes * blockDim.x, h_at = SD::kThread * blockDim.x, e_at = h_at + SH::kThread * blockDim.x, ring_at = smem_u32(ring);
+  int row = first, ahead = first;   // the row at hand, and the next to be fetched
+  const int64_t d_step = stride * p.lddy, h_step = stride * p.ldh, e_step = stride * p.lddh, o_step = stride * p.lddx;
+  const TD *pd = static_cast<const TD*>(p.dy) + row * p.lddy + c_lane, *d_ahead = pd;
+  const TH *ph = static_cast<const TH*>(p.h) + row * p.ldh + c_lane, *h_ahead = ph, *pe = p.dh ? static_cast<const TH*>(p.dh) + row * p.lddh + c_lane : nullptr, *e_ahead = pe;
+  TH* po = static_cast<TH*>(p.dx) + row * p.lddx + c_lane;
+  auto fetch = [&](int slot) {
+    if constexpr (S::kOn) {
+      if (ahead < p.rows) {
+        const bool edge = ahead == 0 || ahead == p.rows - 1;
+        SD::fetch(d_ahead, ring_at + slot * slot_bytes, step, lane, group_left, edge);
+        SH::fetch(h_ahead, ring_at + slot * slot_bytes + h_at, step, lane, group_left, edge);
+        if (pe) SH::fetch(e_ahead, ring_at + slot * slot_bytes + e_at, step, lane, group_left, edge);
+      }
+      copy_commit();
+      ahead += stride, d_ahead += d_step, h_ahead += h_step;
+      if (pe) e_ahead += e_step;
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) fetch(k);
+  float dw[V][kPieces][kL];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int k = 0; k < kPieces; ++k)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) dw[v][q][i] = 0.f;
-  const int64_t rounds = (p.rows - (int64_t)blockIdx.x * p.side_rows + stride - 1) / stride;
-  int64_t row = first;
-  for (int64_t n = 0; n < rounds; ++n, row += stride) {
-    const bool live = row < p.rows;
-    const float s = live ? p.root[row] : 0.f;
+      for (int i = 0; i < kL; ++i) dw[v][k][i] = 0.f;
+  const int rounds = (p.rows - (int)blockIdx.x * p.side_rows + stride - 1) / stride;   // the same for all threads: they meet at barriers
+  int slot = 0;
+  float s = row < p.rows ? p.root[row] : 0.f;
+  for (int n = 0; n < rounds; ++n) {
+    const bool live = row < p.rows, edge = row == 0 || row == p.rows - 1;
+    const float s_next = row + stride < p.rows ? p.root[row + stride] : 0.f;
+    const uint32_t base = ring_at + slot * slot_bytes;
     float sum = 0.f;
+    // Group v of the row, before the sum is known (adds to dw and to the sum) and after (writes dx).
+    auto look = [&](auto full, int v, int left) {
+      constexpr bool kFull = decltype(full)::value;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
+        Piece<TD, kL> d;
+        Piece<TH, kL> h;
+        SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
+        SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
+        float w[kL];
+        load_weights<kFull, kL>(p.w, p.w_kind, c_lane + at, rest, w);
+#pragma unroll
+        for (int i = 0; i < kL; ++i) {
+          const float hn = value(h, i) * s;
+          dw[v][k][i] = fmaf(value(d, i), hn, dw[v][k][i]);
+          sum = fmaf(value(d, i) * w[i], hn, sum);
+        }
+      }
+    };
+    auto write = [&](auto full, int v, int left, float minus_mean) {
+      constexpr bool kFull = decltype(full)::value;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
+        Piece<TD, kL> d;
+        Piece<TH, kL> h, e = {}, out;
+        SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
+        SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
+        if (pe) SH::template take<kFull>(pe, base + e_at, at, rest, edge, v, k, e);
+        float w[kL], dx[kL];
+        load_weights<kFull, kL>(p.w, p.w_kind, c_lane + at, rest, w);
+#pragma unroll
+        for (int i = 0; i < kL; ++i) dx[i] = fmaf(s, fmaf(value(h, i) * s, minus_mean, value(d, i) * w[i]), value(e, i));
+#pragma unroll
+        for (int i = 0; i < kL; i += 2) set2(out, i, dx[i], dx[i + 1]);
+        store_piece<kFull, kE>(po + at, rest, out);
+      }
+    };
+    if constexpr (S::kOn) copy_wait<kSlots - 1>();
     if (live) {
-      const TD* pd = static_cast<const TD*>(p.dy) + row * p.lddy;
-      const TH* ph = static_cast<const TH*>(p.h) + row * p.ldh;
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          load_quad<kVec>(pd, c_first + v * step + q * kBlock, lane, p.cols, d[v][q]);
-          load_quad<kVec>(ph, c_first + v * step + q * kBlock, lane, p.cols, h[v][q]);
-        }
-      if constexpr (V == 1) {
-        if (p.dh) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) load_quad<kVec>(static_cast<const TH*>(p.dh) + row * p.lddh, c_first + q * kBlock, lane, p.cols, e[q]);
-        }
+      for (int v = 0; v < V; ++v) {
+        const int left = group_left - v * step;
+        if (left <= 0) continue;
+        if constexpr (kWhole) look(std::true_type{}, v, left - lane * kL);
+        else if (left >= kGroup) look(std::true_type{}, v, left - lane * kL);
+        else look(std::false_type{}, v, left - lane * kL);
       }
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float w[4];
-          load_weight<kVec>(p.w, p.w_bf16, c_first + v * step + q * kBlock, lane, p.cols, w);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float dy = quad_value(d[v][q], i), hn = quad_value(h[v][q], i) * s;
-            dw[v][q][i] = fmaf(dy, hn, dw[v][q][i]);
-            sum = fmaf(dy * w[i], hn, sum);
-          }
-        }
     }
-    sum = row_sum(sum, part, (int)(n & 1), p.warps, warp);
-    if (!live) continue;
-    const float mean = __fdiv_rn(sum, (float)p.cols);
+    sum = row_sum(sum, part, n & 1, p.warps, warp);
+    if (live) {
+      const float minus_mean = -sum * p.inv_cols;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c0 = c_first + v * step + q * kBlock;
-        if (c0 >= p.cols) continue;
-        float out[4], w[4];
-        load_weight<kVec>(p.w, p.w_bf16, c0, lane, p.cols, w);
-        if constexpr (V > 1) {
-          if (p.dh) load_quad<kVec>(static_cast<const TH*>(p.dh) + row * p.lddh, c0, lane, p.cols, e[q]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float g = quad_value(d[v][q], i) * w[i], hn = quad_value(h[v][q], i) * s;
-          out[i] = s * fmaf(-hn, mean, g);
-          if (p.dh) out[i] += quad_value(e[q], i);
-        }
-        store_quad<kVec>(static_cast<TH*>(p.dx) + row * p.lddx, c0, lane, p.cols, out);
+      for (int v = 0; v < V; ++v) {
+        const int left = group_left - v * step;
+        if (left <= 0) continue;
+        if constexpr (kWhole) write(std::true_type{}, v, left - lane * kL, minus_mean);
+        else if (left >= kGroup) write(std::true_type{}, v, left - lane * kL, minus_mean);
+        else write(std::false_type{}, v, left - lane * kL, minus_mean);
       }
+    }
+    fetch(slot);
+    slot = slot + 1 == kSlots ? 0 : slot + 1;
+    s = s_next;
+    row += stride, pd += d_step, ph += h_step, po += o_step;
+    if (pe) pe += e_step;
   }
   if (!p.parts) return;
-  float* mine = p.parts + first * p.cols;   // the first row that this warp saw names its sums
+  float* mine = p.parts + (int64_t)first * p.cols;   // the first row that this warp saw names its sums
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int k = 0; k < kPieces; ++k)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = quad_col<kVec>(c_first + v * step + q * kBlock, lane, i);
-        if (c < p.cols) mine[c] = dw[v][q][i];
+      for (int i = 0; i < kL; ++i) {
+        const int c = c_lane + v * step + k * 32 * kL + i;
+        if (c < p.cols) mine[c] = dw[v][k][i];
       }
 }
 
@@ -392,48 +774,90 @@ __global__ void __launch_bounds__(1024) norm_dw_kernel(const float* parts, int c
 bool type_ok(int t) { return t == OZK_F32 || t == OZK_BF16; }
 int type_size(int t) { return t == OZK_F32 ? 4 : 2; }
 bool on(const void* p, int size) { return p && (reinterpret_cast<uintptr_t>(p) & (size - 1)) == 0; }
-// Four elements at a time.
-bool quads(const void* p, int64_t ld, int size) { return (reinterpret_cast<uintptr_t>(p) & (4 * size - 1)) == 0 && ld % 4 == 0; }
+// How many elements a row's place and stride let be read together: 16 bytes at most; 8, 4 or 1.
+int together(const void* p, int64_t ld, int size) {
+  for (int n = size == 2 ? 8 : 4; n > 2; n /= 2)
+    if ((reinterpret_cast<uintptr_t>(p) & (n * size - 1)) == 0 && ld % n == 0) return n;
+  return 1;
+}
+int least(int a, int b) { return a < b ? a : b; }
+// Lanes take eight columns where all is BF16 and aligned; FP32 comes in 16-byte accesses of four.
+template <class TX, class TR>
+constexpr bool kAllBf16 = sizeof(TX) == 2 && !std::is_same<TR, float>::value;
 
-// Thread blocks of the backward pass: what runs at once, so that there are few partial sums of dw.
-int grad_grid(int64_t rows, const Layout& l) {
-  const int64_t need = ceil_div(rows, l.rows), room = (int64_t)device_sm_count() * (l.v == 1 ? 3 : l.warps <= 8 ? 2 : 1);
+int weight_kind(const void* w, int type) { return (type == OZK_BF16 ? kWeightBf16 : 0) | (aligned16(w) ? 0 : kWeightLoose); }
+
+// Thread blocks of a persistent kernel: what runs at once, or what there is to do.
+// `blocks` of them share a multiprocessor where they have 256 or 512 threads, more where they have fewer.
+int grid_of(int64_t rows, const Layout& l, int blocks) {
+  const int warps = l.warps * l.rows;
+  const int64_t need = ceil_div(rows, l.rows), room = (int64_t)device_sm_count() * (warps <= 8 ? blocks * 8 / warps : blocks);
   return (int)(need < room ? need : room);
 }
 
-template <class TX, class TR, bool kVec>
-void launch_norm_rows(const NormParams& p, const Layout& l, cudaStream_t st) {
-  const unsigned grid = (unsigned)ceil_div(p.rows, l.rows), threads = (unsigned)(32 * l.warps * l.rows);
-  switch (l.v) {
-    case 1: norm_rows_kernel<TX, TR, kVec, 1><<<grid, threads, 0, st>>>(p); break;
-    case 2: norm_rows_kernel<TX, TR, kVec, 2><<<grid, threads, 0, st>>>(p); break;
-    default: norm_rows_kernel<TX, TR, kVec, 4><<<grid, threads, 0, st>>>(p); break;
-  }
+template <class TX, class TR, int kL, int kE, int V, int kThreads, bool kWhole>
+bool launch_norm_rows_as(const NormParams& p, const Layout& l, cudaStream_t st) {
+  using S = NormShape<TX, TR, kL, kE, V, kThreads, kWhole>;
+  static std::atomic<bool> done[kMaxDevices];
+  auto kernel = norm_rows_kernel<TX, TR, kL, kE, V, kThreads, kWhole>;
+  if (!raise_smem(kernel, (size_t)S::kStages * S::kThreadBytes * kThreads, done)) return false;
+  const unsigned threads = (unsigned)(32 * l.warps * l.rows);
+  kernel<<<(unsigned)grid_of(p.rows, l, S::kBlocks), threads, (size_t)S::kStages * S::kThreadBytes * threads, st>>>(p);
+  return cudaGetLastError() == cudaSuccess;
+}
+template <class TX, class TR, int kL, int kE, bool kWhole>
+bool launch_norm_rows(const NormParams& p, const Layout& l, cudaStream_t st) {
+  if (l.warps > 8) return launch_norm_rows_as<TX, TR, kL, kE, 4, 512, kWhole>(p, l, st);
+  return l.v == 1 ? launch_norm_rows_as<TX, TR, kL, kE, 1, 256, kWhole>(p, l, st)
+                  : l.v == 2 ? launch_norm_rows_as<TX, TR, kL, kE, 2, 256, kWhole>(p, l, st) : launch_norm_rows_as<TX, TR, kL, kE, 4, 256, kWhole>(p, l, st);
 }
 template <class TX, class TR>
-void launch_norm_rows(bool vec, const NormParams& p, const Layout& l, cudaStream_t st) {
-  if (vec) launch_norm_rows<TX, TR, true>(p, l, st); else launch_norm_rows<TX, TR, false>(p, l, st);
+bool launch_norm_rows(int e, const NormParams& p, const Layout& l, cudaStream_t st) {
+  if constexpr (kAllBf16<TX, TR>) {
+    if (e == 8) return p.cols % kGroup == 0 ? launch_norm_rows<TX, TR, 8, 8, true>(p, l, st) : launch_norm_rows<TX, TR, 8, 8, false>(p, l, st);
+  } else {
+    if (e >= 4 && p.cols % kGroup == 0) return launch_norm_rows<TX, TR, 4, 4, true>(p, l, st);
+  }
+  return e >= 4 ? launch_norm_rows<TX, TR, 4, 4, false>(p, l, st) : launch_norm_rows<TX, TR, 4, 1, false>(p, l, st);
+}
+template <class TH, int kL, int kE>
+void launch_norm_cols(const void* h, int64_t ldh, const NormParams& p, uint8_t* q, int64_t ldq, uint8_t* s, cudaStream_t st) {
+  const unsigned tiles = (unsigned)(ceil_div(p.rows, kBlock) * ceil_div(p.cols, kBlock));
+  norm_cols_kernel<TH, kL, kE><<<tiles, 256, 0, st>>>(static_cast<const TH*>(h), ldh, p.root, p.w, p.w_kind, p.rows, p.cols, q, ldq, s);
 }
 template <class TH>
-void launch_norm_cols(bool vec, const void* h, int64_t ldh, const NormParams& p, uint8_t* q, int64_t ldq, uint8_t* s, cudaStream_t st) {
-  const unsigned tiles = (unsigned)(ceil_div(p.rows, kBlock) * ceil_div(p.cols, kBlock));
-  if (vec)
-    norm_cols_kernel<TH, true><<<tiles, 256, 0, st>>>(static_cast<const TH*>(h), ldh, p.root, p.w, p.w_bf16, p.rows, p.cols, q, ldq, s);
-  else
-    norm_cols_kernel<TH, false><<<tiles, 256, 0, st>>>(static_cast<const TH*>(h), ldh, p.root, p.w, p.w_bf16, p.rows, p.cols, q, ldq, s);
-}
-template <class TD, class TH, bool kVec>
-void launch_backward(const GradParams& p, const Layout& l, int grid, cudaStream_t st) {
-  const unsigned threads = (unsigned)(32 * l.warps * l.rows);
-  switch (l.v) {
-    case 1: norm_backward_kernel<TD, TH, kVec, 1><<<(unsigned)grid, threads, 0, st>>>(p); break;
-    case 2: norm_backward_kernel<TD, TH, kVec, 2><<<(unsigned)grid, threads, 0, st>>>(p); break;
-    default: norm_backward_kernel<TD, TH, kVec, 4><<<(unsigned)grid, threads, 0, st>>>(p); break;
+void launch_norm_cols(int e, const void* h, int64_t ldh, const NormParams& p, uint8_t* q, int64_t ldq, uint8_t* s, cudaStream_t st) {
+  if constexpr (sizeof(TH) == 2) {
+    if (e == 8) return launch_norm_cols<TH, 8, 8>(h, ldh, p, q, ldq, s, st);
   }
+  if (e >= 4) launch_norm_cols<TH, 4, 4>(h, ldh, p, q, ldq, s, st); else launch_norm_cols<TH, 4, 1>(h, ldh, p, q, ldq, s, st);
+}
+constexpr int kGradBlocks = 3;   // a multiprocessor, at most: what the scratch of the partial sums is for
+template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
+bool launch_backward_as(const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
+  using S = GradShape<TD, TH, kL, kE, V, kThreads, kWhole>;
+  static_assert(S::kBlocks <= kGradBlocks, "room for partial sums");
+  static std::atomic<bool> done[kMaxDevices];
+  auto kernel = norm_backward_kernel<TD, TH, kL, kE, V, kThreads, kWhole>;
+  if (!raise_smem(kernel, (size_t)S::kStages * S::kThreadBytes * kThreads, done)) return false;
+  const unsigned threads = (unsigned)(32 * l.warps * l.rows);
+  *grid = grid_of(p.rows, l, S::kBlocks);
+  kernel<<<(unsigned)*grid, threads, (size_t)S::kStages * S::kThreadBytes * threads, st>>>(p);
+  return cudaGetLastError() == cudaSuccess;
+}
+template <class TD, class TH, int kL, int kE, bool kWhole>
+bool launch_backward(const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
+  if (l.warps <= 8) return l.v == 1 ? launch_backward_as<TD, TH, kL, kE, 1, 256, kWhole>(p, l, grid, st) : launch_backward_as<TD, TH, kL, kE, 2, 256, kWhole>(p, l, grid, st);
+  return l.v == 2 ? launch_backward_as<TD, TH, kL, kE, 2, 512, kWhole>(p, l, grid, st) : launch_backward_as<TD, TH, kL, kE, 4, 512, kWhole>(p, l, grid, st);
 }
 template <class TD, class TH>
-void launch_backward(bool vec, const GradParams& p, const Layout& l, int grid, cudaStream_t st) {
-  if (vec) launch_backward<TD, TH, true>(p, l, grid, st); else launch_backward<TD, TH, false>(p, l, grid, st);
+bool launch_backward(int e, const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
+  if constexpr (kAllBf16<TD, TH>) {
+    if (e == 8) return p.cols % kGroup == 0 ? launch_backward<TD, TH, 8, 8, true>(p, l, grid, st) : launch_backward<TD, TH, 8, 8, false>(p, l, grid, st);
+  } else {
+    if (e >= 4 && p.cols % kGroup == 0) return launch_backward<TD, TH, 4, 4, true>(p, l, grid, st);
+  }
+  return e >= 4 ? launch_backward<TD, TH, 4, 4, false>(p, l, grid, st) : launch_backward<TD, TH, 4, 1, false>(p, l, grid, st);
 }
 
 }  // namespace
@@ -448,7 +872,7 @@ ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, i
                         uint8_t* row_scales, uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales, void* stream) {
   if (rows < 0 || cols < 0 || !type_ok(x_type) || !type_ok(w_type) || ldx < cols || !(eps >= 0.0)) return OZK_ERR_INVALID_ARG;
   if (R && (!type_ok(r_type) || ldr < cols || ldh < cols)) return OZK_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 1024 || cols > kMostCols || (R && r_type != x_type && r_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX - 65536 || cols > kMostCols || (R && r_type != x_type && r_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
   const bool by_rows = row_codes || row_scales, by_cols = col_codes || col_scales;
   if (rows == 0 || cols == 0) return OZK_OK;
   const int h_type = R ? r_type : x_type;
@@ -459,28 +883,28 @@ ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, i
   if (by_cols && (!col_codes || !col_scales || !aligned16(col_codes) || col_ld % 16 || col_ld < cols)) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const Layout l = row_layout(cols, kNormOne);
+  const Layout l = row_layout(rows, cols, kNormMost);
   const int xs = type_size(x_type), hs = type_size(h_type);
   NormParams p = {};
   p.x = X, p.r = R, p.w = weight, p.h = H, p.y = Y;
   p.ldx = ldx, p.ldr = ldr, p.ldh = ldh, p.ldy = ldy, p.ldq = row_ld;
-  p.rows = (int)rows, p.cols = (int)cols, p.w_bf16 = w_type == OZK_BF16, p.warps = l.warps, p.side_rows = l.rows;
-  p.eps = (float)eps, p.root = root, p.codes = row_codes, p.scales = reinterpret_cast<uint32_t*>(row_scales);
-  const bool vec = quads(X, ldx, xs) && (!R || (quads(R, ldr, hs) && quads(H, ldh, hs))) && (!Y || quads(Y, ldy, xs)) && quads(weight, 0, type_size(w_type));
-  if (x_type == OZK_BF16) {
-    if (!R) launch_norm_rows<__nv_bfloat16, None>(vec, p, l, st);
-    else if (r_type == OZK_BF16) launch_norm_rows<__nv_bfloat16, __nv_bfloat16>(vec, p, l, st);
-    else launch_norm_rows<__nv_bfloat16, float>(vec, p, l, st);
-  } else {
-    if (!R) launch_norm_rows<float, None>(vec, p, l, st);
-    else launch_norm_rows<float, float>(vec, p, l, st);
-  }
-  if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
+  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(weight, w_type), p.warps = l.warps, p.side_rows = l.rows;
+  p.eps = (float)eps, p.inv_cols = 1.f / (float)cols, p.root = root, p.codes = row_codes, p.scales = reinterpret_cast<uint32_t*>(row_scales);
+  int vec = together(X, ldx, xs);
+  if (R) vec = least(vec, least(together(R, ldr, hs), together(H, ldh, hs)));
+  if (Y) vec = least(vec, together(Y, ldy, xs));
+  bool ok;
+  if (x_type == OZK_BF16)
+    ok = !R ? launch_norm_rows<__nv_bfloat16, None>(vec, p, l, st)
+            : r_type == OZK_BF16 ? launch_norm_rows<__nv_bfloat16, __nv_bfloat16>(vec, p, l, st) : launch_norm_rows<__nv_bfloat16, float>(vec, p, l, st);
+  else
+    ok = !R ? launch_norm_rows<float, None>(vec, p, l, st) : launch_norm_rows<float, float>(vec, p, l, st);
+  if (!ok) return OZK_ERR_CUDA;
   if (by_cols) {
     const void* h = R ? H : X;
     const int64_t ld = R ? ldh : ldx;
-    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(quads(h, ld, 2) && quads(weight, 0, type_size(w_type)), h, ld, p, col_codes, col_ld, col_scales, st);
-    else launch_norm_cols<float>(quads(h, ld, 4) && quads(weight, 0, type_size(w_type)), h, ld, p, col_codes, col_ld, col_scales, st);
+    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(together(h, ld, 2), h, ld, p, col_codes, col_ld, col_scales, st);
+    else launch_norm_cols<float>(together(h, ld, 4), h, ld, p, col_codes, col_ld, col_scales, st);
     if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
   }
   return OZK_OK;
@@ -488,8 +912,8 @@ ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, i
 
 size_t ozk_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || cols > kMostCols) return 0;
-  const Layout l = row_layout(cols, kGradOne);
-  return (size_t)grad_grid(rows, l) * l.rows * (size_t)cols * 4;
+  const Layout l = row_layout(rows, cols, kGradMost);
+  return (size_t)grid_of(rows, l, kGradBlocks) * l.rows * (size_t)cols * 4;
 }
 
 ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int dy_type, int64_t lddy, const void* H, int h_type, int64_t ldh, const float* root,
@@ -497,7 +921,7 @@ ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int
                                  size_t scratch_bytes, void* stream) {
   if (rows < 0 || cols < 0 || !type_ok(dy_type) || !type_ok(h_type) || !type_ok(w_type) || lddy < cols || ldh < cols || lddx < cols) return OZK_ERR_INVALID_ARG;
   if (dH && lddh < cols) return OZK_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 1024 || cols > kMostCols) return OZK_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX - 65536 || cols > kMostCols) return OZK_ERR_UNSUPPORTED;
   if (cols == 0) return OZK_OK;
   if (dweight && !on(dweight, 4)) return OZK_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -505,23 +929,23 @@ ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int
   const int ds = type_size(dy_type), hs = type_size(h_type);
   if (!on(dY, ds) || !on(H, hs) || !on(root, 4) || !on(weight, type_size(w_type)) || !on(dX, hs) || (dH && !on(dH, hs))) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
-  const Layout l = row_layout(cols, kGradOne);
-  const int grid = grad_grid(rows, l);
+  const Layout l = row_layout(rows, cols, kGradMost);
   if (dweight && (!on(scratch, 16) || scratch_bytes < ozk_rms_norm_backward_scratch_bytes(rows, cols))) return OZK_ERR_WORKSPACE;
   GradParams p = {};
   p.dy = dY, p.h = H, p.dh = dH, p.w = weight, p.dx = dX, p.root = root;
   p.lddy = lddy, p.ldh = ldh, p.lddh = lddh, p.lddx = lddx;
-  p.rows = (int)rows, p.cols = (int)cols, p.w_bf16 = w_type == OZK_BF16, p.warps = l.warps, p.side_rows = l.rows;
+  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(weight, w_type), p.warps = l.warps, p.side_rows = l.rows;
+  p.inv_cols = 1.f / (float)cols;
   p.parts = dweight ? static_cast<float*>(scratch) : nullptr;
-  const bool vec = quads(dY, lddy, ds) && quads(H, ldh, hs) && quads(dX, lddx, hs) && (!dH || quads(dH, lddh, hs)) && quads(weight, 0, type_size(w_type));
-  if (dy_type == OZK_BF16) {
-    if (h_type == OZK_BF16) launch_backward<__nv_bfloat16, __nv_bfloat16>(vec, p, l, grid, st);
-    else launch_backward<__nv_bfloat16, float>(vec, p, l, grid, st);
-  } else {
-    if (h_type == OZK_BF16) launch_backward<float, __nv_bfloat16>(vec, p, l, grid, st);
-    else launch_backward<float, float>(vec, p, l, grid, st);
-  }
-  if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
+  int vec = least(least(together(dY, lddy, ds), together(H, ldh, hs)), together(dX, lddx, hs));
+  if (dH) vec = least(vec, together(dH, lddh, hs));
+  int grid = 0;
+  bool ok;
+  if (dy_type == OZK_BF16)
+    ok = h_type == OZK_BF16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<__nv_bfloat16, float>(vec, p, l, &grid, st);
+  else
+    ok = h_type == OZK_BF16 ? launch_backward<float, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<float, float>(vec, p, l, &grid, st);
+  if (!ok) return OZK_ERR_CUDA;
   if (dweight) {
     const int64_t parts = rows < (int64_t)grid * l.rows ? rows : (int64_t)grid * l.rows;
     norm_dw_kernel<<<(unsigned)ceil_div(cols, 32), 1024, 0, st>>>(p.parts, (int)parts, p.cols, dweight);
