@@ -2,6 +2,7 @@
 // meets the weights of its own.  The offsets are read on the GPU, so that a router's answer need not reach the host.
 //
 //   experts_pair_kernel    C[t, n] = sum_k X(t, k) W_e(n, k), e the expert of row t: forward products, and input gradients, which sum over the stored rows of W_e
+//   experts_rows_kernel    the same where experts have few rows and reading W is what costs: 128 lines of W and 16 to 64 rows a tile, clusters along K
 //   segments_pair_kernel   C_e[m, n] = sum over the rows t of e of A(t, m) B(t, n): weight gradients
 //
 // UE8M0 scales, applied by the tensor cores (tcgen05.mma kind::mxf8f6f4), as in the product with one matrix; pairs of CTAs with the TMA producer, the MMA issuer,
@@ -39,7 +40,7 @@ struct ExpertParams {
   int64_t ldc;
   int N, tiles_n, groups;
   int chunk;               // blocks summed in tensor memory before the sum is added to C in FP32, a multiple of 4
-  int pairs_ok;            // BF16 results may be stored two at a time
+  int pairs_ok, wide_ok;   // BF16 results may be stored two or four at a time
   int clear;               // rows outside the segments become zero
   StatusBlock* status;
 };
@@ -352,6 +353,259 @@ experts_pair_kernel(const __grid_constant__ ExpertMaps maps, const __grid_consta
   }
 }
 
+// ---- few rows an expert -----------------------------------------------------------------
+// Which tile of a segment this is: its expert, first row and rows (count = 0: there is none), and the rows that segments cover.
+struct RowsTile {
+  int expert, t0, count, first, behind;
+};
+// By one warp, each lane with a run of consecutive experts: offsets are held within the rows and never fall.
+__device__ __forceinline__ RowsTile rows_tile(const int* offsets, int experts, int rows, int tile, int height, int lane) {
+  const int per = (experts + 31) / 32, e0 = min(lane * per, experts), e1 = min(e0 + per, experts);
+  const int first = min(max(__ldg(offsets), 0), rows);
+  int top = first;   // largest offset up to the end of this lane's run
+  for (int e = e0; e < e1; ++e) top = max(top, min(__ldg(offsets + e + 1), rows));
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int v = __shfl_up_sync(0xFFFFFFFFu, top, d);
+    if (lane >= d) top = max(top, v);
+  }
+  const int behind = __shfl_sync(0xFFFFFFFFu, top, 31);
+  int before = __shfl_up_sync(0xFFFFFFFFu, top, 1);   // where this lane's run begins
+  if (lane == 0) before = first;
+  int tiles = 0;
+  for (int e = e0, b = before; e < e1; ++e) {
+    const int f = max(b, min(__ldg(offsets + e + 1), rows));
+    tiles += (f - b + height - 1) / height;
+    b = f;
+  }
+  int sum = tiles;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+    if (lane >= d) sum += v;
+  }
+  RowsTile r{0, 0, 0, first, behind};
+  const uint32_t beyond = __ballot_sync(0xFFFFFFFFu, tile < sum);
+  if (!beyond) return r;
+  const int l = __ffs(beyond) - 1;
+  int left = tile - (sum - tiles);   // in this lane's run, if it is lane l's
+  if (lane == l) {
+    for (int e = e0, b = before; e < e1; ++e) {
+      const int f = max(b, min(__ldg(offsets + e + 1), rows)), n = (f - b + height - 1) / height;
+      if (left < n) {
+        r.expert = e, r.t0 = b + left * height, r.count = min(height, f - r.t0);
+        break;
+      }
+      left -= n;
+      b = f;
+    }
+  }
+  r.expert = __shfl_sync(0xFFFFFFFFu, r.expert, l), r.t0 = __shfl_sync(0xFFFFFFFFu, r.t0, l), r.count = __shfl_sync(0xFFFFFFFFu, r.count, l);
+  return r;
+}
+
+constexpr int kRowsThreads = 6 * 32;   // producer, issuer, 4 warps for scales and epilogue
+constexpr int kRowsMostCluster = 8;
+constexpr int kRowsRange = 8;          // groups summed by the tensor cores alone where the result is FP32
+template <int NT>
+struct ExpertRowsShape {
+  static constexpr int kWBytes = 128 * kBlock, kStageBytes = kWBytes + NT * kBlock, kStages = 4, kSets = 4;
+  static constexpr int kCols = NT + kSets * 8 <= 64 ? 64 : 128;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 512 + 1024;
+  static_assert(NT * 128 * 4 <= kStages * kStageBytes, "the partial sums are exchanged in the stages' memory");
+};
+struct __align__(8) ExpertRowsShared {
+  uint64_t full[4], empty[4], sf_full[4], sf_empty[4], acc_full, drained;
+  uint32_t tmem_base;
+  volatile int abort;
+  RowsTile tile;
+};
+static_assert(sizeof(ExpertRowsShared) <= 512, "room reserved behind the stages");
+
+__device__ __forceinline__ float4 load_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+
+// The lines of W are the instruction's 128 rows, NT rows of C its columns.  The CTAs of a cluster share K and add their sums through distributed shared memory.
+// Tiles of one expert's lines follow each other, so that the clusters at work together read neighbouring memory.
+template <int NT, class T>
+__global__ void __launch_bounds__(kRowsThreads)
+experts_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ ExpertParams p) {
+  using S = ExpertRowsShape<NT>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  ExpertRowsShared* sh = reinterpret_cast<ExpertRowsShared*>(tiles + S::kStages * S::kStageBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank(), size = (int)cluster_size();
+  const int index = (int)(blockIdx.x / size), n0 = index % p.tiles_n * 128;
+  const int g_begin = (int)((int64_t)rank * p.groups / size), g_end = (int)((int64_t)(rank + 1) * p.groups / size);
+  const int b_begin = 4 * g_begin, b_end = min(4 * g_end, p.x.blocks);
+
+  if (warp == 0) {
+    const RowsTile found = rows_tile(p.offsets, p.experts, p.rows, index / p.tiles_n, NT, lane);
+    if (lane == 0) sh->tile = found;
+  } else if (warp == 1) {
+    tmem_alloc(smem_u32(&sh->tmem_base), S::kCols);
+    tmem_relinquish();
+  } else if (threadIdx.x == 64) {
+    prefetch_tensormap(&map_x);
+    prefetch_tensormap(&map_w);
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(smem_u32(&sh->full[s]), 1), mbar_init(smem_u32(&sh->empty[s]), 1);
+      mbar_init(smem_u32(&sh->sf_full[s]), 4), mbar_init(smem_u32(&sh->sf_empty[s]), 1);
+    }
+    mbar_init(smem_u32(&sh->acc_full), 1);
+    mbar_init(smem_u32(&sh->drained), 1);
+    sh->abort = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh->tmem_base;
+  const RowsTile tile = sh->tile;
+  if (p.clear) {
+    const int rest = tile.first + p.rows - tile.behind;
+    T* out = static_cast<T*>(p.out);
+    for (int i = (int)blockIdx.x; i < rest; i += (int)gridDim.x) {
+      T* row = out + (int64_t)(i < tile.first ? i : i - tile.first + tile.behind) * p.ldc;
+      for (int n = threadIdx.x; n < p.N; n += kRowsThreads) store_element(row + n, 0.f);
+    }
+  }
+  if (tile.count == 0) {   // the whole cluster: there are at most as many tiles as were launched
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, S::kCols);
+    return;
+  }
+  float* sums = reinterpret_cast<float*>(tiles);   // [NT][128] once the operands have been consumed
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int issued = 0;
+      for (int b = b_begin; b < b_end; ++b, ++issued) {
+        const int stage = issued % S::kStages;
+        if (!wait_bounded(smem_u32(&sh->empty[stage]), ((uint32_t)(issued / S::kStages) & 1u) ^ 1u, &sh->abort, p.status, 0xC00 + stage)) break;
+        const uint32_t dst = smem_u32(tiles + stage * S::kStageBytes), full = smem_u32(&sh->full[stage]);
+        mbar_arrive_expect_tx(full, S::kStageBytes);
+        int x, y;
+        tile_at(p.w.contract_rows, n0, b, x, y);
+        tma_load_3d(dst, &map_w, full, x, y, tile.expert);
+        tma_load_2d(dst + S::kWBytes, &map_x, full, b * kBlock, tile.t0);
+      }
+      if (sh->abort) {   // copies in flight land before this CTA leaves
+        const uint64_t t0 = global_timer_ns();
+        for (int j = max(0, issued - S::kStages); j < issued; ++j)
+          while (!mbar_try_wait(smem_u32(&sh->full[j % S::kStages]), (uint32_t)(j / S::kStages) & 1u) && global_timer_ns() - t0 < kWaitLimitNs) {
+          }
+      }
+    }
+  } else if (warp == 1) {
+    const int w_lines = p.w.contract_rows;
+    const uint32_t w_step = operand_step(w_lines), x_step = operand_step(0), idesc = idesc_mxf8(128, NT, w_lines, 0);
+    for (int b = b_begin; b < b_end; ++b) {
+      const int i = b - b_begin, stage = i % S::kStages, set = (i / 4) % S::kSets;
+      if (i % 4 == 0 && !wait_warp(smem_u32(&sh->sf_full[set]), (uint32_t)(i / 4 / S::kSets) & 1u, &sh->abort, p.status, 0xC11)) break;
+      if (!wait_warp(smem_u32(&sh->full[stage]), (uint32_t)(i / S::kStages) & 1u, &sh->abort, p.status, 0xC20 + stage)) break;
+      tc_fence_after();
+      const uint32_t base = smem_u32(tiles + stage * S::kStageBytes);
+      const uint64_t dw = operand_desc(w_lines, base), dx = operand_desc(0, base + S::kWBytes);
+      if (elect_one()) {
+#pragma unroll
+        for (uint32_t ks = 0; ks < 4; ++ks)
+          mma_mxf8(tmem, dw + ks * w_step, dx + ks * x_step, idesc | idesc_mxf8_block((uint32_t)b & 3u), tmem + NT + set * 8, tmem + NT + set * 8 + 4, (i || ks) ? 1u : 0u);
+        mma_commit(smem_u32(&sh->empty[stage]));
+        if (b + 1 == b_end) mma_commit(smem_u32(&sh->acc_full));
+        if (i % 4 == 3 || b + 1 == b_end) mma_commit(smem_u32(&sh->sf_empty[set]));
+      }
+      __syncwarp();
+    }
+    if (sh->abort && elect_one()) {
+      mma_commit(smem_u32(&sh->drained));
+      const uint64_t t0 = global_timer_ns();
+      while (!mbar_try_wait(smem_u32(&sh->drained), 0u) && global_timer_ns() - t0 < kWaitLimitNs) {
+      }
+    }
+  } else {
+    const uint32_t quad = (uint32_t)(warp & 3);
+    const uint32_t lanes = tmem + ((quad * 32u) << 16);
+    const int line = (int)quad * 32 + lane;   // of the 128
+    bool ok = true;
+    Operand w = p.w;
+    w.scales = static_cast<const uint8_t*>(p.w.scales) + tile.expert * p.w_scale_step;
+    for (int g = g_begin; g < g_end; ++g) {
+      const int i = g - g_begin, set = i % S::kSets;
+      uint32_t ww[4], wx[4];
+      scale_words<4>(w, n0, lane, g, ww);
+      scale_words<(NT + 31) / 32>(p.x, tile.t0, lane, g, wx);
+      if (!wait_warp(smem_u32(&sh->sf_empty[set]), ((uint32_t)(i / S::kSets) & 1u) ^ 1u, &sh->abort, p.status, 0xC31)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      tmem_st_32x4(lanes + NT + set * 8, ww);
+      tmem_st_32x4(lanes + NT + set * 8 + 4, wx);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh->sf_full[set]));
+    }
+    if (ok) ok = wait_warp(smem_u32(&sh->acc_full), 0u, &sh->abort, p.status, 0xC32);
+    if (ok) {
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < NT / 16; ++c) {
+        uint32_t d[16];
+        tmem_ld_32x16(lanes + c * 16, d);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[(c * 16 + e) * 128 + line] = __uint_as_float(d[e]);
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem, S::kCols);
+  }
+  // each CTA of the cluster joins its share of the sums, in the order of the ranges, four columns a thread
+  const uint32_t local = smem_u32(sums);
+  for (int e = rank * kRowsThreads + (int)threadIdx.x; e < tile.count * 32; e += size * kRowsThreads) {
+    const int n = n0 + e % 32 * 4, left = p.N - n;
+    if (left <= 0) continue;
+    float4 v[kRowsMostCluster];
+#pragma unroll
+    for (int r = 0; r < kRowsMostCluster; ++r)
+      if (r < size) v[r] = load_cluster_f32x4(map_to_cta(local + (uint32_t)e * 16u, (uint32_t)r));
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < kRowsMostCluster; ++r)
+      if (r < size) sum[0] += v[r].x, sum[1] += v[r].y, sum[2] += v[r].z, sum[3] += v[r].w;
+    T* c = static_cast<T*>(p.out) + (int64_t)(tile.t0 + e / 32) * p.ldc + n;
+    if (sizeof(T) == 2 && p.wide_ok && left >= 4) {
+      *reinterpret_cast<uint2*>(c) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) store_element(c + k, sum[k]);
+    }
+  }
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");   // no CTA leaves while another reads its sums; nothing was written that another waits for
+  cluster_wait();
+}
+
 // ---- weight gradients -------------------------------------------------------------------
 // 256 x 256 tiles; both operands are summed over their rows, expert e's blocks of 128 rows being before[e] .. before[e+1] - 1.
 constexpr int kTile = 256;
@@ -633,6 +887,52 @@ bool launch_segments_pair(const CUtensorMap& a, const CUtensorMap& b, const CUte
   return cudaGetLastError() == cudaSuccess;
 }
 
+template <int NT, class T>
+bool launch_experts_rows(const ExpertMaps& maps, const ExpertParams& p, int64_t tiles, int cluster, cudaStream_t st) {
+  static std::atomic<bool> done[kMaxDevices];
+  auto kernel = experts_rows_kernel<NT, T>;
+  if (!raise_smem(kernel, ExpertRowsShape<NT>::kSmem, done)) return false;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * cluster), 1, 1);
+  cfg.blockDim = dim3(kRowsThreads, 1, 1);
+  cfg.dynamicSmemBytes = ExpertRowsShape<NT>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, maps.x[0], maps.w, p) == cudaSuccess;
+}
+template <class T>
+bool launch_experts_rows(int nt, const ExpertMaps& maps, const ExpertParams& p, int64_t tiles, int cluster, cudaStream_t st) {
+  return nt == 16 ? launch_experts_rows<16, T>(maps, p, tiles, cluster, st) : nt == 32 ? launch_experts_rows<32, T>(maps, p, tiles, cluster, st) : launch_experts_rows<64, T>(maps, p, tiles, cluster, st);
+}
+
+// Tiles of at most `height` rows that any segments of these rows need.
+int64_t most_tiles(int64_t rows, int64_t experts, int height) { return (rows + (height - 1) * (experts < rows ? experts : rows)) / height; }
+
+// How experts_rows_kernel would run: NT rows a tile (0: it does not), `cluster` CTAs along K.  The host knows the mean of the rows of an expert, not how they lie.
+struct ExpertRowsPlan {
+  int nt, cluster;
+  int64_t tiles;
+};
+ExpertRowsPlan expert_rows_plan(int64_t rows, int64_t experts, int64_t N, int groups, bool bf16, int sms) {
+  ExpertRowsPlan r = {};
+  const int64_t used = experts < rows ? experts : rows;
+  if (rows > 32 * used) return r;
+  r.nt = rows <= 4 * used ? 16 : rows <= 16 * used ? 32 : 64;
+  r.tiles = most_tiles(rows, experts, r.nt) * ceil_div(N, 128);
+  int64_t c = r.tiles >= 2 * sms ? 1 : 2 * sms / r.tiles;   // two CTAs fit a multiprocessor: K is split over a cluster while that fills them
+  if (!bf16 && c * kRowsRange < groups) c = ceil_div(groups, kRowsRange);   // FP32 results: short ranges
+  if (c > groups) c = groups;
+  if (c > kRowsMostCluster) c = kRowsMostCluster;
+  r.cluster = (int)c;
+  if (!bf16 && c * kRowsRange < groups) r.nt = 0;
+  return r;
+}
+
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 // Codes that a tensor map may be made of.
 bool good_operand(const uint8_t* codes, int64_t ld, const void* scales, int64_t cols, uintptr_t scale_align) {
@@ -691,15 +991,22 @@ ozk_status ozk_fp8_grouped_gemm(int64_t rows, int64_t N, int64_t K, const ozk_fp
   p.experts = (int)experts, p.rows = (int)rows;
   p.out = C, p.ldc = ldc, p.N = (int)N, p.tiles_n = (int)ceil_div(N, kLines), p.groups = (int)ceil_div(K, kGroupK);
   p.chunk = bf16 ? 4 * p.groups : 4 * kRangeGroups;
-  p.pairs_ok = aligned(C, 4) && ldc % 2 == 0;
+  p.pairs_ok = aligned(C, 4) && ldc % 2 == 0, p.wide_ok = aligned(C, 8) && ldc % 4 == 0;
   p.clear = clear_rest;
   p.status = static_cast<StatusBlock*>(status);
-  const int64_t tiles = (rows + (kTokens - 1) * (experts < rows ? experts : rows)) / kTokens;   // at most
+  const ExpertRowsPlan few = expert_rows_plan(rows, experts, N, p.groups, bf16, sms);
+  const int64_t tiles = most_tiles(rows, experts, kTokens);
   if ((tiles * p.tiles_n + sms) * ceil_div(p.groups, kRangeGroups) > INT32_MAX) return OZK_ERR_UNSUPPORTED;
   ozk_fp8_experts w = *W;
   if (w.stride == 0) w.stride = w.ld * w_rows;   // a single expert's is not used, but a map wants one
   ExpertMaps maps;
   if (!expert_map(&maps.w, w, experts, w_rows, w_cols)) return OZK_ERR_CUDA;
+  if (few.nt) {
+    if (few.tiles * few.cluster > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+    if (!operand_map(&maps.x[0], p.x, K, few.nt)) return OZK_ERR_CUDA;
+    p.tiles_n = (int)ceil_div(N, 128);
+    return (bf16 ? launch_experts_rows<__nv_bfloat16>(few.nt, maps, p, few.tiles, few.cluster, st) : launch_experts_rows<float>(few.nt, maps, p, few.tiles, few.cluster, st)) ? OZK_OK : OZK_ERR_CUDA;
+  }
   for (int i = 0; i < kXBoxes; ++i)
     if (!operand_map(&maps.x[i], p.x, K, x_box(i))) return OZK_ERR_CUDA;
   const int64_t items = tiles * p.tiles_n;

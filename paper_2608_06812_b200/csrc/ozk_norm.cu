@@ -308,6 +308,20 @@ struct NormParams {
   uint32_t* scales;
 };
 
+// 1 / sqrt(sum / cols + eps).  The approximate root is off by two units in its last place: a Newton step with the residual of its product taken exactly
+// brings it to the nearest number but for rare cases, and one step does the same for the quotient, so that codes fall where the formula's do.
+__device__ __forceinline__ float inverse_root(float sum, float cols, float inv_cols, float eps) {
+  float m = sum * inv_cols;
+  if (m < 3.0e38f) m = fmaf(fmaf(-m, cols, sum), inv_cols, m);
+  m += eps;
+  float s = rsqrtf(m);
+  if (m > 1.2e-38f && m < 3.0e38f) {
+    const float h = m * s, rest = fmaf(m, s, -h);
+    s = fmaf(0.5f * s, fmaf(-rest, s, fmaf(-h, s, 1.f)), s);
+  }
+  return s;
+}
+
 struct None {};   // no residual: h is x and is not written
 template <class TX, class TR>
 struct Stored { using type = TR; };
@@ -478,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, NormShape<TX, TR, kL, kE, V, kThread
     slot = slot + 1 == kSlots ? 0 : slot + 1;
     sum = row_sum(sum, part, n & 1, p.warps, warp);
     if (live) {
-      const float s = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
+      const float s = inverse_root(sum, (float)p.cols, p.inv_cols, p.eps);
       if (in_row == 0 && lane == 0 && p.root) p.root[row] = s;
       if (codes || y) {
 #pragma unroll
