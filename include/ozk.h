@@ -393,28 +393,61 @@ ozk_status ozk_get_workspace_status(void* workspace, void* stream);
  * Around the 8-bit products: the norm that writes their operands, and products grouped by expert.
  * ------------------------------------------------------------------------------------- */
 
-/* RMS norm of X (rows x cols, x_type) with the residual stream R (r_type: x_type or OZK_F32) added first:
- *   h = x + r, rounded to r_type and written to H (the updated stream);  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
- * R NULL: h = x, and H is not used.  H may be R (same ld), or X where the types agree: the stream is updated in place.
- * The norm is of h as it is stored.  weight: cols numbers of w_type.  FP32 arithmetic, sums in an order that depends on cols alone.
+/* RMS norm of x (rows x cols) with the residual stream r (of x_type, or OZK_F32) added first:
+ *   h = x + r, rounded to the stream's type and written to total (the updated stream);  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
+ * residual NULL: h = x, and total is not used.  total may be the residual (same ld), or x where the types agree: the stream is updated in place.
+ * The norm is of h as it is stored.  weight: cols numbers.  FP32 arithmetic, sums in an order that depends on the sizes alone.
  *   root       optional, rows floats: s, which the backward pass reads (wanted where col_codes are)
- *   Y          optional, rows x cols of x_type: y without quantisation
+ *   y          optional, rows x cols: y without quantisation
  *   row_codes, row_scales / col_codes, col_scales   optional: y by 1 x 128 / 128 x 1 blocks, as by ozk_fp8_quantize_lines
  * Mean squares beyond FP32 count as infinite (s = 0).  A NaN or an infinity in a row makes NaN of the row's y (0 of what is finite beside an infinity).
  * cols <= 32768.  rows, cols = 0 are allowed. */
-ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, const void* R, int r_type, int64_t ldr,
-                        void* H, int64_t ldh, const void* weight, int w_type, double eps, float* root, void* Y, int64_t ldy,
-                        uint8_t* row_codes, int64_t row_ld, uint8_t* row_scales, uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales,
-                        void* stream);
+typedef struct {
+  int64_t rows, cols;
+  const void* x;             /* x_type */
+  int64_t ldx;
+  const void* residual;      /* residual_type, or NULL */
+  int64_t ldr;
+  void* total;               /* residual_type: h */
+  int64_t ldt;
+  const void* weight;        /* weight_type */
+  float* root;
+  void* y;                   /* x_type */
+  int64_t ldy;
+  uint8_t* row_codes;
+  int64_t row_ld;
+  uint8_t* row_scales;
+  uint8_t* col_codes;
+  int64_t col_ld;
+  uint8_t* col_scales;
+  double eps;
+  int x_type, residual_type, weight_type;
+} ozk_rms_norm_args;
+ozk_status ozk_rms_norm(const ozk_rms_norm_args* args, void* stream);
 
-/* Its gradients.  dY (dy_type): gradient of y; H (h_type), root: what the forward pass normed and its s; dH: optional gradient of h from
- * elsewhere (h_type).
- *   g = dy w;  dX = dh + s (g - h s mean(g h s)), in h_type, the gradient of x and of r alike;  dweight = sum over the rows of dy h s (FP32, optional)
- * dX may be dH.  scratch: ozk_rms_norm_backward_scratch_bytes(), 16-byte aligned, for this call alone; not needed without dweight. */
+/* Its gradients.  dy: gradient of y; total, root: what the forward pass normed (x, where there was no residual) and its s; dtotal: optional
+ * gradient of h from elsewhere.
+ *   g = dy w;  dx = dh + s (g - h s mean(g h s)), the gradient of x and of r alike;  dweight = sum over the rows of dy h s (FP32, optional)
+ * dx may be dtotal.  scratch: ozk_rms_norm_backward_scratch_bytes(), 16-byte aligned, for this call alone; not needed without dweight. */
 size_t ozk_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols);
-ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int dy_type, int64_t lddy, const void* H, int h_type, int64_t ldh,
-                                 const float* root, const void* weight, int w_type, const void* dH, int64_t lddh, void* dX, int64_t lddx,
-                                 float* dweight, void* scratch, size_t scratch_bytes, void* stream);
+typedef struct {
+  int64_t rows, cols;
+  const void* dy;            /* dy_type */
+  int64_t lddy;
+  const void* total;         /* total_type */
+  int64_t ldt;
+  const float* root;
+  const void* weight;        /* weight_type */
+  const void* dtotal;        /* total_type, or NULL */
+  int64_t lddt;
+  void* dx;                  /* total_type */
+  int64_t lddx;
+  float* dweight;            /* or NULL */
+  void* scratch;
+  size_t scratch_bytes;
+  int dy_type, total_type, weight_type;
+} ozk_rms_norm_backward_args;
+ozk_status ozk_rms_norm_backward(const ozk_rms_norm_backward_args* args, void* stream);
 
 /* Segments: rows lie in the order of the experts they belong to; expert e has rows offsets[e] .. offsets[e+1] - 1 (offsets: experts + 1 numbers in
  * device memory, ascending from offsets[0] >= 0 to offsets[experts] <= rows).  Segments may be empty; rows before the first and behind the last

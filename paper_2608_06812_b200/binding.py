@@ -41,6 +41,18 @@ class ozk_fp8_experts(ctypes.Structure):
     _fields_ = [("codes", c_void_p), ("ld", c_int64), ("stride", c_int64), ("scales", c_void_p), ("contract_rows", c_int)]
 
 
+class ozk_rms_norm_args(ctypes.Structure):
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("x", c_void_p), ("ldx", c_int64), ("residual", c_void_p), ("ldr", c_int64), ("total", c_void_p), ("ldt", c_int64),
+                ("weight", c_void_p), ("root", c_void_p), ("y", c_void_p), ("ldy", c_int64), ("row_codes", c_void_p), ("row_ld", c_int64), ("row_scales", c_void_p),
+                ("col_codes", c_void_p), ("col_ld", c_int64), ("col_scales", c_void_p), ("eps", c_double), ("x_type", c_int), ("residual_type", c_int), ("weight_type", c_int)]
+
+
+class ozk_rms_norm_backward_args(ctypes.Structure):
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("dy", c_void_p), ("lddy", c_int64), ("total", c_void_p), ("ldt", c_int64), ("root", c_void_p), ("weight", c_void_p),
+                ("dtotal", c_void_p), ("lddt", c_int64), ("dx", c_void_p), ("lddx", c_int64), ("dweight", c_void_p), ("scratch", c_void_p), ("scratch_bytes", c_size_t),
+                ("dy_type", c_int), ("total_type", c_int), ("weight_type", c_int)]
+
+
 class ozk_adamw_tensor(ctypes.Structure):
     _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
                 ("copy", c_void_p), ("n", c_int64)]
@@ -91,11 +103,9 @@ SIGNATURES = {
     "ozk_fp8_gemm": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
     "ozk_fp8_gemm_scratch": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ozk_fp8_gemm_plan": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int, c_void_p]),
-    "ozk_rms_norm": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int, c_double, c_void_p, c_void_p, c_int64,
-                             c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "ozk_rms_norm": (c_int, [c_void_p, c_void_p]),
     "ozk_rms_norm_backward_scratch_bytes": (c_size_t, [c_int64, c_int64]),
-    "ozk_rms_norm_backward": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int, c_int64, c_void_p, c_void_p, c_int, c_void_p, c_int64, c_void_p, c_int64,
-                                      c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ozk_rms_norm_backward": (c_int, [c_void_p, c_void_p]),
     "ozk_fp8_segment_blocks": (c_int64, [c_int64, c_int64]),
     "ozk_fp8_quantize_segments": (c_int, [c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
     "ozk_fp8_quantize_experts": (c_int, [c_int64, c_int64, c_int64, c_void_p, c_int, c_int64, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_void_p]),
@@ -299,18 +309,16 @@ def ozk_fp8_gemm_plan(M, N, K, A, B, c_type, sms=0) -> ozk_fp8_plan:
     return plan
 
 
-def ozk_rms_norm(rows, cols, X, x_type, ldx, R, r_type, ldr, H, ldh, weight, w_type, eps, root=None, Y=None, ldy=0,
-                 row_codes=None, row_ld=0, row_scales=None, col_codes=None, col_ld=0, col_scales=None, stream=0) -> int:
-    return lib().ozk_rms_norm(rows, cols, X, x_type, ldx, R, r_type, ldr, H, ldh, weight, w_type, eps, root, Y, ldy,
-                              row_codes, row_ld, row_scales, col_codes, col_ld, col_scales, stream)
+def ozk_rms_norm(args: ozk_rms_norm_args, stream=0) -> int:
+    return lib().ozk_rms_norm(ctypes.byref(args), stream)
 
 
 def ozk_rms_norm_backward_scratch_bytes(rows: int, cols: int) -> int:
     return lib().ozk_rms_norm_backward_scratch_bytes(rows, cols)
 
 
-def ozk_rms_norm_backward(rows, cols, dY, dy_type, lddy, H, h_type, ldh, root, weight, w_type, dH, lddh, dX, lddx, dweight=None, scratch=None, scratch_bytes=0, stream=0) -> int:
-    return lib().ozk_rms_norm_backward(rows, cols, dY, dy_type, lddy, H, h_type, ldh, root, weight, w_type, dH, lddh, dX, lddx, dweight, scratch, scratch_bytes, stream)
+def ozk_rms_norm_backward(args: ozk_rms_norm_backward_args, stream=0) -> int:
+    return lib().ozk_rms_norm_backward(ctypes.byref(args), stream)
 
 
 def ozk_fp8_segment_blocks(rows: int, experts: int) -> int:

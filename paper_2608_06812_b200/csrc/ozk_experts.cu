@@ -914,6 +914,9 @@ bool launch_experts_rows(int nt, const ExpertMaps& maps, const ExpertParams& p, 
 int64_t most_tiles(int64_t rows, int64_t experts, int height) { return (rows + (height - 1) * (experts < rows ? experts : rows)) / height; }
 
 // How experts_rows_kernel would run: NT rows a tile (0: it does not), `cluster` CTAs along K.  The host knows the mean of the rows of an expert, not how they lie.
+// It serves up to 8 rows an expert, and up to 64 where the pairs have too few tiles to be at work all.  Rows against pairs, us: 244 rows of 32 experts (4096 -> 2048) 46.6 : 51.9,
+// 64 of 8 (4096 -> 4096) 26.5 : 30.0, 8 of 64 (2048 -> 4096) 18.0 : 21.1, but 1000 of 64 (2048 -> 2048) 57.8 : 52.0.  K is split only while CTAs are
+// missing: 64 of 8 26.5, split by two 30.0; one row (4096 -> 4096) 14.9, split by eight 10.7.
 struct ExpertRowsPlan {
   int nt, cluster;
   int64_t tiles;
@@ -921,7 +924,7 @@ struct ExpertRowsPlan {
 ExpertRowsPlan expert_rows_plan(int64_t rows, int64_t experts, int64_t N, int groups, bool bf16, int sms) {
   ExpertRowsPlan r = {};
   const int64_t used = experts < rows ? experts : rows;
-  if (rows > 32 * used) return r;
+  if (rows > 8 * used && (rows > 64 * used || most_tiles(rows, experts, kTokens) * ceil_div(N, kLines) >= sms / 2)) return r;
   r.nt = rows <= 4 * used ? 16 : rows <= 16 * used ? 32 : 64;
   r.tiles = most_tiles(rows, experts, r.nt) * ceil_div(N, 128);
   int64_t c = r.tiles >= 2 * sms ? 1 : 2 * sms / r.tiles;   // two CTAs fit a multiprocessor: K is split over a cluster while that fills them

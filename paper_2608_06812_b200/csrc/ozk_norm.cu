@@ -268,22 +268,23 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 constexpr int kMostWarps = 16;
 constexpr int kMostCols = kGroup * kMostWarps * 4;
+constexpr int64_t kMostRows = INT32_MAX - 65536;   // row indexes are ints, with room for what lies ahead
 
 // How a row is laid over a thread block: `warps` a row, `rows` of them side by side, V groups of 512 columns a warp.
 struct Layout {
   int warps, rows, v;
 };
-// A row's own cost (its sum, addresses, barriers) is shared by two groups a warp where there are rows enough to fill the GPU all the same; few rows
-// have as many warps as they can use.  `most`: groups a warp takes in thread blocks of eight warps; wider rows have thread blocks of 16.
-Layout row_layout(int64_t rows, int64_t cols, int most) {
+// Forward, a row's own cost (its sum, addresses, barriers) is shared by two groups a warp where there are rows enough to fill the GPU all the same (16384 x 4096: 82 us, one
+// group a warp 99); few rows have as many warps as they can use.  The backward pass, whose sums of dw take registers, is faster with one (108 us : 114).  `most`: groups a warp takes in thread blocks of eight warps; wider rows have thread blocks of 16.
+Layout row_layout(int64_t rows, int64_t cols, int most, bool forward) {
   const int groups = (int)ceil_div(cols, kGroup);
-  int v = most == 4 && groups > 1 && rows * groups >= (int64_t)device_sm_count() * 64 ? 2 : 1;
+  int v = forward && groups > 1 && rows * groups >= (int64_t)device_sm_count() * 64 ? 2 : 1;
   while (v < most && 8 * v < groups) v *= 2;
   if (8 * v < groups) v = groups <= 32 ? 2 : 4;
   const int warps = (int)ceil_div(groups, v);
   return {warps, warps < 8 ? 8 / warps : 1, v};
 }
-constexpr int kNormMost = 4, kGradMost = 2;
+constexpr int kNormMost = 4, kNormMostF32 = 2, kGradMost = 2;   // FP32 rows: what four groups hold leaves no room for the next row
 // Sum over the warps of this thread's row, the same in all of them.  `side` alternates, so that one barrier is enough.
 __device__ __forceinline__ float row_sum(float v, float (*part)[kMostWarps], int side, int warps, int warp) {
   v = warp_sum(v);
@@ -637,6 +638,8 @@ struct GradShape {
   static constexpr int kStages = ring_stages(bytes<true>(), kThreads, kBlocks);
   static constexpr bool kOn = kStages > 0;
   static constexpr int kThreadBytes = bytes<kOn>();
+  // Room for one row only: dy and h stay in registers, so that the next row's may follow before this one's sum is known.
+  static constexpr bool kHold = kStages == 1 && V <= 2 && kE > 1;
 };
 
 // Rows as in the forward pass; what is needed again after the sum is read again from shared memory.  Each thread adds up its
@@ -671,8 +674,30 @@ __global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThread
       if (pe) e_ahead += e_step;
     }
   };
+  // With one slot: dy and h of the next row once this one's are in registers, dh after it has been written.
+  auto fetch_early = [&]() {
+    if (ahead < p.rows) {
+      const bool edge = ahead == 0 || ahead == p.rows - 1;
+      SD::fetch(d_ahead, ring_at, step, lane, group_left, edge);
+      SH::fetch(h_ahead, ring_at + h_at, step, lane, group_left, edge);
+    }
+    d_ahead += d_step, h_ahead += h_step;
+  };
+  auto fetch_late = [&]() {
+    if (pe && ahead < p.rows) SH::fetch(e_ahead, ring_at + e_at, step, lane, group_left, ahead == 0 || ahead == p.rows - 1);
+    if (pe) e_ahead += e_step;
+    copy_commit();
+    ahead += stride;
+  };
+  if constexpr (S::kHold) {
+    fetch_early();
+    fetch_late();
+  } else {
 #pragma unroll
-  for (int k = 0; k < kSlots; ++k) fetch(k);
+    for (int k = 0; k < kSlots; ++k) fetch(k);
+  }
+  Piece<TD, kL> d_held[S::kHold ? V : 1][kPieces];
+  Piece<TH, kL> h_held[S::kHold ? V : 1][kPieces];
   float dw[V][kPieces][kL];
 #pragma unroll
   for (int v = 0; v < V; ++v)
@@ -694,8 +719,8 @@ __global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThread
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
         const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
-        Piece<TD, kL> d;
-        Piece<TH, kL> h;
+        Piece<TD, kL> d_now, &d = S::kHold ? d_held[S::kHold ? v : 0][k] : d_now;
+        Piece<TH, kL> h_now, &h = S::kHold ? h_held[S::kHold ? v : 0][k] : h_now;
         SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
         SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
         float w[kL];
@@ -715,8 +740,12 @@ __global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThread
         const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
         Piece<TD, kL> d;
         Piece<TH, kL> h, e = {}, out;
-        SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
-        SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
+        if constexpr (S::kHold) {
+          d = d_held[v][k], h = h_held[v][k];
+        } else {
+          SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
+          SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
+        }
         if (pe) SH::template take<kFull>(pe, base + e_at, at, rest, edge, v, k, e);
         float w[kL], dx[kL];
         load_weights<kFull, kL>(p.w, p.w_kind, c_lane + at, rest, w);
@@ -738,6 +767,7 @@ __global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThread
         else look(std::false_type{}, v, left - lane * kL);
       }
     }
+    if constexpr (S::kHold) fetch_early();
     sum = row_sum(sum, part, n & 1, p.warps, warp);
     if (live) {
       const float minus_mean = -sum * p.inv_cols;
@@ -750,8 +780,12 @@ __global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThread
         else write(std::false_type{}, v, left - lane * kL, minus_mean);
       }
     }
-    fetch(slot);
-    slot = slot + 1 == kSlots ? 0 : slot + 1;
+    if constexpr (S::kHold) {
+      fetch_late();
+    } else {
+      fetch(slot);
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
+    }
     s = s_next;
     row += stride, pd += d_step, ph += h_step, po += o_step;
     if (pe) pe += e_step;
@@ -821,7 +855,12 @@ bool launch_norm_rows_as(const NormParams& p, const Layout& l, cudaStream_t st) 
 }
 template <class TX, class TR, int kL, int kE, bool kWhole>
 bool launch_norm_rows(const NormParams& p, const Layout& l, cudaStream_t st) {
-  if (l.warps > 8) return launch_norm_rows_as<TX, TR, kL, kE, 4, 512, kWhole>(p, l, st);
+  if (l.warps > 8) {
+    if constexpr (sizeof(typename Stored<TX, TR>::type) == 4) {
+      if (l.v == 2) return launch_norm_rows_as<TX, TR, kL, kE, 2, 512, kWhole>(p, l, st);
+    }
+    return launch_norm_rows_as<TX, TR, kL, kE, 4, 512, kWhole>(p, l, st);
+  }
   return l.v == 1 ? launch_norm_rows_as<TX, TR, kL, kE, 1, 256, kWhole>(p, l, st)
                   : l.v == 2 ? launch_norm_rows_as<TX, TR, kL, kE, 2, 256, kWhole>(p, l, st) : launch_norm_rows_as<TX, TR, kL, kE, 4, 256, kWhole>(p, l, st);
 }
@@ -881,44 +920,45 @@ using namespace ozk;
 
 extern "C" {
 
-ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, int64_t ldx, const void* R, int r_type, int64_t ldr, void* H, int64_t ldh,
-                        const void* weight, int w_type, double eps, float* root, void* Y, int64_t ldy, uint8_t* row_codes, int64_t row_ld,
-                        uint8_t* row_scales, uint8_t* col_codes, int64_t col_ld, uint8_t* col_scales, void* stream) {
-  if (rows < 0 || cols < 0 || !type_ok(x_type) || !type_ok(w_type) || ldx < cols || !(eps >= 0.0)) return OZK_ERR_INVALID_ARG;
-  if (R && (!type_ok(r_type) || ldr < cols || ldh < cols)) return OZK_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 65536 || cols > kMostCols || (R && r_type != x_type && r_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
-  const bool by_rows = row_codes || row_scales, by_cols = col_codes || col_scales;
+ozk_status ozk_rms_norm(const ozk_rms_norm_args* args, void* stream) {
+  if (!args) return OZK_ERR_INVALID_ARG;
+  const ozk_rms_norm_args& a = *args;
+  const int64_t rows = a.rows, cols = a.cols;
+  const void *X = a.x, *R = a.residual;
+  if (rows < 0 || cols < 0 || !type_ok(a.x_type) || !type_ok(a.weight_type) || a.ldx < cols || !(a.eps >= 0.0)) return OZK_ERR_INVALID_ARG;
+  if (R && (!type_ok(a.residual_type) || a.ldr < cols || a.ldt < cols)) return OZK_ERR_INVALID_ARG;
+  if (rows > kMostRows || cols > kMostCols || (R && a.residual_type != a.x_type && a.residual_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
+  const bool by_rows = a.row_codes || a.row_scales, by_cols = a.col_codes || a.col_scales;
   if (rows == 0 || cols == 0) return OZK_OK;
-  const int h_type = R ? r_type : x_type;
-  if (!on(X, type_size(x_type)) || !on(weight, type_size(w_type)) || (R && (!on(R, type_size(r_type)) || !on(H, type_size(r_type))))) return OZK_ERR_INVALID_ARG;
-  if (Y && (!on(Y, type_size(x_type)) || ldy < cols)) return OZK_ERR_INVALID_ARG;
-  if ((root && !on(root, 4)) || (by_cols && !root)) return OZK_ERR_INVALID_ARG;
-  if (by_rows && (!row_codes || !row_scales || !aligned16(row_codes) || row_ld % 16 || row_ld < cols || !on(row_scales, 4))) return OZK_ERR_INVALID_ARG;
-  if (by_cols && (!col_codes || !col_scales || !aligned16(col_codes) || col_ld % 16 || col_ld < cols)) return OZK_ERR_INVALID_ARG;
+  const int h_type = R ? a.residual_type : a.x_type, xs = type_size(a.x_type), hs = type_size(h_type);
+  if (!on(X, xs) || !on(a.weight, type_size(a.weight_type)) || (R && (!on(R, hs) || !on(a.total, hs)))) return OZK_ERR_INVALID_ARG;
+  if (a.y && (!on(a.y, xs) || a.ldy < cols)) return OZK_ERR_INVALID_ARG;
+  if ((a.root && !on(a.root, 4)) || (by_cols && !a.root)) return OZK_ERR_INVALID_ARG;
+  if (by_rows && (!a.row_codes || !a.row_scales || !aligned16(a.row_codes) || a.row_ld % 16 || a.row_ld < cols || !on(a.row_scales, 4))) return OZK_ERR_INVALID_ARG;
+  if (by_cols && (!a.col_codes || !a.col_scales || !aligned16(a.col_codes) || a.col_ld % 16 || a.col_ld < cols)) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const Layout l = row_layout(rows, cols, kNormMost);
-  const int xs = type_size(x_type), hs = type_size(h_type);
+  const Layout l = row_layout(rows, cols, h_type == OZK_F32 ? kNormMostF32 : kNormMost, true);
   NormParams p = {};
-  p.x = X, p.r = R, p.w = weight, p.h = H, p.y = Y;
-  p.ldx = ldx, p.ldr = ldr, p.ldh = ldh, p.ldy = ldy, p.ldq = row_ld;
-  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(weight, w_type), p.warps = l.warps, p.side_rows = l.rows;
-  p.eps = (float)eps, p.inv_cols = 1.f / (float)cols, p.root = root, p.codes = row_codes, p.scales = reinterpret_cast<uint32_t*>(row_scales);
-  int vec = together(X, ldx, xs);
-  if (R) vec = least(vec, least(together(R, ldr, hs), together(H, ldh, hs)));
-  if (Y) vec = least(vec, together(Y, ldy, xs));
+  p.x = X, p.r = R, p.w = a.weight, p.h = a.total, p.y = a.y;
+  p.ldx = a.ldx, p.ldr = a.ldr, p.ldh = a.ldt, p.ldy = a.ldy, p.ldq = a.row_ld;
+  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(a.weight, a.weight_type), p.warps = l.warps, p.side_rows = l.rows;
+  p.eps = (float)a.eps, p.inv_cols = 1.f / (float)cols, p.root = a.root, p.codes = a.row_codes, p.scales = reinterpret_cast<uint32_t*>(a.row_scales);
+  int vec = together(X, a.ldx, xs);
+  if (R) vec = least(vec, least(together(R, a.ldr, hs), together(a.total, a.ldt, hs)));
+  if (a.y) vec = least(vec, together(a.y, a.ldy, xs));
   bool ok;
-  if (x_type == OZK_BF16)
+  if (a.x_type == OZK_BF16)
     ok = !R ? launch_norm_rows<__nv_bfloat16, None>(vec, p, l, st)
-            : r_type == OZK_BF16 ? launch_norm_rows<__nv_bfloat16, __nv_bfloat16>(vec, p, l, st) : launch_norm_rows<__nv_bfloat16, float>(vec, p, l, st);
+            : h_type == OZK_BF16 ? launch_norm_rows<__nv_bfloat16, __nv_bfloat16>(vec, p, l, st) : launch_norm_rows<__nv_bfloat16, float>(vec, p, l, st);
   else
     ok = !R ? launch_norm_rows<float, None>(vec, p, l, st) : launch_norm_rows<float, float>(vec, p, l, st);
   if (!ok) return OZK_ERR_CUDA;
   if (by_cols) {
-    const void* h = R ? H : X;
-    const int64_t ld = R ? ldh : ldx;
-    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(together(h, ld, 2), h, ld, p, col_codes, col_ld, col_scales, st);
-    else launch_norm_cols<float>(together(h, ld, 4), h, ld, p, col_codes, col_ld, col_scales, st);
+    const void* h = R ? a.total : X;
+    const int64_t ld = R ? a.ldt : a.ldx;
+    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(together(h, ld, 2), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
+    else launch_norm_cols<float>(together(h, ld, 4), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
     if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
   }
   return OZK_OK;
@@ -926,43 +966,44 @@ ozk_status ozk_rms_norm(int64_t rows, int64_t cols, const void* X, int x_type, i
 
 size_t ozk_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || cols > kMostCols) return 0;
-  const Layout l = row_layout(rows, cols, kGradMost);
+  const Layout l = row_layout(rows, cols, kGradMost, false);
   return (size_t)grid_of(rows, l, kGradBlocks) * l.rows * (size_t)cols * 4;
 }
 
-ozk_status ozk_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int dy_type, int64_t lddy, const void* H, int h_type, int64_t ldh, const float* root,
-                                 const void* weight, int w_type, const void* dH, int64_t lddh, void* dX, int64_t lddx, float* dweight, void* scratch,
-                                 size_t scratch_bytes, void* stream) {
-  if (rows < 0 || cols < 0 || !type_ok(dy_type) || !type_ok(h_type) || !type_ok(w_type) || lddy < cols || ldh < cols || lddx < cols) return OZK_ERR_INVALID_ARG;
-  if (dH && lddh < cols) return OZK_ERR_INVALID_ARG;
-  if (rows > INT32_MAX - 65536 || cols > kMostCols) return OZK_ERR_UNSUPPORTED;
+ozk_status ozk_rms_norm_backward(const ozk_rms_norm_backward_args* args, void* stream) {
+  if (!args) return OZK_ERR_INVALID_ARG;
+  const ozk_rms_norm_backward_args& a = *args;
+  const int64_t rows = a.rows, cols = a.cols;
+  if (rows < 0 || cols < 0 || !type_ok(a.dy_type) || !type_ok(a.total_type) || !type_ok(a.weight_type) || a.lddy < cols || a.ldt < cols || a.lddx < cols) return OZK_ERR_INVALID_ARG;
+  if (a.dtotal && a.lddt < cols) return OZK_ERR_INVALID_ARG;
+  if (rows > kMostRows || cols > kMostCols) return OZK_ERR_UNSUPPORTED;
   if (cols == 0) return OZK_OK;
-  if (dweight && !on(dweight, 4)) return OZK_ERR_INVALID_ARG;
+  if (a.dweight && !on(a.dweight, 4)) return OZK_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (rows == 0) return !dweight || cudaMemsetAsync(dweight, 0, (size_t)cols * 4, st) == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
-  const int ds = type_size(dy_type), hs = type_size(h_type);
-  if (!on(dY, ds) || !on(H, hs) || !on(root, 4) || !on(weight, type_size(w_type)) || !on(dX, hs) || (dH && !on(dH, hs))) return OZK_ERR_INVALID_ARG;
+  if (rows == 0) return !a.dweight || cudaMemsetAsync(a.dweight, 0, (size_t)cols * 4, st) == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
+  const int ds = type_size(a.dy_type), hs = type_size(a.total_type);
+  if (!on(a.dy, ds) || !on(a.total, hs) || !on(a.root, 4) || !on(a.weight, type_size(a.weight_type)) || !on(a.dx, hs) || (a.dtotal && !on(a.dtotal, hs))) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
-  const Layout l = row_layout(rows, cols, kGradMost);
-  if (dweight && (!on(scratch, 16) || scratch_bytes < ozk_rms_norm_backward_scratch_bytes(rows, cols))) return OZK_ERR_WORKSPACE;
+  const Layout l = row_layout(rows, cols, kGradMost, false);
+  if (a.dweight && (!on(a.scratch, 16) || a.scratch_bytes < ozk_rms_norm_backward_scratch_bytes(rows, cols))) return OZK_ERR_WORKSPACE;
   GradParams p = {};
-  p.dy = dY, p.h = H, p.dh = dH, p.w = weight, p.dx = dX, p.root = root;
-  p.lddy = lddy, p.ldh = ldh, p.lddh = lddh, p.lddx = lddx;
-  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(weight, w_type), p.warps = l.warps, p.side_rows = l.rows;
+  p.dy = a.dy, p.h = a.total, p.dh = a.dtotal, p.w = a.weight, p.dx = a.dx, p.root = a.root;
+  p.lddy = a.lddy, p.ldh = a.ldt, p.lddh = a.lddt, p.lddx = a.lddx;
+  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(a.weight, a.weight_type), p.warps = l.warps, p.side_rows = l.rows;
   p.inv_cols = 1.f / (float)cols;
-  p.parts = dweight ? static_cast<float*>(scratch) : nullptr;
-  int vec = least(least(together(dY, lddy, ds), together(H, ldh, hs)), together(dX, lddx, hs));
-  if (dH) vec = least(vec, together(dH, lddh, hs));
+  p.parts = a.dweight ? static_cast<float*>(a.scratch) : nullptr;
+  int vec = least(least(together(a.dy, a.lddy, ds), together(a.total, a.ldt, hs)), together(a.dx, a.lddx, hs));
+  if (a.dtotal) vec = least(vec, together(a.dtotal, a.lddt, hs));
   int grid = 0;
   bool ok;
-  if (dy_type == OZK_BF16)
-    ok = h_type == OZK_BF16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<__nv_bfloat16, float>(vec, p, l, &grid, st);
+  if (a.dy_type == OZK_BF16)
+    ok = a.total_type == OZK_BF16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<__nv_bfloat16, float>(vec, p, l, &grid, st);
   else
-    ok = h_type == OZK_BF16 ? launch_backward<float, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<float, float>(vec, p, l, &grid, st);
+    ok = a.total_type == OZK_BF16 ? launch_backward<float, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<float, float>(vec, p, l, &grid, st);
   if (!ok) return OZK_ERR_CUDA;
-  if (dweight) {
+  if (a.dweight) {
     const int64_t parts = rows < (int64_t)grid * l.rows ? rows : (int64_t)grid * l.rows;
-    norm_dw_kernel<<<(unsigned)ceil_div(cols, 32), 1024, 0, st>>>(p.parts, (int)parts, p.cols, dweight);
+    norm_dw_kernel<<<(unsigned)ceil_div(cols, 32), 1024, 0, st>>>(p.parts, (int)parts, p.cols, a.dweight);
     if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
   }
   return OZK_OK;

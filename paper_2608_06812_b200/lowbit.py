@@ -26,6 +26,7 @@ through libozk.so; arguments are checked here (ValueError) and in the library (O
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import NamedTuple
 
 import torch
@@ -337,15 +338,29 @@ class Normed(NamedTuple):
     root: "torch.Tensor | None"
 
 
-def _beside(t: torch.Tensor, what: str, x: torch.Tensor, dtypes) -> int:
-    """Checks a matrix of the shape of x, and returns its leading dimension."""
-    if t.dtype not in dtypes or t.shape != x.shape or t.get_device() != x.get_device() or (t.shape[1] > 1 and t.stride(1) != 1 and t.shape[0]):
-        raise ValueError(f"{what} is {' or '.join(map(str, dtypes))} {tuple(x.shape)} on {x.device} with contiguous rows, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+# The structures of the norm's arguments, packed: a call with each of them converted by itself costs 2 us more.
+_NORM_ARGS = struct.Struct("@qqPqPqPqPPPqPqPPqPdiii4x")
+_NORM_GRAD_ARGS = struct.Struct("@qqPqPqPPPqPqPPNiii4x")
+assert _NORM_ARGS.size == ctypes.sizeof(ozk.ozk_rms_norm_args) and _NORM_GRAD_ARGS.size == ctypes.sizeof(ozk.ozk_rms_norm_backward_args)
+_NOWHERE = (0, 0, 0)
+
+
+def _beside(t: torch.Tensor, what: str, r: int, c: int, index: int, dtype: torch.dtype, or_dtype: torch.dtype | None = None) -> int:
+    """Checks a matrix that lies beside another, and returns its leading dimension."""
+    if t.dtype is not dtype and t.dtype is not or_dtype:
+        raise ValueError(f"{what} is {dtype if or_dtype in (None, dtype) else f'{dtype} or {or_dtype}'}, not {t.dtype}")
+    if t.shape != (r, c) or t.get_device() != index:
+        raise ValueError(f"{what} is [{r}, {c}] on GPU {index}, not {list(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and c > 1 and r:
+        raise ValueError(f"the rows of {what} are contiguous")
+    return ld if r > 1 else c or 1
 
 
 def _vector(t: torch.Tensor, what: str, n: int, index: int) -> int:
-    kind = _type(t, what)
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        _type(t, what)
     if t.shape != (n,) or t.get_device() != index or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{what} is a contiguous [{n}] on GPU {index}")
     return kind
@@ -359,42 +374,45 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     `rows`, `cols`: as for quantize_lines; `y`: whether (or where) the answer is wanted in the type of x too; `total`: where h is written (a new tensor if
     None; may be `residual`, or x if of one type); `root`: whether (or where) s is wanted, float32 [rows], for rms_norm_backward."""
     r, c, kind, ld = _input(x)
-    index, device = x.get_device(), x.device
+    index = x.get_device()
     w_kind = _vector(weight, "weight", c, index)
     written = []
     if residual is None:
         if total is not None:
             raise ValueError("total is written where there is a residual")
-        total, to_residual = x, (None, 0, 0, None, 0)
+        total, from_residual, r_kind = x, (0, 0, 0, 0), 0
     else:
-        ldr = _beside(residual, "residual", x, (x.dtype,) if x.dtype is torch.float32 else (x.dtype, torch.float32))
+        ldr = _beside(residual, "residual", r, c, index, x.dtype, torch.float32)
+        r_type = residual.dtype
+        r_kind = _TYPES[r_type]
         if total is None:
-            total = torch.empty(r, c, dtype=residual.dtype, device=device)
+            total = torch.empty(r, c, dtype=r_type, device=x.device)
+            ldt = c or 1
         else:
+            ldt = _beside(total, "total", r, c, index, r_type)
             written.append(total)
-        ldt = _beside(total, "total", x, (residual.dtype,))
-        to_residual = (residual.data_ptr(), _TYPES[residual.dtype], ldr, total.data_ptr(), ldt)
-    by_rows = Fp8Matrix.empty(r, c, ROWS, device) if rows is True else rows or None
-    by_cols = Fp8Matrix.empty(r, c, COLS, device) if cols is True else cols or None
-    to_rows = _NONE if by_rows is None else _output(by_rows, r, c, ROWS, index)
-    to_cols = _NONE if by_cols is None else _output(by_cols, r, c, COLS, index)
+        from_residual = (residual.data_ptr(), ldr, total.data_ptr(), ldt)
+    by_rows = Fp8Matrix.empty(r, c, ROWS, x.device) if rows is True else rows or None
+    by_cols = Fp8Matrix.empty(r, c, COLS, x.device) if cols is True else cols or None
+    to_rows = _NOWHERE if by_rows is None else _output(by_rows, r, c, ROWS, index)
+    to_cols = _NOWHERE if by_cols is None else _output(by_cols, r, c, COLS, index)
+    y_at, ldy = 0, 0
     if y is True:
-        y, ldy = torch.empty(r, c, dtype=x.dtype, device=device), max(c, 1)
+        y = torch.empty(r, c, dtype=x.dtype, device=x.device)
+        y_at, ldy = y.data_ptr(), c or 1
     elif y is None or y is False:
-        y, ldy = None, 0
+        y = None
     else:
-        ldy = _beside(y, "y", x, (x.dtype,))
+        y_at, ldy = y.data_ptr(), _beside(y, "y", r, c, index, x.dtype)
         written.append(y)
-    if root is True or ((root is None or root is False) and by_cols is not None):
-        root = torch.empty(r, dtype=torch.float32, device=device)
-    elif root is None or root is False:
-        root = None
-    elif _vector(root, "root", r, index) != ozk.OZK_F32:
-        raise ValueError("root is float32")
+    if root is None or root is False or root is True:
+        root = torch.empty(r, dtype=torch.float32, device=x.device) if root or by_cols is not None else None
     else:
+        if _vector(root, "root", r, index) != ozk.OZK_F32:
+            raise ValueError("root is float32")
         written.append(root)
-    _call(index, "ozk_rms_norm", r, c, x.data_ptr(), kind, ld, *to_residual, weight.data_ptr(), w_kind, eps, None if root is None else root.data_ptr(),
-          None if y is None else y.data_ptr(), ldy, *to_rows, *to_cols, _stream(index))
+    args = _NORM_ARGS.pack(r, c, x.data_ptr(), ld, *from_residual, weight.data_ptr(), 0 if root is None else root.data_ptr(), y_at, ldy, *to_rows, *to_cols, eps, kind, r_kind, w_kind)
+    _call(index, "ozk_rms_norm", args, _stream(index))
     if by_rows is rows and rows:
         _rewritten(rows)
     if by_cols is cols and cols:
@@ -410,22 +428,21 @@ def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, root: torch.Tensor,
     dy: the gradient of the answer; total, root: from rms_norm (total is x where there was no residual); dtotal: the gradient that reaches `total` from elsewhere, in its type."""
     r, c, kind, ld = _input(total)
     index = total.get_device()
-    _type(dy, "dy")
-    ldd = _beside(dy, "dy", total, (dy.dtype,))
+    dy_kind = _type(dy, "dy")
+    ldd = _beside(dy, "dy", r, c, index, dy.dtype)
     if _vector(root, "root", r, index) != ozk.OZK_F32:
         raise ValueError("root is float32")
     w_kind = _vector(weight, "weight", c, index)
-    to_dtotal = (None, 0) if dtotal is None else (dtotal.data_ptr(), _beside(dtotal, "dtotal", total, (total.dtype,)))
+    from_dtotal = (0, 0) if dtotal is None else (dtotal.data_ptr(), _beside(dtotal, "dtotal", r, c, index, total.dtype))
     dx = torch.empty(r, c, dtype=total.dtype, device=total.device)
+    dw, to_dw = None, (0, 0, 0)
     if need_weight:
         dw = torch.empty(c, dtype=torch.float32, device=total.device)
         size = _code(index, "ozk_rms_norm_backward_scratch_bytes", r, c)
         scratch = torch.empty(size, dtype=torch.uint8, device=total.device)
         to_dw = (dw.data_ptr(), scratch.data_ptr(), size)
-    else:
-        dw, to_dw = None, (None, None, 0)
-    _call(index, "ozk_rms_norm_backward", r, c, dy.data_ptr(), _TYPES[dy.dtype], ldd, total.data_ptr(), kind, ld, root.data_ptr(), weight.data_ptr(), w_kind, *to_dtotal,
-          dx.data_ptr(), max(c, 1), *to_dw, _stream(index))
+    args = _NORM_GRAD_ARGS.pack(r, c, dy.data_ptr(), ldd, total.data_ptr(), ld, root.data_ptr(), weight.data_ptr(), *from_dtotal, dx.data_ptr(), c or 1, *to_dw, dy_kind, kind, w_kind)
+    _call(index, "ozk_rms_norm_backward", args, _stream(index))
     return dx, dw
 
 
