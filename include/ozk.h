@@ -398,7 +398,7 @@ ozk_status ozk_get_workspace_status(void* workspace, void* stream);
  * residual NULL: h = x, and total is not used.  total may be the residual (same ld), or x where the types agree: the stream is updated in place.
  * The norm is of h as it is stored.  weight: cols numbers.  FP32 arithmetic, sums in an order that depends on the sizes alone.
  *   root       optional, rows floats: s, which the backward pass reads (wanted where col_codes are)
- *   y          optional, rows x cols: y without quantisation
+ *   y          optional, rows x cols: y without quantisation, not in the place of h
  *   row_codes, row_scales / col_codes, col_scales   optional: y by 1 x 128 / 128 x 1 blocks, as by ozk_fp8_quantize_lines
  * Mean squares beyond FP32 count as infinite (s = 0).  A NaN or an infinity in a row makes NaN of the row's y (0 of what is finite beside an infinity).
  * cols <= 32768.  rows, cols = 0 are allowed. */

@@ -8,223 +8,10 @@
 // Rows: a row lies over 1 to 16 warps, 512 columns (one word of scales) a warp and step.  A lane holds eight consecutive columns of each 256, or four of
 // each 128, so that 16 or 32 lanes hold a block.  Thread blocks stay and take row after row, the next ones already on their way to shared memory.
 // Columns: blocks run along the rows, so a second kernel reads h again, tile by tile, with s known.
-#include <type_traits>
-
-#include "ozk_fp8_product.cuh"
+#include "ozk_norm.cuh"
 
 namespace ozk {
 namespace {
-
-using namespace fp8;
-
-// ---- consecutive elements of a lane ---------------------------------------------------------
-constexpr int kGroup = 512;   // columns a warp holds at a time
-template <class T, int kL>
-struct Piece {
-  uint32_t w[kL * sizeof(T) / 4];
-};
-template <int kL>
-__device__ __forceinline__ float value(const Piece<__nv_bfloat16, kL>& q, int i) { return i % 2 ? bf16_hi(q.w[i / 2]) : bf16_lo(q.w[i / 2]); }
-template <int kL>
-__device__ __forceinline__ float value(const Piece<float, kL>& q, int i) { return __uint_as_float(q.w[i]); }
-// Two elements, rounded to the type.
-template <int kL>
-__device__ __forceinline__ void set2(Piece<__nv_bfloat16, kL>& q, int i, float a, float b) { q.w[i / 2] = pack_bf16(a, b); }
-template <int kL>
-__device__ __forceinline__ void set2(Piece<float, kL>& q, int i, float a, float b) { q.w[i] = __float_as_uint(a), q.w[i + 1] = __float_as_uint(b); }
-
-// What is read once need not stay in L1; not through the read-only path, because h may be written over x or r.
-template <int kBytes>
-__device__ __forceinline__ void load_bytes(const void* p, uint32_t* w) {
-  if constexpr (kBytes == 16) asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-  else if constexpr (kBytes == 8) asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-  else if constexpr (kBytes == 4) asm volatile("ld.global.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
-}
-template <int kBytes>
-__device__ __forceinline__ void store_bytes(void* p, const uint32_t* w) {
-  if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-  else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
-}
-__device__ __forceinline__ uint32_t load_16(const void* p) {
-  uint16_t v;
-  asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
-  return v;
-}
-// Bytes of one access: kE elements, as far as places and strides allow, and 16 bytes at most.
-template <class T, int kE>
-__host__ __device__ constexpr int access() { return kE * (int)sizeof(T) > 16 ? 16 : kE * (int)sizeof(T); }
-// BF16 rows at odd places: a lane's elements are cut from the 4-byte words that hold them.  The words at a row's ends hold a neighbour's element too, which
-// in the matrix's first and last rows (`edge`) may not be there: these two are read element by element.
-template <class T, int kE>
-__host__ __device__ constexpr bool odd_places() { return sizeof(T) == 2 && kE == 1; }
-__device__ __forceinline__ int at_odd(const void* p) { return (int)(reinterpret_cast<uintptr_t>(p) & 2); }
-template <int kWords>
-__device__ __forceinline__ void cut(const uint32_t* in, int odd, uint32_t* out) {
-#pragma unroll
-  for (int i = 0; i < kWords; ++i) out[i] = __funnelshift_r(in[i], in[i + 1], 8 * odd);
-}
-// The lane's elements from `p` on.  kFull: all belong to the row; otherwise `left` of them do, and the others are zero.
-template <bool kFull, int kE, class T, int kL>
-__device__ __forceinline__ void load_piece(const T* p, int left, bool edge, Piece<T, kL>& q) {
-  constexpr int kBytes = access<T, kE>(), kStep = kBytes / (int)sizeof(T);
-  if constexpr (odd_places<T, kE>()) {
-    if ((kFull || left >= kL) && !edge) {
-      const int odd = at_odd(p);
-      const char* from = reinterpret_cast<const char*>(p) - odd;
-      uint32_t w[kL / 2 + 1];
-#pragma unroll
-      for (int i = 0; i < kL / 2; ++i) load_bytes<4>(from + 4 * i, w + i);
-      w[kL / 2] = 0;
-      if (odd) load_bytes<4>(from + 2 * kL, w + kL / 2);
-      cut<kL / 2>(w, odd, q.w);
-      return;
-    }
-  } else if (kFull || left >= kL) {
-#pragma unroll
-    for (int i = 0; i < kL; i += kStep) load_bytes<kBytes>(p + i, q.w + i * (int)sizeof(T) / 4);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kL; ++i) {
-    if constexpr (sizeof(T) == 2) {
-      const uint32_t v = i < left ? load_16(p + i) : 0u;
-      q.w[i / 2] = i % 2 ? q.w[i / 2] | v << 16 : v;
-    } else {
-      q.w[i] = 0u;
-      if (i < left) load_bytes<4>(p + i, q.w + i);
-    }
-  }
-}
-template <bool kFull, int kE, class T, int kL>
-__device__ __forceinline__ void store_piece(T* p, int left, const Piece<T, kL>& q) {
-  constexpr int kBytes = access<T, kE>(), kStep = kBytes / (int)sizeof(T);
-  if (kFull || left >= kL) {
-    if constexpr (!odd_places<T, kE>()) {
-#pragma unroll
-      for (int i = 0; i < kL; i += kStep) store_bytes<kBytes>(p + i, q.w + i * (int)sizeof(T) / 4);
-    } else if (at_odd(p)) {
-      reinterpret_cast<uint16_t*>(p)[0] = (uint16_t)q.w[0];
-#pragma unroll
-      for (int i = 1; i < kL - 1; i += 2) *reinterpret_cast<uint32_t*>(p + i) = __funnelshift_r(q.w[i / 2], q.w[i / 2 + 1], 16);
-      reinterpret_cast<uint16_t*>(p)[kL - 1] = (uint16_t)(q.w[kL / 2 - 1] >> 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kL; i += 2) store_bytes<4>(p + i, q.w + i / 2);
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kL; ++i) {
-    if (i >= left) continue;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p + i) = (uint16_t)(q.w[i / 2] >> (16 * (i % 2)));
-    else store_bytes<4>(p + i, q.w + i);
-  }
-}
-// Weights: cols numbers of either type; a lane's are read together where the array is aligned for it.
-enum { kWeightBf16 = 1, kWeightLoose = 2 };
-template <bool kFull, int kL>
-__device__ __forceinline__ void load_weights(const void* w, int kind, int c, int left, float (&v)[kL]) {
-  if ((kFull || left >= kL) && !(kind & kWeightLoose)) {
-    if (kind & kWeightBf16) {
-      Piece<__nv_bfloat16, kL> q;
-      if constexpr (kL == 8) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(w) + c));
-        q.w[0] = u.x, q.w[1] = u.y, q.w[2] = u.z, q.w[3] = u.w;
-      } else {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(w) + c));
-        q.w[0] = u.x, q.w[1] = u.y;
-      }
-#pragma unroll
-      for (int i = 0; i < kL; ++i) v[i] = value(q, i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kL; i += 4) {
-        const float4 f = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + i));
-        v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kL; ++i)
-    v[i] = i >= left ? 0.f : kind & kWeightBf16 ? __bfloat162float(__ldg(static_cast<const __nv_bfloat16*>(w) + c + i)) : __ldg(static_cast<const float*>(w) + c + i);
-}
-
-// ---- rows on their way ----------------------------------------------------------------------
-// A thread copies its own elements of the rows it will see next to shared memory and reads back nobody else's, so that no barrier is needed, no
-// register holds what is in flight, and a row's reduction does not hold up the next one's loads.  A lane's elements that the row ends among are read directly.
-constexpr int kRingBytes = 200 << 10;   // of a multiprocessor's shared memory
-template <int kBytes>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-  if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(kBytes) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
-template <int kBytes>
-__device__ __forceinline__ void load_shared(uint32_t at, uint32_t* w) {
-  if constexpr (kBytes == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-  else if constexpr (kBytes == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
-  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
-}
-template <class T, int kL, int kE, int V, bool kWhole, bool kOn>
-struct Stream {
-  static constexpr bool kOdd = odd_places<T, kE>();
-  static constexpr int kBytes = kOdd ? 4 : access<T, kE>(), kStep = kBytes / (int)sizeof(T), kCopies = kL / kStep + (kOdd ? 1 : 0), kPieces = 16 / kL;
-  static constexpr int kThread = kOn ? V * kPieces * kCopies * kBytes : 0;   // bytes of a thread's share of a row
-  // Copy i of piece k of group v: the threads' copies lie side by side.
-  __device__ static __forceinline__ uint32_t place(uint32_t base, int v, int k, int i) { return base + (uint32_t)((((v * kPieces + k) * kCopies + i) * (int)blockDim.x) + (int)threadIdx.x) * kBytes; }
-  // row: the lane's first column in the row; group_left: columns of the row from the warp's group on.
-  __device__ static __forceinline__ void fetch(const T* row, uint32_t base, int step, int lane, int group_left, bool edge) {
-    if constexpr (kOn) {
-      const int odd = kOdd ? at_odd(row) : 0;
-      if (kOdd && edge) return;
-      const char* from = reinterpret_cast<const char*>(row) - odd;
-      auto copy = [&](int v, int k) {
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i)
-          if (!kOdd || i + 1 < kCopies || odd) copy_async<kBytes>(place(base, v, k, i), from + (int64_t)(v * step + k * 32 * kL) * (int)sizeof(T) + i * kBytes);
-      };
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int left = group_left - v * step;   // the same for all lanes
-        if (kWhole ? left > 0 : left >= kGroup) {
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) copy(v, k);
-        } else if (!kWhole && left > 0) {
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k)
-            if (left - k * 32 * kL - lane * kL >= kL) copy(v, k);
-        }
-      }
-    }
-  }
-  template <bool kFull>
-  __device__ static __forceinline__ void take(const T* row, uint32_t base, int at, int left, bool edge, int v, int k, Piece<T, kL>& out) {
-    if constexpr (kOn) {
-      if ((kFull || left >= kL) && !(kOdd && edge)) {
-        uint32_t w[kCopies * kBytes / 4];
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) load_shared<kBytes>(place(base, v, k, i), w + i * kBytes / 4);
-        if constexpr (kOdd) {
-          cut<kL / 2>(w, at_odd(row), out.w);
-        } else {
-#pragma unroll
-          for (int i = 0; i < kL * (int)sizeof(T) / 4; ++i) out.w[i] = w[i];
-        }
-        return;
-      }
-    }
-    load_piece<kFull, kE>(row + at, left, edge, out);
-  }
-};
-// Rows that are on their way for each thread block of `threads` that shares a multiprocessor with `blocks - 1` others.
-constexpr int ring_stages(int thread_bytes, int threads, int blocks) {
-  const int room = thread_bytes ? kRingBytes / blocks / (thread_bytes * threads) : 0;
-  return room > 2 ? 2 : room;
-}
 
 // ---- scales -----------------------------------------------------------------------------
 // Largest magnitude; NaN where one is not a number, whose bits are above all others'.
@@ -260,44 +47,6 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int left, const uint32_t
       if (i < left) p[i] = (uint8_t)(c[i / 4] >> (8 * (i % 4)));
   }
 }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-
-constexpr int kMostWarps = 16;
-constexpr int kMostCols = kGroup * kMostWarps * 4;
-constexpr int64_t kMostRows = INT32_MAX - 65536;   // row indexes are ints, with room for what lies ahead
-
-// How a row is laid over a thread block: `warps` a row, `rows` of them side by side, V groups of 512 columns a warp.
-struct Layout {
-  int warps, rows, v;
-};
-// Forward, a row's own cost (its sum, addresses, barriers) is shared by two groups a warp where there are rows enough to fill the GPU all the same (16384 x 4096: 82 us, one
-// group a warp 99); few rows have as many warps as they can use.  The backward pass, whose sums of dw take registers, is faster with one (108 us : 114).  `most`: groups a warp takes in thread blocks of eight warps; wider rows have thread blocks of 16.
-Layout row_layout(int64_t rows, int64_t cols, int most, bool forward) {
-  const int groups = (int)ceil_div(cols, kGroup);
-  int v = forward && groups > 1 && rows * groups >= (int64_t)device_sm_count() * 64 ? 2 : 1;
-  while (v < most && 8 * v < groups) v *= 2;
-  if (8 * v < groups) v = groups <= 32 ? 2 : 4;
-  const int warps = (int)ceil_div(groups, v);
-  return {warps, warps < 8 ? 8 / warps : 1, v};
-}
-constexpr int kNormMost = 4, kNormMostF32 = 2, kGradMost = 2;   // FP32 rows: what four groups hold leaves no room for the next row
-// Sum over the warps of this thread's row, the same in all of them.  `side` alternates, so that one barrier is enough.
-__device__ __forceinline__ float row_sum(float v, float (*part)[kMostWarps], int side, int warps, int warp) {
-  v = warp_sum(v);
-  if (warps == 1) return v;
-  if (threadIdx.x % 32 == 0) part[side][warp] = v;
-  __syncthreads();
-  const int i = threadIdx.x % 16;   // both halves of the warp alike
-  v = i < warps ? part[side][warp / warps * warps + i] : 0.f;
-#pragma unroll
-  for (int d = 8; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-  return v;
-}
-
 struct NormParams {
   const void *x, *r, *w;
   void *h, *y;
@@ -619,230 +368,7 @@ __global__ void __launch_bounds__(256, sizeof(TH) == 2 ? 3 : 2) norm_cols_kernel
     norm_cols_tile<TH, kL, kE, false>(H, ldh, root, W, w_kind, rows, cols, Q, ldq, S, part, recips, roots, tr, tc, tiles_r);
 }
 
-// ---- gradients --------------------------------------------------------------------------
-struct GradParams {
-  const void *dy, *h, *dh, *w;
-  void* dx;
-  const float* root;
-  int64_t lddy, ldh, lddh, lddx;
-  int rows, cols, w_kind, warps, side_rows;
-  float inv_cols;
-  float* parts;   // [grid x side_rows][cols], or NULL
-};
-
-template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
-struct GradShape {
-  static constexpr int kBlocks = kThreads == 512 ? 1 : V == 1 && sizeof(TD) + sizeof(TH) == 4 ? 3 : 2;
-  template <bool kOn>
-  static constexpr int bytes() { return Stream<TD, kL, kE, V, kWhole, kOn>::kThread + 2 * Stream<TH, kL, kE, V, kWhole, kOn>::kThread; }
-  static constexpr int kStages = ring_stages(bytes<true>(), kThreads, kBlocks);
-  static constexpr bool kOn = kStages > 0;
-  static constexpr int kThreadBytes = bytes<kOn>();
-  // Room for one row only: dy and h stay in registers, so that the next row's may follow before this one's sum is known.
-  static constexpr bool kHold = kStages == 1 && V <= 2 && kE > 1;
-};
-
-// Rows as in the forward pass; what is needed again after the sum is read again from shared memory.  Each thread adds up its
-// columns' share of dw over the rows it sees; norm_dw_kernel adds the thread blocks' sums.
-template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
-__global__ void __launch_bounds__(kThreads, GradShape<TD, TH, kL, kE, V, kThreads, kWhole>::kBlocks) norm_backward_kernel(const __grid_constant__ GradParams p) {
-  using S = GradShape<TD, TH, kL, kE, V, kThreads, kWhole>;
-  using SD = Stream<TD, kL, kE, V, kWhole, S::kOn>;
-  using SH = Stream<TH, kL, kE, V, kWhole, S::kOn>;
-  constexpr int kSlots = S::kOn ? S::kStages : 1, kPieces = 16 / kL;
-  extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float part[2][kMostWarps];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, in_row = warp % p.warps, step = p.warps * kGroup;
-  const int c_warp = in_row * kGroup, c_lane = c_warp + lane * kL, group_left = p.cols - c_warp;
-  const int first = (int)blockIdx.x * p.side_rows + warp / p.warps, stride = (int)gridDim.x * p.side_rows;
-  const uint32_t slot_bytes = S::kThreadBytes * blockDim.x, h_at = SD::kThread * blockDim.x, e_at = h_at + SH::kThread * blockDim.x, ring_at = smem_u32(ring);
-  int row = first, ahead = first;   // the row at hand, and the next to be fetched
-  const int64_t d_step = stride * p.lddy, h_step = stride * p.ldh, e_step = stride * p.lddh, o_step = stride * p.lddx;
-  const TD *pd = static_cast<const TD*>(p.dy) + row * p.lddy + c_lane, *d_ahead = pd;
-  const TH *ph = static_cast<const TH*>(p.h) + row * p.ldh + c_lane, *h_ahead = ph, *pe = p.dh ? static_cast<const TH*>(p.dh) + row * p.lddh + c_lane : nullptr, *e_ahead = pe;
-  TH* po = static_cast<TH*>(p.dx) + row * p.lddx + c_lane;
-  auto fetch = [&](int slot) {
-    if constexpr (S::kOn) {
-      if (ahead < p.rows) {
-        const bool edge = ahead == 0 || ahead == p.rows - 1;
-        SD::fetch(d_ahead, ring_at + slot * slot_bytes, step, lane, group_left, edge);
-        SH::fetch(h_ahead, ring_at + slot * slot_bytes + h_at, step, lane, group_left, edge);
-        if (pe) SH::fetch(e_ahead, ring_at + slot * slot_bytes + e_at, step, lane, group_left, edge);
-      }
-      copy_commit();
-      ahead += stride, d_ahead += d_step, h_ahead += h_step;
-      if (pe) e_ahead += e_step;
-    }
-  };
-  // With one slot: dy and h of the next row once this one's are in registers, dh after it has been written.
-  auto fetch_early = [&]() {
-    if (ahead < p.rows) {
-      const bool edge = ahead == 0 || ahead == p.rows - 1;
-      SD::fetch(d_ahead, ring_at, step, lane, group_left, edge);
-      SH::fetch(h_ahead, ring_at + h_at, step, lane, group_left, edge);
-    }
-    d_ahead += d_step, h_ahead += h_step;
-  };
-  auto fetch_late = [&]() {
-    if (pe && ahead < p.rows) SH::fetch(e_ahead, ring_at + e_at, step, lane, group_left, ahead == 0 || ahead == p.rows - 1);
-    if (pe) e_ahead += e_step;
-    copy_commit();
-    ahead += stride;
-  };
-  if constexpr (S::kHold) {
-    fetch_early();
-    fetch_late();
-  } else {
-#pragma unroll
-    for (int k = 0; k < kSlots; ++k) fetch(k);
-  }
-  Piece<TD, kL> d_held[S::kHold ? V : 1][kPieces];
-  Piece<TH, kL> h_held[S::kHold ? V : 1][kPieces];
-  float dw[V][kPieces][kL];
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-#pragma unroll
-      for (int i = 0; i < kL; ++i) dw[v][k][i] = 0.f;
-  const int rounds = (p.rows - (int)blockIdx.x * p.side_rows + stride - 1) / stride;   // the same for all threads: they meet at barriers
-  int slot = 0;
-  float s = row < p.rows ? p.root[row] : 0.f;
-  for (int n = 0; n < rounds; ++n) {
-    const bool live = row < p.rows, edge = row == 0 || row == p.rows - 1;
-    const float s_next = row + stride < p.rows ? p.root[row + stride] : 0.f;
-    const uint32_t base = ring_at + slot * slot_bytes;
-    float sum = 0.f;
-    // Group v of the row, before the sum is known (adds to dw and to the sum) and after (writes dx).
-    auto look = [&](auto full, int v, int left) {
-      constexpr bool kFull = decltype(full)::value;
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k) {
-        const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
-        Piece<TD, kL> d_now, &d = S::kHold ? d_held[S::kHold ? v : 0][k] : d_now;
-        Piece<TH, kL> h_now, &h = S::kHold ? h_held[S::kHold ? v : 0][k] : h_now;
-        SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
-        SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
-        float w[kL];
-        load_weights<kFull, kL>(p.w, p.w_kind, c_lane + at, rest, w);
-#pragma unroll
-        for (int i = 0; i < kL; ++i) {
-          const float hn = value(h, i) * s;
-          dw[v][k][i] = fmaf(value(d, i), hn, dw[v][k][i]);
-          sum = fmaf(value(d, i) * w[i], hn, sum);
-        }
-      }
-    };
-    auto write = [&](auto full, int v, int left, float minus_mean) {
-      constexpr bool kFull = decltype(full)::value;
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k) {
-        const int at = v * step + k * 32 * kL, rest = left - k * 32 * kL;
-        Piece<TD, kL> d;
-        Piece<TH, kL> h, e = {}, out;
-        if constexpr (S::kHold) {
-          d = d_held[v][k], h = h_held[v][k];
-        } else {
-          SD::template take<kFull>(pd, base, at, rest, edge, v, k, d);
-          SH::template take<kFull>(ph, base + h_at, at, rest, edge, v, k, h);
-        }
-        if (pe) SH::template take<kFull>(pe, base + e_at, at, rest, edge, v, k, e);
-        float w[kL], dx[kL];
-        load_weights<kFull, kL>(p.w, p.w_kind, c_lane + at, rest, w);
-#pragma unroll
-        for (int i = 0; i < kL; ++i) dx[i] = fmaf(s, fmaf(value(h, i) * s, minus_mean, value(d, i) * w[i]), value(e, i));
-#pragma unroll
-        for (int i = 0; i < kL; i += 2) set2(out, i, dx[i], dx[i + 1]);
-        store_piece<kFull, kE>(po + at, rest, out);
-      }
-    };
-    if constexpr (S::kOn) copy_wait<kSlots - 1>();
-    if (live) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int left = group_left - v * step;
-        if (left <= 0) continue;
-        if constexpr (kWhole) look(std::true_type{}, v, left - lane * kL);
-        else if (left >= kGroup) look(std::true_type{}, v, left - lane * kL);
-        else look(std::false_type{}, v, left - lane * kL);
-      }
-    }
-    if constexpr (S::kHold) fetch_early();
-    sum = row_sum(sum, part, n & 1, p.warps, warp);
-    if (live) {
-      const float minus_mean = -sum * p.inv_cols;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int left = group_left - v * step;
-        if (left <= 0) continue;
-        if constexpr (kWhole) write(std::true_type{}, v, left - lane * kL, minus_mean);
-        else if (left >= kGroup) write(std::true_type{}, v, left - lane * kL, minus_mean);
-        else write(std::false_type{}, v, left - lane * kL, minus_mean);
-      }
-    }
-    if constexpr (S::kHold) {
-      fetch_late();
-    } else {
-      fetch(slot);
-      slot = slot + 1 == kSlots ? 0 : slot + 1;
-    }
-    s = s_next;
-    row += stride, pd += d_step, ph += h_step, po += o_step;
-    if (pe) pe += e_step;
-  }
-  if (!p.parts) return;
-  float* mine = p.parts + (int64_t)first * p.cols;   // the first row that this warp saw names its sums
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-#pragma unroll
-      for (int i = 0; i < kL; ++i) {
-        const int c = c_lane + v * step + k * 32 * kL + i;
-        if (c < p.cols) mine[c] = dw[v][k][i];
-      }
-}
-
-// dw = the thread blocks' sums, added in a fixed order: 32 columns and 32 strands of rows a thread block.
-__global__ void __launch_bounds__(1024) norm_dw_kernel(const float* parts, int count, int cols, float* dw) {
-  __shared__ float strand[32][33];
-  const int lane = threadIdx.x % 32, s = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
-  float sum = 0.f;
-  if (c < cols) {
-#pragma unroll 8
-    for (int i = s; i < count; i += 32) sum += parts[(int64_t)i * cols + c];
-  }
-  strand[s][lane] = sum;
-  __syncthreads();
-  const float v = warp_sum(strand[lane][s]);   // warp s joins the strands of column s
-  if (lane == 0 && blockIdx.x * 32 + s < cols) dw[blockIdx.x * 32 + s] = v;
-}
-
 // ---- host side ----------------------------------------------------------------------------
-bool type_ok(int t) { return t == OZK_F32 || t == OZK_BF16; }
-int type_size(int t) { return t == OZK_F32 ? 4 : 2; }
-bool on(const void* p, int size) { return p && (reinterpret_cast<uintptr_t>(p) & (size - 1)) == 0; }
-// How many elements a row's place and stride let be read together: 16 bytes at most; 8, 4 or 1.
-int together(const void* p, int64_t ld, int size) {
-  for (int n = size == 2 ? 8 : 4; n > 2; n /= 2)
-    if ((reinterpret_cast<uintptr_t>(p) & (n * size - 1)) == 0 && ld % n == 0) return n;
-  return 1;
-}
-int least(int a, int b) { return a < b ? a : b; }
-// Lanes take eight columns where all is BF16 and aligned; FP32 comes in 16-byte accesses of four.
-template <class TX, class TR>
-constexpr bool kAllBf16 = sizeof(TX) == 2 && !std::is_same<TR, float>::value;
-
-int weight_kind(const void* w, int type) { return (type == OZK_BF16 ? kWeightBf16 : 0) | (aligned16(w) ? 0 : kWeightLoose); }
-
-// Thread blocks of a persistent kernel: what runs at once, or what there is to do.
-// `blocks` of them share a multiprocessor where they have 256 or 512 threads, more where they have fewer.
-int grid_of(int64_t rows, const Layout& l, int blocks) {
-  const int warps = l.warps * l.rows;
-  const int64_t need = ceil_div(rows, l.rows), room = (int64_t)device_sm_count() * (warps <= 8 ? blocks * 8 / warps : blocks);
-  return (int)(need < room ? need : room);
-}
-
 template <class TX, class TR, int kL, int kE, int V, int kThreads, bool kWhole>
 bool launch_norm_rows_as(const NormParams& p, const Layout& l, cudaStream_t st) {
   using S = NormShape<TX, TR, kL, kE, V, kThreads, kWhole>;
@@ -885,33 +411,6 @@ void launch_norm_cols(int e, const void* h, int64_t ldh, const NormParams& p, ui
   }
   if (e >= 4) launch_norm_cols<TH, 4, 4>(h, ldh, p, q, ldq, s, st); else launch_norm_cols<TH, 4, 1>(h, ldh, p, q, ldq, s, st);
 }
-constexpr int kGradBlocks = 3;   // a multiprocessor, at most: what the scratch of the partial sums is for
-template <class TD, class TH, int kL, int kE, int V, int kThreads, bool kWhole>
-bool launch_backward_as(const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
-  using S = GradShape<TD, TH, kL, kE, V, kThreads, kWhole>;
-  static_assert(S::kBlocks <= kGradBlocks, "room for partial sums");
-  static std::atomic<bool> done[kMaxDevices];
-  auto kernel = norm_backward_kernel<TD, TH, kL, kE, V, kThreads, kWhole>;
-  if (!raise_smem(kernel, (size_t)S::kStages * S::kThreadBytes * kThreads, done)) return false;
-  const unsigned threads = (unsigned)(32 * l.warps * l.rows);
-  *grid = grid_of(p.rows, l, S::kBlocks);
-  kernel<<<(unsigned)*grid, threads, (size_t)S::kStages * S::kThreadBytes * threads, st>>>(p);
-  return cudaGetLastError() == cudaSuccess;
-}
-template <class TD, class TH, int kL, int kE, bool kWhole>
-bool launch_backward(const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
-  if (l.warps <= 8) return l.v == 1 ? launch_backward_as<TD, TH, kL, kE, 1, 256, kWhole>(p, l, grid, st) : launch_backward_as<TD, TH, kL, kE, 2, 256, kWhole>(p, l, grid, st);
-  return l.v == 2 ? launch_backward_as<TD, TH, kL, kE, 2, 512, kWhole>(p, l, grid, st) : launch_backward_as<TD, TH, kL, kE, 4, 512, kWhole>(p, l, grid, st);
-}
-template <class TD, class TH>
-bool launch_backward(int e, const GradParams& p, const Layout& l, int* grid, cudaStream_t st) {
-  if constexpr (kAllBf16<TD, TH>) {
-    if (e == 8) return p.cols % kGroup == 0 ? launch_backward<TD, TH, 8, 8, true>(p, l, grid, st) : launch_backward<TD, TH, 8, 8, false>(p, l, grid, st);
-  } else {
-    if (e >= 4 && p.cols % kGroup == 0) return launch_backward<TD, TH, 4, 4, true>(p, l, grid, st);
-  }
-  return e >= 4 ? launch_backward<TD, TH, 4, 4, false>(p, l, grid, st) : launch_backward<TD, TH, 4, 1, false>(p, l, grid, st);
-}
 
 }  // namespace
 }  // namespace ozk
@@ -932,10 +431,11 @@ ozk_status ozk_rms_norm(const ozk_rms_norm_args* args, void* stream) {
   if (rows == 0 || cols == 0) return OZK_OK;
   const int h_type = R ? a.residual_type : a.x_type, xs = type_size(a.x_type), hs = type_size(h_type);
   if (!on(X, xs) || !on(a.weight, type_size(a.weight_type)) || (R && (!on(R, hs) || !on(a.total, hs)))) return OZK_ERR_INVALID_ARG;
-  if (a.y && (!on(a.y, xs) || a.ldy < cols)) return OZK_ERR_INVALID_ARG;
+  if (a.y && (!on(a.y, xs) || a.ldy < cols || a.y == (R ? a.total : X))) return OZK_ERR_INVALID_ARG;   // what is normed is read again for the columns
   if ((a.root && !on(a.root, 4)) || (by_cols && !a.root)) return OZK_ERR_INVALID_ARG;
   if (by_rows && (!a.row_codes || !a.row_scales || !aligned16(a.row_codes) || a.row_ld % 16 || a.row_ld < cols || !on(a.row_scales, 4))) return OZK_ERR_INVALID_ARG;
   if (by_cols && (!a.col_codes || !a.col_scales || !aligned16(a.col_codes) || a.col_ld % 16 || a.col_ld < cols)) return OZK_ERR_INVALID_ARG;
+  if (by_cols && ceil_div(rows, kBlock) * ceil_div(cols, kBlock) > INT32_MAX) return OZK_ERR_UNSUPPORTED;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const Layout l = row_layout(rows, cols, h_type == OZK_F32 ? kNormMostF32 : kNormMost, true);
@@ -944,9 +444,10 @@ ozk_status ozk_rms_norm(const ozk_rms_norm_args* args, void* stream) {
   p.ldx = a.ldx, p.ldr = a.ldr, p.ldh = a.ldt, p.ldy = a.ldy, p.ldq = a.row_ld;
   p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(a.weight, a.weight_type), p.warps = l.warps, p.side_rows = l.rows;
   p.eps = (float)a.eps, p.inv_cols = 1.f / (float)cols, p.root = a.root, p.codes = a.row_codes, p.scales = reinterpret_cast<uint32_t*>(a.row_scales);
-  int vec = together(X, a.ldx, xs);
-  if (R) vec = least(vec, least(together(R, a.ldr, hs), together(a.total, a.ldt, hs)));
-  if (a.y) vec = least(vec, together(a.y, a.ldy, xs));
+  const int64_t more = rows > 1;   // a single row's stride does not matter
+  int vec = together(X, more * a.ldx, xs);
+  if (R) vec = least(vec, least(together(R, more * a.ldr, hs), together(a.total, more * a.ldt, hs)));
+  if (a.y) vec = least(vec, together(a.y, more * a.ldy, xs));
   bool ok;
   if (a.x_type == OZK_BF16)
     ok = !R ? launch_norm_rows<__nv_bfloat16, None>(vec, p, l, st)
@@ -957,53 +458,8 @@ ozk_status ozk_rms_norm(const ozk_rms_norm_args* args, void* stream) {
   if (by_cols) {
     const void* h = R ? a.total : X;
     const int64_t ld = R ? a.ldt : a.ldx;
-    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(together(h, ld, 2), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
-    else launch_norm_cols<float>(together(h, ld, 4), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
-    if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
-  }
-  return OZK_OK;
-}
-
-size_t ozk_rms_norm_backward_scratch_bytes(int64_t rows, int64_t cols) {
-  if (rows <= 0 || cols <= 0 || cols > kMostCols) return 0;
-  const Layout l = row_layout(rows, cols, kGradMost, false);
-  return (size_t)grid_of(rows, l, kGradBlocks) * l.rows * (size_t)cols * 4;
-}
-
-ozk_status ozk_rms_norm_backward(const ozk_rms_norm_backward_args* args, void* stream) {
-  if (!args) return OZK_ERR_INVALID_ARG;
-  const ozk_rms_norm_backward_args& a = *args;
-  const int64_t rows = a.rows, cols = a.cols;
-  if (rows < 0 || cols < 0 || !type_ok(a.dy_type) || !type_ok(a.total_type) || !type_ok(a.weight_type) || a.lddy < cols || a.ldt < cols || a.lddx < cols) return OZK_ERR_INVALID_ARG;
-  if (a.dtotal && a.lddt < cols) return OZK_ERR_INVALID_ARG;
-  if (rows > kMostRows || cols > kMostCols) return OZK_ERR_UNSUPPORTED;
-  if (cols == 0) return OZK_OK;
-  if (a.dweight && !on(a.dweight, 4)) return OZK_ERR_INVALID_ARG;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (rows == 0) return !a.dweight || cudaMemsetAsync(a.dweight, 0, (size_t)cols * 4, st) == cudaSuccess ? OZK_OK : OZK_ERR_CUDA;
-  const int ds = type_size(a.dy_type), hs = type_size(a.total_type);
-  if (!on(a.dy, ds) || !on(a.total, hs) || !on(a.root, 4) || !on(a.weight, type_size(a.weight_type)) || !on(a.dx, hs) || (a.dtotal && !on(a.dtotal, hs))) return OZK_ERR_INVALID_ARG;
-  if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
-  const Layout l = row_layout(rows, cols, kGradMost, false);
-  if (a.dweight && (!on(a.scratch, 16) || a.scratch_bytes < ozk_rms_norm_backward_scratch_bytes(rows, cols))) return OZK_ERR_WORKSPACE;
-  GradParams p = {};
-  p.dy = a.dy, p.h = a.total, p.dh = a.dtotal, p.w = a.weight, p.dx = a.dx, p.root = a.root;
-  p.lddy = a.lddy, p.ldh = a.ldt, p.lddh = a.lddt, p.lddx = a.lddx;
-  p.rows = (int)rows, p.cols = (int)cols, p.w_kind = weight_kind(a.weight, a.weight_type), p.warps = l.warps, p.side_rows = l.rows;
-  p.inv_cols = 1.f / (float)cols;
-  p.parts = a.dweight ? static_cast<float*>(a.scratch) : nullptr;
-  int vec = least(least(together(a.dy, a.lddy, ds), together(a.total, a.ldt, hs)), together(a.dx, a.lddx, hs));
-  if (a.dtotal) vec = least(vec, together(a.dtotal, a.lddt, hs));
-  int grid = 0;
-  bool ok;
-  if (a.dy_type == OZK_BF16)
-    ok = a.total_type == OZK_BF16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<__nv_bfloat16, float>(vec, p, l, &grid, st);
-  else
-    ok = a.total_type == OZK_BF16 ? launch_backward<float, __nv_bfloat16>(vec, p, l, &grid, st) : launch_backward<float, float>(vec, p, l, &grid, st);
-  if (!ok) return OZK_ERR_CUDA;
-  if (a.dweight) {
-    const int64_t parts = rows < (int64_t)grid * l.rows ? rows : (int64_t)grid * l.rows;
-    norm_dw_kernel<<<(unsigned)ceil_div(cols, 32), 1024, 0, st>>>(p.parts, (int)parts, p.cols, a.dweight);
+    if (h_type == OZK_BF16) launch_norm_cols<__nv_bfloat16>(together(h, more * ld, 2), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
+    else launch_norm_cols<float>(together(h, more * ld, 4), h, ld, p, a.col_codes, a.col_ld, a.col_scales, st);
     if (cudaGetLastError() != cudaSuccess) return OZK_ERR_CUDA;
   }
   return OZK_OK;

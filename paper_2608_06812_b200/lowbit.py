@@ -371,7 +371,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
              root: "bool | torch.Tensor | None" = False) -> Normed:
     """The RMS norm of x + residual, times `weight` [cols], as operands of the products: h = x + residual, s = 1 / sqrt(mean(h^2) + eps), h s weight.
     x [rows, cols] float32 or bfloat16; residual of the same type or float32, and h is rounded to it before it is normed.
-    `rows`, `cols`: as for quantize_lines; `y`: whether (or where) the answer is wanted in the type of x too; `total`: where h is written (a new tensor if
+    `rows`, `cols`: as for quantize_lines; `y`: whether (or where, but for the place of what is normed) the answer is wanted in the type of x too; `total`: where h is written (a new tensor if
     None; may be `residual`, or x if of one type); `root`: whether (or where) s is wanted, float32 [rows], for rms_norm_backward."""
     r, c, kind, ld = _input(x)
     index = x.get_device()
@@ -404,6 +404,8 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         y = None
     else:
         y_at, ldy = y.data_ptr(), _beside(y, "y", r, c, index, x.dtype)
+        if y_at and y_at == total.data_ptr():
+            raise ValueError("y does not take the place of what is normed")
         written.append(y)
     if root is None or root is False or root is True:
         root = torch.empty(r, dtype=torch.float32, device=x.device) if root or by_cols is not None else None

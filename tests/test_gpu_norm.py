@@ -119,6 +119,26 @@ def test_the_stream_is_updated_in_place():
         check_forward(kept[0], w, kept[1], n, 1e-6)
 
 
+def test_the_answer_does_not_take_the_place_of_what_is_normed():
+    """The columns' codes are formed from it after the answer has been written; the place of x is free once the stream has it."""
+    x, r, w = make(140, 300, BF16, 1), make(140, 300, BF16, 2), make(1, 300, F32, 3)[0]
+    for arguments in (dict(y=x), dict(residual=r, total=r, y=r), dict(residual=r, total=x, y=x)):
+        with pytest.raises(ValueError, match="place"):
+            lowbit.rms_norm(x, w, **arguments)
+    kept = x.clone()
+    check_forward(kept, w, r, lowbit.rms_norm(x, w, r, rows=True, cols=True, y=x, root=True), 1e-6)
+
+
+@pytest.mark.parametrize("cols", [4096, 4097, 4100, 515])
+def test_a_single_row_at_any_place(cols):
+    for offset in (0, 1, 4):
+        x, r = make(1, cols, BF16, 1, pad=3, offset=offset), make(1, cols, F32, 2, pad=1, offset=offset)
+        w = make(1, cols, BF16, 3)[0]
+        n = lowbit.rms_norm(x, w, r, cols=True, y=True, root=True)
+        check_forward(x, w, r, n, 1e-6)
+        check_backward(n.y, n.total, n.root, w, r, lowbit.rms_norm_backward(n.y, n.total, n.root, w, r))
+
+
 def test_zeros_infinities_and_nan():
     rows, cols = 9, 700
     x = make(rows, cols, F32, 1)

@@ -23,7 +23,7 @@ def norm_args(**changes):
 
 @pytest.mark.parametrize("changes", [dict(rows=-1), dict(cols=-1), dict(ldx=63), dict(x_type=2), dict(weight_type=-1), dict(eps=-1e-6), dict(eps=float("nan")), dict(x=None), dict(x=P + 1), dict(weight=None),
                                      dict(weight=P + 2), dict(root=P + 2), dict(residual=P, ldr=64, ldt=64), dict(residual=P, ldr=63, total=P, ldt=64), dict(residual=P, ldr=64, total=P, ldt=1),
-                                     dict(residual=P, ldr=64, total=P, ldt=64, residual_type=3), dict(y=P, ldy=63), dict(y=P + 1, ldy=64), dict(row_codes=P + 8), dict(row_ld=72), dict(row_ld=48), dict(row_scales=None),
+                                     dict(residual=P, ldr=64, total=P, ldt=64, residual_type=3), dict(y=P, ldy=63), dict(y=P, ldy=64), dict(y=P + 1, ldy=64), dict(residual=P, ldr=64, total=P + 64, ldt=64, residual_type=ozk.OZK_BF16, y=P + 64, ldy=64), dict(row_codes=P + 8), dict(row_ld=72), dict(row_ld=48), dict(row_scales=None),
                                      dict(row_codes=None), dict(row_scales=P + 2), dict(root=None, col_codes=P, col_ld=64, col_scales=P), dict(col_codes=P, col_ld=64), dict(col_codes=P, col_ld=65, col_scales=P)])
 def test_norm_arguments(changes):
     assert ozk.ozk_rms_norm(norm_args(**changes)) == ozk.OZK_ERR_INVALID_ARG
