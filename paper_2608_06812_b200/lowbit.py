@@ -26,6 +26,7 @@ through libozk.so; arguments are checked here (ValueError) and in the library (O
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 from typing import NamedTuple
 
@@ -424,6 +425,11 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     return Normed(by_rows, by_cols, y, total, root)
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_scratch(index: int, rows: int, cols: int) -> int:
+    return _code(index, "ozk_rms_norm_backward_scratch_bytes", rows, cols)
+
+
 def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, root: torch.Tensor, weight: torch.Tensor, dtotal: torch.Tensor | None = None,
                       need_weight: bool = True) -> tuple[torch.Tensor, torch.Tensor | None]:
     """Gradients of rms_norm: (that of x and of the residual, in the type of `total`; that of the weight, float32, if wanted).
@@ -440,7 +446,7 @@ def rms_norm_backward(dy: torch.Tensor, total: torch.Tensor, root: torch.Tensor,
     dw, to_dw = None, (0, 0, 0)
     if need_weight:
         dw = torch.empty(c, dtype=torch.float32, device=total.device)
-        size = _code(index, "ozk_rms_norm_backward_scratch_bytes", r, c)
+        size = _norm_scratch(index, r, c)
         scratch = torch.empty(size, dtype=torch.uint8, device=total.device)
         to_dw = (dw.data_ptr(), scratch.data_ptr(), size)
     args = _NORM_GRAD_ARGS.pack(r, c, dy.data_ptr(), ldd, total.data_ptr(), ld, root.data_ptr(), weight.data_ptr(), *from_dtotal, dx.data_ptr(), c or 1, *to_dw, dy_kind, kind, w_kind)
