@@ -391,8 +391,11 @@ bool launch_norm_rows(const NormParams& p, const Layout& l, cudaStream_t st) {
     }
     return launch_norm_rows_as<TX, TR, kL, kE, 4, 512, kWhole>(p, l, st);
   }
-  return l.v == 1 ? launch_norm_rows_as<TX, TR, kL, kE, 1, 256, kWhole>(p, l, st)
-                  : l.v == 2 ? launch_norm_rows_as<TX, TR, kL, kE, 2, 256, kWhole>(p, l, st) : launch_norm_rows_as<TX, TR, kL, kE, 4, 256, kWhole>(p, l, st);
+  if (l.v == 1) return launch_norm_rows_as<TX, TR, kL, kE, 1, 256, kWhole>(p, l, st);
+  if constexpr (sizeof(typename Stored<TX, TR>::type) == 2) {
+    if (l.v == 4) return launch_norm_rows_as<TX, TR, kL, kE, 4, 256, kWhole>(p, l, st);
+  }
+  return launch_norm_rows_as<TX, TR, kL, kE, 2, 256, kWhole>(p, l, st);
 }
 template <class TX, class TR>
 bool launch_norm_rows(int e, const NormParams& p, const Layout& l, cudaStream_t st) {

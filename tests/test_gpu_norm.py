@@ -139,6 +139,24 @@ def test_a_single_row_at_any_place(cols):
         check_backward(n.y, n.total, n.root, w, r, lowbit.rms_norm_backward(n.y, n.total, n.root, w, r))
 
 
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32)], ids=["bf16", "bf16_f32", "f32"])
+def test_the_stream_of_any_bits(types):
+    """Every kind of number: subnormal, both zeros, infinities, NaN; sums as torch's, rounded once."""
+    g = torch.Generator().manual_seed(0)
+    bits = lambda d: torch.randint(-2 ** 15, 2 ** 15, (64, 2048), generator=g, dtype=torch.int16).view(BF16).to(d).cuda()  # noqa: E731
+    x, r = bits(types[0]), bits(types[1])
+    r[::2] = torch.where(torch.rand(32, 2048, generator=g).cuda() < 0.5, -x[::2].to(types[1]), x[::2].to(types[1]))   # what cancels
+    x[:4] *= 1e-36
+    r[:4] *= 1e-36
+    for shift in (0, 1):   # rows at even and odd places
+        a, b = x[:, shift:], r[:, shift:]
+        total = lowbit.rms_norm(a, torch.ones(2048 - shift, device="cuda"), b, rows=False).total
+        want = (a.float() + b.float()).to(types[1])
+        assert torch.equal(total.isnan(), want.isnan())
+        same = total.view(torch.int16 if types[1] is BF16 else torch.int32) == want.view(torch.int16 if types[1] is BF16 else torch.int32)
+        assert (same | want.isnan()).all()
+
+
 def test_zeros_infinities_and_nan():
     rows, cols = 9, 700
     x = make(rows, cols, F32, 1)
