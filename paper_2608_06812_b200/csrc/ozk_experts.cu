@@ -10,7 +10,8 @@
 //
 // In experts_pair_kernel the WEIGHTS' lines are the 256 rows of the instruction and the tokens its columns, 32 to 224 of them: a segment of any length is
 // divided into tiles of nearly equal width, so that a short one costs what it holds and not a tile of 256.  Two accumulators of 224 columns and the scale words fit tensor
-// memory side by side.  Results leave from registers, row by row of C, 64 bytes a warp: no row of another segment is touched.
+// memory side by side.  Results leave row by row of C, 64 bytes a warp, BF16 ones in pieces of 16 bytes a lane by way of shared memory (K = 500: 71 us, pairs of columns from
+// registers 118; level from K = 2048 on): no row of another segment is touched.
 // Measured in bursts: 16384 rows of 16 uneven experts, 4096 -> 4096, 240 us (2.3 PFLOP/s; twelve equal ones 2.5, the product with one matrix 2.8), bound by the tensor cores, by
 // the traffic of narrower tiles, and back to back by the power limit (280 us); 9001 rows of 24 experts, 2048 -> 4096, 92 us, and 131 us where the
 // weights' rows are not whole 128-byte lines (2056).  244 rows of 32 experts, 4096 -> 2048, 47 us (5.0 TB/s, memory).  Weight gradients of 16 experts, 4096 x 2048 from 16384
@@ -44,7 +45,7 @@ struct ExpertParams {
   int64_t ldc;
   int N, tiles_n, groups;
   int chunk;               // blocks summed in tensor memory before the sum is added to C in FP32, a multiple of 4
-  int pairs_ok, wide_ok;   // BF16 results may be stored two or four at a time
+  int pairs_ok, wide_ok, pieces_ok;   // BF16 results may be stored two, four or eight at a time
   int clear;               // rows outside the segments become zero
   StatusBlock* status;
 };
@@ -65,7 +66,8 @@ constexpr int kScaleCol = 480;   // two sets of 4 columns for one operand, 8 for
 struct ExpertShape {
   static constexpr int kWBytes = 128 * kBlock, kXBytes = kTokens / 2 * kBlock;
   static constexpr int kStageBytes = kWBytes + kXBytes;
-  static size_t smem(int experts) { return (size_t)kPairStages * kStageBytes + 512 + (size_t)(3 * experts + 1) * 4 + 1024; }
+  static constexpr int kStaging = kEpilogueWarps * 2048;   // 32 rows of 32 BF16 results a warp
+  static size_t smem(int experts) { return (size_t)kPairStages * kStageBytes + kStaging + 512 + (size_t)(3 * experts + 1) * 4 + 1024; }
 };
 
 // The table of segments: where each begins and ends, and how many tiles of at most kTokens rows lie before it.  By one warp.  Offsets are held within the
@@ -151,8 +153,9 @@ experts_pair_kernel(const __grid_constant__ ExpertMaps maps, const __grid_consta
   using S = ExpertShape;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  ExpertShared* sh = reinterpret_cast<ExpertShared*>(tiles + kPairStages * S::kStageBytes);
-  int* before = reinterpret_cast<int*>(tiles + kPairStages * S::kStageBytes + 512);
+  uint8_t* staging = tiles + kPairStages * S::kStageBytes;
+  ExpertShared* sh = reinterpret_cast<ExpertShared*>(staging + S::kStaging);
+  int* before = reinterpret_cast<int*>(staging + S::kStaging + 512);
   int *begin = before + p.experts + 1, *end = begin + p.experts;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)cluster_ctarank();
@@ -318,6 +321,33 @@ experts_pair_kernel(const __grid_constant__ ExpertMaps maps, const __grid_consta
         T* row = out + (int64_t)(it.t0 + c * 32) * p.ldc;
         const int count = it.count - c * 32;   // the same for all lanes
         if constexpr (kBf16) {
+          if (p.pieces_ok) {   // through the warp's staging memory: eight columns of one row a lane
+            uint32_t* box = reinterpret_cast<uint32_t*>(staging + (warp - kFirstEpilogue) * 2048);
+            const int odd = lane & 1, first = n - lane;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float got = __uint_as_float(__shfl_xor_sync(0xFFFFFFFFu, odd ? d[j] : d[j + 1], 1));
+              box[(j + odd) * 16 + lane / 2] = odd ? pack_bf16(got, __uint_as_float(d[j + 1])) : pack_bf16(__uint_as_float(d[j]), got);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int j = i * 8 + lane / 4, col = first + lane % 4 * 8;
+              const uint4 v = *reinterpret_cast<const uint4*>(box + j * 16 + lane % 4 * 4);
+              if (j >= count || col >= p.N) continue;
+              T* at = row + (int64_t)j * p.ldc + col;
+              if (col + 8 <= p.N) {
+                *reinterpret_cast<uint4*>(at) = v;
+              } else {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                  if (col + k < p.N) at[k] = (uint16_t)(w[k / 2] >> (16 * (k % 2)));
+              }
+            }
+            __syncwarp();
+            continue;
+          }
           if (p.pairs_ok) {   // two columns of one row a lane: even lanes the even rows, odd lanes the odd ones
             const int odd = lane & 1, col = n - odd;
 #pragma unroll
@@ -998,7 +1028,7 @@ ozk_status ozk_fp8_grouped_gemm(int64_t rows, int64_t N, int64_t K, const ozk_fp
   p.experts = (int)experts, p.rows = (int)rows;
   p.out = C, p.ldc = ldc, p.N = (int)N, p.tiles_n = (int)ceil_div(N, kLines), p.groups = (int)ceil_div(K, kGroupK);
   p.chunk = bf16 ? 4 * p.groups : 4 * kRangeGroups;
-  p.pairs_ok = aligned(C, 4) && ldc % 2 == 0, p.wide_ok = aligned(C, 8) && ldc % 4 == 0;
+  p.pairs_ok = aligned(C, 4) && ldc % 2 == 0, p.wide_ok = aligned(C, 8) && ldc % 4 == 0, p.pieces_ok = aligned(C, 16) && ldc % 8 == 0;
   p.clear = clear_rest;
   p.status = static_cast<StatusBlock*>(status);
   const ExpertRowsPlan few = expert_rows_plan(rows, experts, N, p.groups, bf16, sms);
