@@ -451,7 +451,8 @@ ozk_status ozk_rms_norm_backward(const ozk_rms_norm_backward_args* args, void* s
 
 /* Segments: rows lie in the order of the experts they belong to; expert e has rows offsets[e] .. offsets[e+1] - 1 (offsets: experts + 1 numbers in
  * device memory, ascending from offsets[0] >= 0 to offsets[experts] <= rows).  Segments may be empty; rows before the first and behind the last
- * belong to nobody.  Offsets that fall or leave the rows are read as the nearest that do not.  experts <= 1024 in products. */
+ * belong to nobody.  Offsets that fall or leave the rows are read as the nearest that do not.  experts <= 1024 in products.
+ * 128 x ozk_fp8_segment_blocks() is below 2^31 in ozk_fp8_quantize_segments and ozk_fp8_segment_gemm (OZK_ERR_UNSUPPORTED). */
 
 /* The operand of a product that sums over the rows of each expert: blocks of 128 rows that begin with each segment.  Block b of the segments has
  * rows 128 b .. 128 b + 127 of col_codes, with zeros behind the end of a segment, and scales as LINES (lines = cols, k = 128 x

@@ -1056,7 +1056,8 @@ ozk_status ozk_fp8_segment_gemm(int64_t experts, int64_t M, int64_t N, int64_t r
   if (experts < 0 || M < 0 || N < 0 || rows < 0 || !A || !B || (c_type != OZK_F32 && c_type != OZK_BF16) || ldc < N) return OZK_ERR_INVALID_ARG;
   if ((accumulate != 0 && accumulate != 1) || (experts > 1 && stride < (M - 1) * ldc + N)) return OZK_ERR_INVALID_ARG;
   const int64_t most = INT32_MAX - 1024;
-  if (rows > most || M > most || N > most || experts > kMostExperts || (accumulate && c_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
+  const int64_t blocks = ozk_fp8_segment_blocks(rows, experts);   // up to 127 rows an expert more than there are, and indexed by ints too
+  if (rows > most || blocks * kBlock > INT32_MAX || M > most || N > most || experts > kMostExperts || (accumulate && c_type != OZK_F32)) return OZK_ERR_UNSUPPORTED;
   if (experts == 0 || M == 0 || N == 0) return OZK_OK;
   const bool bf16 = c_type == OZK_BF16;
   const size_t size = bf16 ? 2 : 4;
@@ -1077,7 +1078,6 @@ ozk_status ozk_fp8_segment_gemm(int64_t experts, int64_t M, int64_t N, int64_t r
   const int sms = device_sm_count();
   if (sms < 2) return OZK_ERR_CUDA;
 
-  const int64_t blocks = ozk_fp8_segment_blocks(rows, experts);
   SegmentParams p = {};
   p.a = Operand{A->codes, A->ld, A->scales, OZK_SCALE_LINES, 1, (int)M, (int)blocks, 0};
   p.b = Operand{B->codes, B->ld, B->scales, OZK_SCALE_LINES, 1, (int)N, (int)blocks, 0};

@@ -424,9 +424,9 @@ ozk_status ozk_fp8_quantize_segments(int64_t rows, int64_t cols, const void* X, 
   if (segments < 0) return OZK_ERR_INVALID_ARG;
   if (segments > INT32_MAX - 1024) return OZK_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0 || segments == 0) return OZK_OK;
-  if (!offsets || (reinterpret_cast<uintptr_t>(offsets) & 3)) return OZK_ERR_INVALID_ARG;
   const int64_t blocks = ozk_fp8_segment_blocks(rows, segments);
-  if (blocks * ceil_div(cols, kBlock) > INT32_MAX) return OZK_ERR_UNSUPPORTED;
+  if (blocks * kBlock > INT32_MAX || blocks * ceil_div(cols, kBlock) > INT32_MAX) return OZK_ERR_UNSUPPORTED;   // rows of the blocks are ints too, up to 127 a segment more
+  if (!offsets || (reinterpret_cast<uintptr_t>(offsets) & 3)) return OZK_ERR_INVALID_ARG;
   if ((row_codes || row_scales) && !good_codes(row_codes, row_ld, cols, row_scales, 4)) return OZK_ERR_INVALID_ARG;
   if (!good_codes(col_codes, col_ld, cols, col_scales, 4)) return OZK_ERR_INVALID_ARG;
   if (!device_is_sm100()) return OZK_ERR_UNSUPPORTED;
