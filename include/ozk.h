@@ -478,7 +478,7 @@ typedef struct {
 
 /* C[t,n] = sum_k X(t,k) W_e(n,k) for the rows t of each expert e (X: rows x K, LINES, contract_rows = 0; C: rows x N), as ozk_fp8_gemm with that
  * expert's weights; input gradients have W's contract_rows = 1.  Rows of C outside the segments are left as they were, or cleared with
- * clear_rest = 1.  status: as for ozk_fp8_gemm_scratch.  No other memory is used. */
+ * clear_rest = 1.  status: as for ozk_fp8_gemm_scratch.  No other memory is used.  rows < 2^31 - 65536 (OZK_ERR_UNSUPPORTED). */
 ozk_status ozk_fp8_grouped_gemm(int64_t rows, int64_t N, int64_t K, const ozk_fp8_operand* X, const ozk_fp8_experts* W, int64_t experts,
                                 const int32_t* offsets, void* C, int c_type, int64_t ldc, int clear_rest, void* status, void* stream);
 

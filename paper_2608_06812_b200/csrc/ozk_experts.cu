@@ -970,6 +970,7 @@ ExpertRowsPlan expert_rows_plan(int64_t rows, int64_t experts, int64_t N, int gr
   return r;
 }
 
+constexpr int64_t kMostRows = INT32_MAX - 65536;   // rows are cleared in steps of 8 a multiprocessor, whose last one passes them
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 // Codes that a tensor map may be made of.
 bool good_operand(const uint8_t* codes, int64_t ld, const void* scales, int64_t cols, uintptr_t scale_align) {
@@ -993,7 +994,7 @@ ozk_status ozk_fp8_grouped_gemm(int64_t rows, int64_t N, int64_t K, const ozk_fp
   if (rows < 0 || N < 0 || K < 0 || experts < 0 || !X || !W || (c_type != OZK_F32 && c_type != OZK_BF16) || ldc < N) return OZK_ERR_INVALID_ARG;
   if ((clear_rest != 0 && clear_rest != 1) || (W->contract_rows != 0 && W->contract_rows != 1)) return OZK_ERR_INVALID_ARG;
   const int64_t most = INT32_MAX - 1024;
-  if (rows > most || N > most || K > most || experts > kMostExperts) return OZK_ERR_UNSUPPORTED;
+  if (rows > kMostRows || N > most || K > most || experts > kMostExperts) return OZK_ERR_UNSUPPORTED;
   if (rows == 0 || N == 0) return OZK_OK;
   const bool bf16 = c_type == OZK_BF16;
   const size_t size = bf16 ? 2 : 4;
