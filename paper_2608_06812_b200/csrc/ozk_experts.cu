@@ -889,7 +889,15 @@ segments_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 // Rows that belong to a segment (an empty sum), or those that do not, become zero: results of products over nothing.
 template <class T>
 __global__ void __launch_bounds__(256) clear_rows_kernel(const int* offsets, int experts, int rows, T* out, int64_t ldc, int N, int rest_too) {
-  const int begin = min(max(offsets[0], 0), rows), end = min(max(offsets[experts], begin), rows);
+  const int begin = min(max(offsets[0], 0), rows);
+  int end = begin;   // the largest offset within the rows: segments lie side by side up to it
+  for (int e = threadIdx.x; e < experts; e += 256) end = max(end, min(offsets[e + 1], rows));
+  end = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)end);
+  __shared__ int ends[8];
+  if (threadIdx.x % 32 == 0) ends[threadIdx.x / 32] = end;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) end = max(end, ends[i]);
   for (int r = blockIdx.x; r < rows; r += gridDim.x) {
     if (!rest_too && (r < begin || r >= end)) continue;
     for (int n = threadIdx.x; n < N; n += 256) out[(int64_t)r * ldc + n] = T(0);
