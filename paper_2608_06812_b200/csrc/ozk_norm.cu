@@ -40,7 +40,7 @@ __device__ __forceinline__ void codes_of(const float (&y)[kL], const float* reci
   for (int k = 0; k < kL / 4; ++k)
     c[k] = pack4(y[4 * k] * recip[4 * k * step], y[4 * k + 1] * recip[(4 * k + 1) * step], y[4 * k + 2] * recip[(4 * k + 2) * step], y[4 * k + 3] * recip[(4 * k + 3) * step]);
 }
-__device__ __forceinline__ float finite_or_nan(float y) { return y + (y - y); }
+__device__ __forceinline__ float finite_or_nan(float y) { return y - (y - y); }   // subtracted, so that a negative zero keeps its sign
 template <bool kFull, int kL>
 __device__ __forceinline__ void store_codes(uint8_t* p, int left, const uint32_t (&c)[kL / 4]) {
   if (kFull || left >= kL) {
