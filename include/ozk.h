@@ -396,11 +396,12 @@ ozk_status ozk_get_workspace_status(void* workspace, void* stream);
 /* RMS norm of x (rows x cols) with the residual stream r (of x_type, or OZK_F32) added first:
  *   h = x + r, rounded to the stream's type and written to total (the updated stream);  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
  * residual NULL: h = x, and total is not used.  total may be the residual (same ld), or x where the types agree: the stream is updated in place.
- * The norm is of h as it is stored.  weight: cols numbers.  FP32 arithmetic, sums in an order that depends on the sizes alone.
+ * The norm is of h as it is stored.  weight: cols numbers.  FP32 arithmetic; the order of a sum follows from the sizes, the types, how far the rows' places and strides
+ * let elements be read together, and the GPU's multiprocessors: the same call repeats its bits, one on rows at other places may differ in the last ones.
  *   root       optional, rows floats: s, which the backward pass reads (wanted where col_codes are)
  *   y          optional, rows x cols: y without quantisation, not in the place of h
  *   row_codes, row_scales / col_codes, col_scales   optional: y by 1 x 128 / 128 x 1 blocks, as by ozk_fp8_quantize_lines
- * Mean squares beyond FP32 count as infinite (s = 0).  A NaN or an infinity in a row makes NaN of the row's y (0 of what is finite beside an infinity).
+ * A sum of squares beyond FP32 (a mean square above 3.4e38 / cols) counts as infinite: s = 0, y = 0.  Squares below FP32 count as 0, which shows where eps is 0.  A NaN or an infinity in a row makes NaN of the row's y (0 of what is finite beside an infinity).
  * cols <= 32768.  rows, cols = 0 are allowed. */
 typedef struct {
   int64_t rows, cols;

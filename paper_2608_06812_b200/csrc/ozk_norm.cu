@@ -3,7 +3,7 @@
 //   h = round(x + r) in the type of r;  s = 1 / sqrt(mean(h^2) + eps);  y = h s w;  codes and scales of y as the quantiser's.
 //   g = dy w;  dx = dh + s (g - h s mean(g h s));  dw = sum over the rows of dy h s.
 // The norm is of h as it is stored, so that the backward pass, which reads h and s, differentiates what was computed.  Sums and all
-// arithmetic in FP32, in an order that depends on the sizes alone; y is rounded once, to its codes.
+// arithmetic in FP32, in an order that follows from sizes, types, alignment (which columns a lane holds) and the number of multiprocessors; y is rounded once, to its codes.
 //
 // Rows: a row lies over 1 to 16 warps, 512 columns (one word of scales) a warp and step.  A lane holds eight consecutive columns of each 256, or four of
 // each 128, so that 16 or 32 lanes hold a block.  Thread blocks stay and take row after row, the next ones already on their way to shared memory.

@@ -373,7 +373,8 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     """The RMS norm of x + residual, times `weight` [cols], as operands of the products: h = x + residual, s = 1 / sqrt(mean(h^2) + eps), h s weight.
     x [rows, cols] float32 or bfloat16; residual of the same type or float32, and h is rounded to it before it is normed.
     `rows`, `cols`: as for quantize_lines; `y`: whether (or where, but for the place of what is normed) the answer is wanted in the type of x too; `total`: where h is written (a new tensor if
-    None; may be `residual`, or x if of one type); `root`: whether (or where) s is wanted, float32 [rows], for rms_norm_backward."""
+    None; may be `residual`, or x if of one type); `root`: whether (or where) s is wanted, float32 [rows], for rms_norm_backward.
+    Rows whose sum of squares is beyond float32 count as infinite: s and the answer are 0."""
     r, c, kind, ld = _input(x)
     index = x.get_device()
     w_kind = _vector(weight, "weight", c, index)

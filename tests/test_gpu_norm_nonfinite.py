@@ -59,3 +59,15 @@ def test_rows_of_bfloat16_of_any_bits(rows, cols, shift):
     assert np.isfinite(y).all(1).any() and not np.isfinite(y).all()
     check_form(n.rows, y, "rows")
     check_form(n.cols, y, "cols")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [300, 4096, 20004])
+def test_sums_of_squares_at_the_end_of_float32(dtype, cols):
+    """Beyond it they count as infinite, whatever their mean; up to half of it the answer is the formula's."""
+    most = float(np.finfo(np.float32).max)
+    below, above = 2.0 ** np.floor(np.log2((most / 2 / cols) ** 0.5)), 2.0 ** np.ceil(np.log2((most * 2 / cols) ** 0.5))
+    x = torch.tensor([below, above], device="cuda").to(dtype)[:, None].repeat(1, cols)
+    n = lowbit.rms_norm(x, torch.ones(cols, device="cuda"), rows=True, cols=True, y=True, root=True)
+    assert (n.root[0] * below - 1).abs() <= 46 * U and (n.y[0] == 1).all() and (n.rows.dequantize()[0] == 1).all()
+    assert n.root[1] == 0 and (n.y[1] == 0).all() and (n.rows.dequantize()[1] == 0).all() and (n.cols.dequantize() == torch.tensor([[1.0], [0.0]], device="cuda")).all()
