@@ -957,8 +957,10 @@ int64_t most_tiles(int64_t rows, int64_t experts, int height) { return (rows + (
 
 // How experts_rows_kernel would run: NT rows a tile (0: it does not), `cluster` CTAs along K.  The host knows the mean of the rows of an expert, not how they lie.
 // It serves up to 8 rows an expert, and up to 64 where the pairs have too few tiles to be at work all.  Rows against pairs, us: 244 rows of 32 experts (4096 -> 2048) 46.6 : 51.9,
-// 64 of 8 (4096 -> 4096) 26.5 : 30.0, 8 of 64 (2048 -> 4096) 18.0 : 21.1, but 1000 of 64 (2048 -> 2048) 57.8 : 52.0.  K is split only while CTAs are
-// missing: 64 of 8 26.5, split by two 30.0; one row (4096 -> 4096) 14.9, split by eight 10.7.
+// 64 of 8 (4096 -> 4096) 26.5 : 30.0, 8 of 64 (2048 -> 4096) 18.0 : 21.1, but 1000 of 64 (2048 -> 2048) 57.8 : 52.0.  Between 8 and 16 rows an expert, nearly even ones, rows
+// against pairs: 320 of 32 (4096 -> 2048) 51.7 : 54.7, 160 of 16 (4096 -> 4096) 51.4 : 53.9, but 640 of 64 (2048 -> 4096) 106.8 : 95.4, 1280 of 128 (2048 -> 1024) 59.9 : 56.2: what
+// decides there is how many experts there are as much as their rows, within 12 % either way, so the limit stays at 8.
+// K is split only while CTAs are missing: 64 of 8 26.5, split by two 30.0; one row (4096 -> 4096) 14.9, split by eight 10.7.
 struct ExpertRowsPlan {
   int nt, cluster;
   int64_t tiles;

@@ -318,7 +318,7 @@ class _Linear(torch.autograd.Function):
 
 def linear(x: torch.Tensor, w: torch.Tensor, w8: Fp8Matrix | None = None) -> torch.Tensor:
     """x w^T in 8 bits, with gradients of x and w (formed from the same 8-bit weights and from the gradient's own 8-bit forms; gradients of these
-    gradients raise RuntimeError).
+    gradients raise RuntimeError, and so does a change of the answer in place where gradients are wanted).
     x: [..., inputs]; w: [outputs, inputs]; w8: quantize_tiles(w), where a program keeps it between steps (and leaves it as it is until
     the backward pass, which reads it for the gradient of x and raises RuntimeError if it has been written again)."""
     grads = torch.is_grad_enabled()   # a Function's needs_input_grad is set under no_grad too
@@ -498,7 +498,7 @@ def norm_linear(x: torch.Tensor, norm_weight: torch.Tensor, w: torch.Tensor, res
                 w8: Fp8Matrix | None = None) -> tuple[torch.Tensor, torch.Tensor]:
     """(norm(x + residual) w^T, x + residual): rms_norm and linear in 8 bits, with gradients of x, residual, norm_weight and w (gradients of these gradients
     raise RuntimeError).  x, residual: [..., inputs]; norm_weight: [inputs]; w: [outputs, inputs], all the layer's projections side by side; w8: as for `linear`.
-    Without a residual the second answer is x."""
+    Without a residual the second answer is x.  Where gradients are wanted the answers are not to be changed in place (RuntimeError): the stream is saved for the backward pass."""
     grads = torch.is_grad_enabled()
     need_n = grads and (x.requires_grad or norm_weight.requires_grad or (residual is not None and residual.requires_grad))
     need_w = grads and w.requires_grad
@@ -716,7 +716,7 @@ class _ExpertLinear(torch.autograd.Function):
 def expert_linear(x: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, w8: Fp8Experts | None = None) -> torch.Tensor:
     """x w_e^T in 8 bits, e the expert of each row, with gradients of x and w as `linear` has them.  x: [rows, inputs], rows in the order of the experts; w: [experts, outputs, inputs];
     offsets: int32 [experts + 1], ascending, on the GPU: expert e has rows offsets[e] .. offsets[e + 1] - 1.  Rows that belong to nobody answer zeros and get gradients of zero.
-    w8: quantize_experts(w), where a program keeps it between steps."""
+    w8: quantize_experts(w), where a program keeps it between steps.  Where gradients are wanted the answer is not to be changed in place (RuntimeError)."""
     if x.dim() != 2 or w.dim() != 3 or x.shape[1] != w.shape[2]:
         raise ValueError(f"x is [rows, inputs] and w [experts, outputs, inputs], not {tuple(x.shape)} and {tuple(w.shape)}")
     _offsets(offsets, w.shape[0], x.get_device())
