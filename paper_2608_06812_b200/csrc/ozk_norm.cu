@@ -10,7 +10,7 @@
 // Columns: blocks run along the rows, so a second kernel reads h again, tile by tile, with s known.
 //
 // Bound by memory where rows are long and aligned, and by instructions (about 20 an element) where they are read in words: 16384 x 4096 BF16 with a BF16 stream 82 us
-// by rows (5.7 TB/s), 122 us both ways; 4096 x 16384 FP32 144 us (6.1); 5003 x 4100 BF16 with an FP32 stream both ways 84 us; 8191 x 4097 BF16 by rows 109 us
+// by rows (5.7 TB/s), 125 us both ways; 4096 x 16384 FP32 144 us (6.1); 5003 x 4100 BF16 with an FP32 stream both ways 84 us; 8191 x 4097 BF16 by rows 109 us
 // (2.2 TB/s).  One row of 4096: 3.4 us on the GPU, 9 with the call.
 #include "ozk_norm.cuh"
 

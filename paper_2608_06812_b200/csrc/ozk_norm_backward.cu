@@ -1,5 +1,5 @@
 // The gradients of the RMS norm: g = dy w;  dx = dh + s (g - h s mean(g h s));  dw = sum over the rows of dy h s, in FP32.
-// Rows lie over warps as in the forward pass.  Bound by memory and by what a row's sum holds up: 16384 x 4096 BF16 108 us (5.0 TB/s), 8192 x 8192 FP32 200 us (5.4),
+// Rows lie over warps as in the forward pass.  Bound by memory and by what a row's sum holds up: 16384 x 4096 BF16 110 us (4.9 TB/s), 8192 x 8192 FP32 200 us (5.4),
 // 733 x 16384 FP32 with BF16 dy 50 us (3.4: one thread block a multiprocessor, whose rows have room for one more on its way), 8191 x 4097 BF16 190 us (instructions).
 #include "ozk_norm.cuh"
 
